@@ -276,7 +276,7 @@ static size_t full_plan(const ha_problem &p, const ha_feature_map *phi_q, const 
   return total;
 }
 
-static ha_status device_error(hipError_t e) {
+ha_status device_error(hipError_t e) {
   g_last_device_error = static_cast<int>(e);
   return HA_ERR_DEVICE;
 }

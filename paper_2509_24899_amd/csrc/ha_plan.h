@@ -125,6 +125,8 @@ static inline bool route_has_room(const Plan &pl, size_t base, size_t extra) {
 }
 void make_plan(const ha_problem &p, const ha_feature_map *phi_q, const ha_feature_map *phi_k, Plan &pl, size_t limit = SIZE_MAX);
 
+ha_status device_error(hipError_t e);   // HA_ERR_DEVICE; e is what hybrid_attn_last_device_error() reports on this thread
+
 // Kernel launchers (ha_kernels.hip).  Each enqueues on `st` and returns the launch status.
 hipError_t launch_weight_prep(const Plan &pl, const ha_feature_map &fm, bool is_query, void *ws, hipStream_t st);
 // prep_k (optional): the key-side map, whose weights are re-ordered in the same launch

@@ -1,0 +1,298 @@
+// Block-sparse attention, gfx950: the forward.
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i),   j over the keys of the blocks in the tile's list
+//
+// in one pass over the list: m_i follows the largest logit seen, and what has been summed is rescaled when it has moved far.  A workgroup takes
+// one tile of queries of one head, 32 queries to a wave, and walks the list 64 keys at a time; keys and values lie in LDS (two stages, the next on its way
+// while the current one is worked on) and every wave reads all of them.  Per wave and 32 keys: S^T = K Q^T on the matrix cores, exponentials,
+// O^T += V^T P^T with P straight from the registers that hold S.  The logits and the weights' sums are fp32; the weights are rounded to bf16 for
+// the second product only (fp32 tensors: all operands are hi + lo pairs, three products each).
+// Few tiles: the list is cut into ranges, a workgroup each, whose sums a second kernel joins.
+#include <cmath>
+
+#include "ha_sparse.h"
+
+namespace ha {
+namespace {
+
+struct FwdArgs {
+  Sparse s;
+  View q, k, v, out;          // bf16 (fp32 tensors: the hi images; lo stands lo_* elements behind)
+  int64_t lo_q, lo_k;
+  const int32_t *blocks;
+  float *lse;
+  int n_split;                // ranges of the list
+  float *po, *pm, *pl;        // n_split > 1: [n_split][B H N_q][D], [n_split][B H N_q]
+  float scale, scale_log2e;
+  unsigned items, share;
+};
+
+template <int D, int NS, int NW>
+__global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, STAGE = T::bytes(64);
+  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];      // [2 stages][k | v][hi, lo][64 rows]
+  const unsigned item = xcd_item(blockIdx.x, a.share);
+  if (item >= a.items) return;
+  const Sparse &s = a.s;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = item % a.n_split, t = item / a.n_split % s.T, bh = item / a.n_split / s.T, b = bh / s.H, h = bh % s.H, hk = h / s.G;
+  const int held = s.held(b), start = s.start(b);
+  const int q0 = t * s.qb + 32 * w, qi = q0 + r;      // this wave's first query, this lane's
+  const int tile_last = min((t + 1) * s.qb, s.Nq) - 1;
+  // keys that the tile, this wave's first query and this lane's query see
+  const int limit = s.causal ? min(held, start + tile_last + 1) : held;
+  const int wave_limit = s.causal ? min(held, start + q0 + 1) : held, row_limit = s.causal ? min(held, start + qi + 1) : held;
+  const int32_t *list = a.blocks + ((int64_t)(b * s.Hkv + hk) * s.T + t) * s.sel;
+  ListWalk walk(list, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
+
+  const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
+  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  auto request = [&](int key, int stage) {
+    char *to = lds + stage * (2 * NS * STAGE);
+    const int rows = min(limit - key, 64);
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      request_rows<D, 64, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.lo_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
+      request_rows<D, 64, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.lo_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
+    }
+  };
+  int key = walk.next();
+  if (key >= 0) request(key, 0);
+
+  bf16x8 qf[KS][NS];
+  {
+    const int64_t at = b * a.q.sb + h * a.q.sh + (int64_t)min(qi, s.Nq - 1) * a.q.sn + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int n = 0; n < NS; ++n) qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (at + n * a.lo_q + 16 * ks) * 2);
+  }
+  const float c = a.scale_log2e;
+  float m = -INFINITY, l = 0.f;                       // this query's largest logit (lagging, see below), its sum of weights (this lane's keys)
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+
+  for (int stage = 0; key >= 0; stage ^= 1) {
+    const int next = walk.next();
+    landed();
+    if (next >= 0) request(next, stage ^ 1);
+    const char *tk = lds + stage * (2 * NS * STAGE), *tv = tk + NS * STAGE;
+    f32x16 sc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sc[i][x] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) kf[n] = T::rows(tk + n * STAGE, 32 * i, ks, lane);
+        sc[i] = mfma_split<NS>(kf, qf[ks], sc[i]);
+      }
+    }
+    if (key + 64 > wave_limit) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[i][x] = key + 32 * i + crow(x, g) < row_limit ? sc[i][x] : -INFINITY;
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[i][x]);
+    top = xhalf_max(top);
+    // the accumulators follow the maximum when some query's has moved by 8 in the exponent (weights stay below 2^8)
+    if (__any(top > m + 8.f / c)) {
+      const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : fast_exp2((m - to) * c);
+      l *= f;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+      m = to;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;    // (nothing seen yet: every logit is -infinity, every weight 0)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x8 p;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          p[x] = fast_exp2(__builtin_fmaf(sc[i][8 * u + x], c, -mc));
+          l += p[x];
+        }
+        bf16x8 pb[NS];
+        split8<NS>(p, pb);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          bf16x8 vf[NS];
+#pragma unroll
+          for (int n = 0; n < NS; ++n) vf[n] = T::cols(tv + n * STAGE, rb, 32 * i + 16 * u, lane);
+          o[rb] = mfma_split<NS>(vf, pb, o[rb]);
+        }
+      }
+    key = next;
+  }
+  l = xhalf_sum(l);
+  if (a.n_split > 1) {
+    const int64_t row = ((int64_t)range * s.B * s.H + bh) * s.Nq + qi;
+    if (qi < s.Nq) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int x4 = 0; x4 < 4; ++x4)
+          *reinterpret_cast<f32x4 *>(a.po + row * D + 32 * rb + 8 * x4 + 4 * g) = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+      if (g == 0) {
+        a.pm[row] = m;
+        a.pl[row] = l;
+      }
+    }
+    return;
+  }
+  if (a.lse && g == 0 && qi < s.Nq) a.lse[(int64_t)bh * s.Nq + qi] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
+  __syncthreads();                                    // the stages become the staging area of the stores
+  constexpr int ESZ = NS == 2 ? 4 : 2;
+  store_rows<D, NS == 2>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, NS == 2>(), a.out.p + (b * a.out.sb + h * a.out.sh) * ESZ, a.out.sn * ESZ,
+                         q0, min((t + 1) * s.qb, s.Nq), lane);
+}
+
+// Joins the ranges of a row: D / 4 threads to a row.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void sparse_join_kernel(FwdArgs a) {
+  constexpr int TPR = D / 4;
+  const Sparse &s = a.s;
+  const int64_t rows = (int64_t)s.B * s.H * s.Nq, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (row >= rows) return;
+  const int c4 = 4 * (threadIdx.x % TPR);
+  float m = -INFINITY;
+  for (int i = 0; i < a.n_split; ++i) m = fmaxf(m, a.pm[i * rows + row]);
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < a.n_split; ++i) {
+    const float mi = a.pm[i * rows + row];
+    const float f = mi == -INFINITY ? 0.f : fast_exp2((mi - m) * a.scale_log2e);
+    const float li = a.pl[i * rows + row];
+    // (a range that saw nothing has l = 0; a NaN in it has to show)
+    l += mi == -INFINITY ? li : li * f;
+    o += *reinterpret_cast<const f32x4 *>(a.po + (i * rows + row) * D + c4) * f;
+  }
+  const int b = (int)(row / s.Nq / s.H), h = (int)(row / s.Nq % s.H), n = (int)(row % s.Nq);
+  if (a.lse && c4 == 0) a.lse[row] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
+  o *= l == 0.f ? 0.f : 1.f / l;
+  const int64_t at = b * a.out.sb + h * a.out.sh + n * a.out.sn + c4;
+  if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out.p) + at) = o;
+  else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(a.out.p) + at) = __builtin_convertvector(o, bf16x4);
+}
+
+struct FwdPlan {
+  int n_split;
+  size_t off_q, off_k, off_v, off_po, off_pm, off_pl, total;
+};
+
+FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
+  FwdPlan f{};
+  const int64_t tiles = (int64_t)s.B * s.H * s.T;
+  f.n_split = 1;
+  if (tiles > 0 && tiles < 512) {
+    const int64_t want = (512 + tiles - 1) / tiles, most = (s.sel + 1) / 2;
+    f.n_split = (int)(want < most ? want : most);
+    if (f.n_split > 32) f.n_split = 32;
+  }
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round256(bytes);
+    return here;
+  };
+  if (p.dtype == HA_F32) {
+    f.off_q = take((size_t)4 * s.B * s.H * s.Nq * p.d_head);
+    f.off_k = take((size_t)4 * s.B * s.Hkv * s.Nk * p.d_head);
+    f.off_v = take((size_t)4 * s.B * s.Hkv * s.Nk * p.d_head);
+  }
+  if (f.n_split > 1) {
+    const size_t rows = (size_t)f.n_split * s.B * s.H * s.Nq;
+    f.off_po = take(rows * p.d_head * 4);
+    f.off_pm = take(rows * 4);
+    f.off_pl = take(rows * 4);
+  }
+  f.total = at;
+  return f;
+}
+
+template <int D, int NS, int NW>
+hipError_t launch_fwd(const FwdArgs &a, hipStream_t st) {
+  sparse_fwd_kernel<D, NS, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace ha
+
+using namespace ha;
+
+extern "C" size_t hybrid_attn_sparse_workspace_bytes(const ha_sparse_problem *p) {
+  if (check_sparse(p) != HA_OK) return 0;
+  return plan_forward(*p, sparse_of(*p)).total;
+}
+
+extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, const ha_view *q, const ha_view *k, const ha_view *v, const int32_t *blocks,
+                                                const ha_view *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  ha_status st = check_sparse(p);
+  if (st != HA_OK) return st;
+  FwdArgs a{};
+  if ((st = check_view(*p, q, p->H, p->N_q, p->q_block, false, a.q)) != HA_OK || (st = check_view(*p, k, p->H_kv, p->N_k, p->k_block, false, a.k)) != HA_OK ||
+      (st = check_view(*p, v, p->H_kv, p->N_k, p->k_block, false, a.v)) != HA_OK || (st = check_view(*p, out, p->H, p->N_q, p->q_block, true, a.out)) != HA_OK)
+    return st;
+  if (p->N_q == 0) return HA_OK;
+  if (!blocks) return HA_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(blocks) & 3u || reinterpret_cast<uintptr_t>(lse) & 3u) return HA_ERR_ALIGN;
+  const Sparse s = a.s = sparse_of(*p);
+  const FwdPlan f = plan_forward(*p, s);
+  if (f.total > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < f.total)) return HA_ERR_WORKSPACE;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  char *ws = static_cast<char *>(workspace);
+  hipError_t e;
+  const int d = p->d_head;
+  const bool f32 = p->dtype == HA_F32;
+  if (f32) {
+    const SplitJob jobs[3] = {{a.q, reinterpret_cast<__bf16 *>(ws + f.off_q), s.H, s.Nq}, {a.k, reinterpret_cast<__bf16 *>(ws + f.off_k), s.Hkv, s.Nk},
+                              {a.v, reinterpret_cast<__bf16 *>(ws + f.off_v), s.Hkv, s.Nk}};
+    if ((e = launch_split(s, d, jobs, 3, stream)) != hipSuccess) return device_error(e);
+    a.q = split_view(jobs[0], d);
+    a.k = split_view(jobs[1], d);
+    a.v = split_view(jobs[2], d);
+    a.lo_q = (int64_t)s.B * s.H * s.Nq * d;
+    a.lo_k = (int64_t)s.B * s.Hkv * s.Nk * d;
+  }
+  a.blocks = blocks;
+  a.lse = lse;
+  a.n_split = f.n_split;
+  a.po = reinterpret_cast<float *>(ws + f.off_po);
+  a.pm = reinterpret_cast<float *>(ws + f.off_pm);
+  a.pl = reinterpret_cast<float *>(ws + f.off_pl);
+  a.scale = p->softmax_scale;
+  a.scale_log2e = p->softmax_scale * kLog2e;
+  a.items = (unsigned)((int64_t)s.B * s.H * s.T * f.n_split);
+  a.share = xcd_share(a.items);
+  if (d == 128) {
+    if (f32) e = s.qb == 128 ? launch_fwd<128, 2, 4>(a, stream) : launch_fwd<128, 2, 2>(a, stream);
+    else e = s.qb == 128 ? launch_fwd<128, 1, 4>(a, stream) : launch_fwd<128, 1, 2>(a, stream);
+  } else {
+    if (f32) e = s.qb == 128 ? launch_fwd<64, 2, 4>(a, stream) : launch_fwd<64, 2, 2>(a, stream);
+    else e = s.qb == 128 ? launch_fwd<64, 1, 4>(a, stream) : launch_fwd<64, 1, 2>(a, stream);
+  }
+  if (e != hipSuccess) return device_error(e);
+  if (f.n_split > 1) {
+    const unsigned blocks_j = (unsigned)(((int64_t)s.B * s.H * s.Nq + 256 / (d / 4) - 1) / (256 / (d / 4)));
+    if (d == 128) { if (f32) sparse_join_kernel<128, true><<<blocks_j, 256, 0, stream>>>(a); else sparse_join_kernel<128, false><<<blocks_j, 256, 0, stream>>>(a); }
+    else { if (f32) sparse_join_kernel<64, true><<<blocks_j, 256, 0, stream>>>(a); else sparse_join_kernel<64, false><<<blocks_j, 256, 0, stream>>>(a); }
+    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+  }
+  return HA_OK;
+}

@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import importlib
 import importlib.machinery
 import importlib.util
 import inspect
@@ -124,6 +125,10 @@ def _lib():
         lib.hybrid_attn_param_update.argtypes = [ctypes.POINTER(ha_optimizer), ctypes.c_size_t, vp, vp, vp, vp, vp,
                                                  ctypes.c_int32, vp]
         lib.hybrid_attn_param_update.restype = ctypes.c_int
+        from . import block_sparse, optim
+        for name, arguments, result in (*block_sparse.SIGNATURES, *optim.SIGNATURES):
+            function = getattr(lib, name)
+            function.argtypes, function.restype = arguments, result
         lib.hybrid_attn_abi_version.argtypes = []
         lib.hybrid_attn_abi_version.restype = ctypes.c_int
         _LIB = lib
@@ -292,6 +297,15 @@ def _alloc_on(stream):
     caching allocator ties the block to the stream the kernels run on (a block allocated under another stream could be
     handed out again while they still run)."""
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _on_device(device):
+    """Context in which `device` is the current GPU: the C ABI launches on the current one."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _on_device_of(tensor):
+    return _on_device(tensor.device)
 
 
 def _stream_handle(stream, tensor) -> int:
@@ -641,3 +655,21 @@ def device_inputs(w, device="cuda"):
     def fm(m):
         return FeatureMap(m["w1"], m["b1"], m["w2"], m["b2"], w.poly_degree, w_mid=m.get("w_mid"), b_mid=m.get("b_mid"))
     return q, k, v, fm(mq), fm(mk)
+
+
+# The calls of include/hybrid_attn_sparse.h and include/hybrid_attn_optim.h, under the names that their modules (which import this one) give them.
+_ELSEWHERE = {
+    "block_sparse": ("ha_sparse_problem", "ha_view", "make_sparse_problem", "hybrid_attn_sparse_validate", "hybrid_attn_key_means",
+                     "hybrid_attn_select_workspace_bytes", "hybrid_attn_select_blocks", "hybrid_attn_sparse_workspace_bytes", "hybrid_attn_sparse_forward",
+                     "hybrid_attn_sparse_grad_workspace_bytes", "hybrid_attn_sparse_grad"),
+    "optim": ("ha_tensor", "ha_param", "TensorList", "ParamList", "hybrid_attn_grad_norm_workspace_bytes", "hybrid_attn_grad_norm", "hybrid_attn_grad_clip",
+              "hybrid_attn_param_update_many"),
+}
+
+
+def __getattr__(name):
+    for module, names in _ELSEWHERE.items():
+        if name in names:
+            globals()[name] = value = getattr(importlib.import_module(f".{module}", __package__), name)
+            return value
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
