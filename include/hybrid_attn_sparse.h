@@ -32,8 +32,8 @@ typedef struct ha_sparse_problem {
   int32_t B, H, H_kv;     /* H a multiple of H_kv */
   int32_t N_q, N_k;       /* 0 is allowed: no queries, or no keys */
   int32_t d_head;         /* 64 or 128 */
-  int32_t dtype;          /* ha_dtype of q, k, v, out and their gradients.  HA_F32 tensors are split into two bf16 values each and multiplied with
-                             fp32 accumulation in three products (about 16 bits of precision), they are not rounded to bf16. */
+  int32_t dtype;          /* ha_dtype of q, k, v, out and their gradients.  HA_F32 tensors are not rounded to bf16: every value is
+                             split into three bf16 ones and multiplied in six products with fp32 accumulation, about fp32's own precision. */
   int32_t q_block, k_block;   /* 64 or 128 each */
   int32_t n_select;       /* length of a list, 1 .. 2^20 */
   int32_t causal;         /* 0 or 1 */

@@ -87,26 +87,31 @@ static __device__ __forceinline__ void landed() {
   __syncthreads();
 }
 
-// hi + lo bf16 pieces of eight fp32 values (NSPLIT 2) or their rounding alone.
-template <int NSPLIT>
-static __device__ __forceinline__ void split8(const f32x8 &x, bf16x8 (&out)[NSPLIT]) {
-  out[0] = __builtin_convertvector(x, bf16x8);
-  if constexpr (NSPLIT == 2) {
-    f32x8 rest;
+// bf16 pieces of eight fp32 values: each the rounding of what the ones before it leave.  Three hold all 24 bits.
+template <int NS>
+static __device__ __forceinline__ void split8(f32x8 x, bf16x8 (&out)[NS]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = x[i] - static_cast<float>(out[0][i]);
-    out[1] = __builtin_convertvector(rest, bf16x8);
+  for (int n = 0; n < NS; ++n) {
+    out[n] = __builtin_convertvector(x, bf16x8);
+    if (n + 1 < NS)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] -= static_cast<float>(out[n][i]);
   }
 }
-// a b with both as hi + lo: hi hi + hi lo + lo hi (lo lo is below the last bit kept), small terms first.
-template <int NSPLIT>
-static __device__ __forceinline__ f32x16 mfma_split(const bf16x8 (&a)[NSPLIT], const bf16x8 (&b)[NSPLIT], f32x16 c) {
-  if constexpr (NSPLIT == 2) {
-    c = mfma32(a[1], b[0], c);
-    c = mfma32(a[0], b[1], c);
-  }
-  return mfma32(a[0], b[0], c);
+// a b with both in pieces, small terms first; of three pieces the products that stay below the last bit are left out (six of nine are formed).
+template <int NS>
+static __device__ __forceinline__ f32x16 mfma_split(const bf16x8 (&a)[NS], const bf16x8 (&b)[NS], f32x16 c) {
+#pragma unroll
+  for (int order = NS - 1; order >= 0; --order)
+#pragma unroll
+    for (int n = 0; n <= order; ++n) c = mfma32(a[order - n], b[n], c);
+  return c;
 }
+// Pieces of a tensor, and rows that lie in LDS at a time (two stages of keys and values, or of queries and gradients, have to fit).
+template <bool F32>
+struct Pieces {
+  static constexpr int N = F32 ? 3 : 1, ROWS = F32 ? 32 : 64;
+};
 
 // Writes a 32-row tile held as C^T (NB blocks of 32 columns; the row is the lane's) times `f` through `stage` (this wave's own LDS, 32 rows
 // of D values and 16 bytes) to rows first .. of `out`, those below `limit`.
@@ -140,13 +145,14 @@ static __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], flo
 template <int D, bool F32>
 static constexpr int store_bytes() { return 32 * ((F32 ? D / 2 * 4 : D * 2) + 16); }
 
-// Walks a list 64 keys at a time: the steps whose keys someone in the tile may see.
+// Walks a list STEP keys at a time: the steps whose keys someone in the tile may see.
+template <int STEP>
 struct ListWalk {
   const int32_t *list;
   int at, end, sub, subs, Tk, kb, limit, lane, held_from;
   int entry;                  // lane l: list[held_from + l]
   __device__ __forceinline__ ListWalk(const int32_t *l, int lo, int hi, const Sparse &s, int lim, int lane_)
-      : list(l), at(lo), end(hi), sub(0), subs(s.kb >> 6), Tk(s.Tk), kb(s.kb), limit(lim), lane(lane_), held_from(lo) { fetch(); }
+      : list(l), at(lo), end(hi), sub(0), subs(s.kb / STEP), Tk(s.Tk), kb(s.kb), limit(lim), lane(lane_), held_from(lo) { fetch(); }
   __device__ __forceinline__ void fetch() { entry = held_from + lane < end ? list[held_from + lane] : -1; }
   // first key of the next step, or -1
   __device__ __forceinline__ int next() {
@@ -155,7 +161,7 @@ struct ListWalk {
         held_from = at;
         fetch();
       }
-      const int j = __builtin_amdgcn_readlane(entry, at - held_from), key = j * kb + 64 * sub;
+      const int j = __builtin_amdgcn_readlane(entry, at - held_from), key = j * kb + STEP * sub;
       if (++sub == subs) {
         sub = 0;
         ++at;
@@ -177,7 +183,7 @@ ha_status check_sparse(const ha_sparse_problem *p);
 ha_status check_view(const ha_sparse_problem &p, const ha_view *v, int heads, int n, int block, bool written, View &out);
 Sparse sparse_of(const ha_sparse_problem &p);
 static inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-// hi and lo bf16 images of an fp32 view, contiguous [2][B, heads, N, d]; `out` is the view of hi, lo stands B heads N d elements behind.
+// The three bf16 images of an fp32 view, contiguous [3][B, heads, N, d]; split_view is that of the first.
 struct SplitJob {
   View in;
   __bf16 *out;

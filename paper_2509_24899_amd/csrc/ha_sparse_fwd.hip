@@ -3,10 +3,10 @@
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i),   j over the keys of the blocks in the tile's list
 //
 // in one pass over the list: m_i follows the largest logit seen, and what has been summed is rescaled when it has moved far.  A workgroup takes
-// one tile of queries of one head, 32 queries to a wave, and walks the list 64 keys at a time; keys and values lie in LDS (two stages, the next on its way
+// one tile of queries of one head, 32 queries to a wave, and walks the list 64 keys at a time (fp32: 32); keys and values lie in LDS (two stages, the next on its way
 // while the current one is worked on) and every wave reads all of them.  Per wave and 32 keys: S^T = K Q^T on the matrix cores, exponentials,
 // O^T += V^T P^T with P straight from the registers that hold S.  The logits and the weights' sums are fp32; the weights are rounded to bf16 for
-// the second product only (fp32 tensors: all operands are hi + lo pairs, three products each).
+// the second product only (fp32 tensors: all operands are three bf16 pieces, six products each).
 // Few tiles: the list is cut into ranges, a workgroup each, whose sums a second kernel joins.
 #include <cmath>
 
@@ -17,8 +17,8 @@ namespace {
 
 struct FwdArgs {
   Sparse s;
-  View q, k, v, out;          // bf16 (fp32 tensors: the hi images; lo stands lo_* elements behind)
-  int64_t lo_q, lo_k;
+  View q, k, v, out;          // bf16 (fp32 tensors: the first pieces; the next stand piece_* elements behind)
+  int64_t piece_q, piece_k;
   const int32_t *blocks;
   float *lse;
   int n_split;                // ranges of the list
@@ -27,11 +27,11 @@ struct FwdArgs {
   unsigned items, share;
 };
 
-template <int D, int NS, int NW>
-__global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
+template <int D, bool F32, int NW>
+__global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, STAGE = T::bytes(64);
-  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];      // [2 stages][k | v][hi, lo][64 rows]
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
+  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];      // [2 stages][k | v][pieces][ROWS]
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -44,17 +44,17 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
   const int limit = s.causal ? min(held, start + tile_last + 1) : held;
   const int wave_limit = s.causal ? min(held, start + q0 + 1) : held, row_limit = s.causal ? min(held, start + qi + 1) : held;
   const int32_t *list = a.blocks + ((int64_t)(b * s.Hkv + hk) * s.T + t) * s.sel;
-  ListWalk walk(list, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
+  ListWalk<ROWS> walk(list, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
 
   const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
   auto request = [&](int key, int stage) {
     char *to = lds + stage * (2 * NS * STAGE);
-    const int rows = min(limit - key, 64);
+    const int rows = min(limit - key, ROWS);
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      request_rows<D, 64, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.lo_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
-      request_rows<D, 64, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.lo_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.piece_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.piece_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
     }
   };
   int key = walk.next();
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int n = 0; n < NS; ++n) qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (at + n * a.lo_q + 16 * ks) * 2);
+      for (int n = 0; n < NS; ++n) qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (at + n * a.piece_q + 16 * ks) * 2);
   }
   const float c = a.scale_log2e;
   float m = -INFINITY, l = 0.f;                       // this query's largest logit (lagging, see below), its sum of weights (this lane's keys)
@@ -81,9 +81,9 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
     landed();
     if (next >= 0) request(next, stage ^ 1);
     const char *tk = lds + stage * (2 * NS * STAGE), *tv = tk + NS * STAGE;
-    f32x16 sc[2];
+    f32x16 sc[ROWS / 32];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ROWS / 32; ++i) {
 #pragma unroll
       for (int x = 0; x < 16; ++x) sc[i][x] = 0.f;
 #pragma unroll
@@ -94,15 +94,15 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
         sc[i] = mfma_split<NS>(kf, qf[ks], sc[i]);
       }
     }
-    if (key + 64 > wave_limit) {
+    if (key + ROWS > wave_limit) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < ROWS / 32; ++i)
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[i][x] = key + 32 * i + crow(x, g) < row_limit ? sc[i][x] : -INFINITY;
     }
     float top = sc[0][0];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < ROWS / 32; ++i)
 #pragma unroll
       for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[i][x]);
     top = xhalf_max(top);
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
     }
     const float mc = m == -INFINITY ? 0.f : m * c;    // (nothing seen yet: every logit is -infinity, every weight 0)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < ROWS / 32; ++i)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x8 p;
@@ -157,8 +157,8 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_fw
   }
   if (a.lse && g == 0 && qi < s.Nq) a.lse[(int64_t)bh * s.Nq + qi] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
   __syncthreads();                                    // the stages become the staging area of the stores
-  constexpr int ESZ = NS == 2 ? 4 : 2;
-  store_rows<D, NS == 2>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, NS == 2>(), a.out.p + (b * a.out.sb + h * a.out.sh) * ESZ, a.out.sn * ESZ,
+  constexpr int ESZ = F32 ? 4 : 2;
+  store_rows<D, F32>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, F32>(), a.out.p + (b * a.out.sb + h * a.out.sh) * ESZ, a.out.sn * ESZ,
                          q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
@@ -211,9 +211,9 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
     return here;
   };
   if (p.dtype == HA_F32) {
-    f.off_q = take((size_t)4 * s.B * s.H * s.Nq * p.d_head);
-    f.off_k = take((size_t)4 * s.B * s.Hkv * s.Nk * p.d_head);
-    f.off_v = take((size_t)4 * s.B * s.Hkv * s.Nk * p.d_head);
+    f.off_q = take((size_t)6 * s.B * s.H * s.Nq * p.d_head);
+    f.off_k = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
+    f.off_v = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
   }
   if (f.n_split > 1) {
     const size_t rows = (size_t)f.n_split * s.B * s.H * s.Nq;
@@ -225,9 +225,9 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
   return f;
 }
 
-template <int D, int NS, int NW>
+template <int D, bool F32, int NW>
 hipError_t launch_fwd(const FwdArgs &a, hipStream_t st) {
-  sparse_fwd_kernel<D, NS, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  sparse_fwd_kernel<D, F32, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -267,8 +267,8 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
     a.q = split_view(jobs[0], d);
     a.k = split_view(jobs[1], d);
     a.v = split_view(jobs[2], d);
-    a.lo_q = (int64_t)s.B * s.H * s.Nq * d;
-    a.lo_k = (int64_t)s.B * s.Hkv * s.Nk * d;
+    a.piece_q = (int64_t)s.B * s.H * s.Nq * d;
+    a.piece_k = (int64_t)s.B * s.Hkv * s.Nk * d;
   }
   a.blocks = blocks;
   a.lse = lse;
@@ -281,11 +281,11 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   a.items = (unsigned)((int64_t)s.B * s.H * s.T * f.n_split);
   a.share = xcd_share(a.items);
   if (d == 128) {
-    if (f32) e = s.qb == 128 ? launch_fwd<128, 2, 4>(a, stream) : launch_fwd<128, 2, 2>(a, stream);
-    else e = s.qb == 128 ? launch_fwd<128, 1, 4>(a, stream) : launch_fwd<128, 1, 2>(a, stream);
+    if (f32) e = s.qb == 128 ? launch_fwd<128, true, 4>(a, stream) : launch_fwd<128, true, 2>(a, stream);
+    else e = s.qb == 128 ? launch_fwd<128, false, 4>(a, stream) : launch_fwd<128, false, 2>(a, stream);
   } else {
-    if (f32) e = s.qb == 128 ? launch_fwd<64, 2, 4>(a, stream) : launch_fwd<64, 2, 2>(a, stream);
-    else e = s.qb == 128 ? launch_fwd<64, 1, 4>(a, stream) : launch_fwd<64, 1, 2>(a, stream);
+    if (f32) e = s.qb == 128 ? launch_fwd<64, true, 4>(a, stream) : launch_fwd<64, true, 2>(a, stream);
+    else e = s.qb == 128 ? launch_fwd<64, false, 4>(a, stream) : launch_fwd<64, false, 2>(a, stream);
   }
   if (e != hipSuccess) return device_error(e);
   if (f.n_split > 1) {

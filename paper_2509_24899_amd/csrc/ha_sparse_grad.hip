@@ -18,8 +18,8 @@ constexpr int kChunk = 16;       // tiles counted together while the inverse lis
 
 struct GradArgs {
   Sparse s;
-  View q, k, v, dout, dq, dk, dv;      // inputs bf16 (fp32 tensors: the hi images, lo stands lo_* elements behind)
-  int64_t lo_q, lo_k;
+  View q, k, v, dout, dq, dk, dv;      // inputs bf16 (fp32 tensors: the first pieces; the next stand piece_* elements behind)
+  int64_t piece_q, piece_k;
   const int32_t *blocks;
   const float *lse2, *delta;           // [B H][T qb]: lse log2 e (+infinity for rows that take no part), delta
   int32_t *hist;                       // [B Hkv][n_chunks][Tk]
@@ -154,10 +154,10 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
-template <int D, int NS, int NW>
-__global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
+template <int D, bool F32, int NW>
+__global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, STAGE = T::bytes(64);
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
   __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
@@ -169,16 +169,16 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_dq
   const int limit = s.causal ? min(held, start + min((t + 1) * s.qb, s.Nq)) : held;
   const int wave_limit = s.causal ? min(held, start + q0 + 1) : held, row_limit = s.causal ? min(held, start + qi + 1) : held;
   const int32_t *list = a.blocks + ((int64_t)(b * s.Hkv + hk) * s.T + t) * s.sel;
-  ListWalk walk(list, 0, s.sel, s, limit, lane);
+  ListWalk<ROWS> walk(list, 0, s.sel, s, limit, lane);
   const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
   auto request = [&](int key, int stage) {
     char *to = lds + stage * (2 * NS * STAGE);
-    const int rows = min(limit - key, 64);
+    const int rows = min(limit - key, ROWS);
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      request_rows<D, 64, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.lo_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
-      request_rows<D, 64, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.lo_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.piece_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.piece_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
     }
   };
   int key = walk.next();
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_dq
   for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (b * a.q.sb + h * a.q.sh + row * a.q.sn + n * a.lo_q + 16 * ks + 8 * g) * 2);
-      df[ks][n] = *reinterpret_cast<const bf16x8 *>(a.dout.p + (b * a.dout.sb + h * a.dout.sh + row * a.dout.sn + n * a.lo_q + 16 * ks + 8 * g) * 2);
+      qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (b * a.q.sb + h * a.q.sh + row * a.q.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
+      df[ks][n] = *reinterpret_cast<const bf16x8 *>(a.dout.p + (b * a.dout.sb + h * a.dout.sh + row * a.dout.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
     }
   const int64_t st = (int64_t)bh * s.T * s.qb + qi;
   const float lse2 = a.lse2[st], delta = a.delta[st], c = a.scale_log2e;
@@ -204,9 +204,9 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_dq
     landed();
     if (next >= 0) request(next, stage ^ 1);
     const char *tk = lds + stage * (2 * NS * STAGE), *tv = tk + NS * STAGE;
-    const bool mask = key + 64 > wave_limit;
+    const bool mask = key + ROWS > wave_limit;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ROWS / 32; ++i) {
       f32x16 sc, dp;
 #pragma unroll
       for (int x = 0; x < 16; ++x) sc[x] = dp[x] = 0.f;
@@ -246,19 +246,19 @@ __global__ __launch_bounds__(64 * NW, NS == 1 && NW == 4 ? 2 : 1) void sparse_dq
     key = next;
   }
   __syncthreads();
-  constexpr int ESZ = NS == 2 ? 4 : 2;
-  store_rows<D, NS == 2>(o, a.scale, lds + w * store_bytes<D, NS == 2>(), a.dq.p + (b * a.dq.sb + h * a.dq.sh) * ESZ, a.dq.sn * ESZ, q0,
+  constexpr int ESZ = F32 ? 4 : 2;
+  store_rows<D, F32>(o, a.scale, lds + w * store_bytes<D, F32>(), a.dq.p + (b * a.dq.sb + h * a.dq.sh) * ESZ, a.dq.sn * ESZ, q0,
                          min((t + 1) * s.qb, s.Nq), lane);
 }
 
 // ---- dK, dV ----------------------------------------------------------------------------------------------------------------
 // A workgroup takes one part of one key block's list: 32 keys to a wave, whose K and V stay in registers; 64 queries at a time lie in LDS, Q and dO,
 // read as rows for S = Q K^T and dP = dO V^T and as columns for dK^T += Q^T dS and dV^T += dO^T P.
-template <int D, int NS, int NW>
+template <int D, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, STAGE = T::bytes(64), STAT = 2 * 64 * 4;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * (2 * NS * STAGE + STAT)];      // [2 stages][q | dO][hi, lo][64 rows], lse2 | delta
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS), STAT = 2 * 64 * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * (2 * NS * STAGE + STAT)];      // [2 stages][q | dO][pieces][ROWS], lse2 | delta
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -271,14 +271,14 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
   const int32_t *list = a.inv + (int64_t)bh * s.T * s.sel;
   const int held = s.held(b), start = s.start(b);
   const int key0 = j * s.kb, k0 = key0 + 32 * w, ki = k0 + r;
-  // steps: (place in the list, head of the group, 64 queries of the tile)
-  const int subs = s.qb >> 6;
+  // steps: (place in the list, head of the group, ROWS queries of the tile)
+  const int subs = s.qb / ROWS;
   int at = first + part * kPart, end = min(at + kPart, last), head = 0, sub = 0;
   if (key0 >= held) at = end;
   struct Step { int h, row; };        // row < 0: none left
   auto next_step = [&]() {
     while (at < end) {
-      const Step st = {hk * s.G + head, __builtin_amdgcn_readfirstlane(list[at]) * s.qb + 64 * sub};
+      const Step st = {hk * s.G + head, __builtin_amdgcn_readfirstlane(list[at]) * s.qb + ROWS * sub};
       if (++sub == subs) {
         sub = 0;
         if (++head == s.G) {
@@ -287,18 +287,18 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
         }
       }
       // rows behind the last query, and (causal) all of whose rows stand before the block, take no part
-      if (st.row < s.Nq && !(s.causal && start + min(st.row + 63, s.Nq - 1) < key0)) return st;
+      if (st.row < s.Nq && !(s.causal && start + min(st.row + ROWS - 1, s.Nq - 1) < key0)) return st;
     }
     return Step{0, -1};
   };
   const int qsn = (int)a.q.sn * 2, dsn = (int)a.dout.sn * 2;
   auto request = [&](const Step &st, int stage) {
     char *to = lds + stage * (2 * NS * STAGE + STAT);
-    const int rows = min(s.Nq - st.row, 64);
+    const int rows = min(s.Nq - st.row, ROWS);
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      request_rows<D, 64, NW>(rows_rsrc<D>(a.q.p + (b * a.q.sb + st.h * a.q.sh + st.row * a.q.sn + n * a.lo_q) * 2, rows, qsn), qsn, to + n * STAGE, w, lane);
-      request_rows<D, 64, NW>(rows_rsrc<D>(a.dout.p + (b * a.dout.sb + st.h * a.dout.sh + st.row * a.dout.sn + n * a.lo_q) * 2, rows, dsn), dsn,
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(a.q.p + (b * a.q.sb + st.h * a.q.sh + st.row * a.q.sn + n * a.piece_q) * 2, rows, qsn), qsn, to + n * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(a.dout.p + (b * a.dout.sb + st.h * a.dout.sh + st.row * a.dout.sn + n * a.piece_q) * 2, rows, dsn), dsn,
                               to + (NS + n) * STAGE, w, lane);
     }
     if (w < 2) {
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
   for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      kf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.k.p + (b * a.k.sb + hk * a.k.sh + krow * a.k.sn + n * a.lo_k + 16 * ks + 8 * g) * 2);
-      vf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.v.p + (b * a.v.sb + hk * a.v.sh + krow * a.v.sn + n * a.lo_k + 16 * ks + 8 * g) * 2);
+      kf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.k.p + (b * a.k.sb + hk * a.k.sh + krow * a.k.sn + n * a.piece_k + 16 * ks + 8 * g) * 2);
+      vf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.v.p + (b * a.v.sb + hk * a.v.sh + krow * a.v.sn + n * a.piece_k + 16 * ks + 8 * g) * 2);
     }
   const float c = a.scale_log2e;
   f32x16 dk[RB], dv[RB];
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
     const float *lse2 = reinterpret_cast<const float *>(tq + 2 * NS * STAGE), *delta = lse2 + 64;
     const bool mask = k0 + 32 > held || (s.causal && start + cur.row < k0 + 31);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ROWS / 32; ++i) {
       f32x16 sc, dp;
 #pragma unroll
       for (int x = 0; x < 16; ++x) sc[x] = dp[x] = 0.f;
@@ -404,11 +404,11 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
     return;
   }
   __syncthreads();
-  constexpr int ESZ = NS == 2 ? 4 : 2;
-  char *stage = lds + w * store_bytes<D, NS == 2>();
-  store_rows<D, NS == 2>(dk, a.scale, stage, a.dk.p + (b * a.dk.sb + hk * a.dk.sh) * ESZ, a.dk.sn * ESZ, k0, s.Nk, lane);
+  constexpr int ESZ = F32 ? 4 : 2;
+  char *stage = lds + w * store_bytes<D, F32>();
+  store_rows<D, F32>(dk, a.scale, stage, a.dk.p + (b * a.dk.sb + hk * a.dk.sh) * ESZ, a.dk.sn * ESZ, k0, s.Nk, lane);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  store_rows<D, NS == 2>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * ESZ, a.dv.sn * ESZ, k0, s.Nk, lane);
+  store_rows<D, F32>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * ESZ, a.dv.sn * ESZ, k0, s.Nk, lane);
 }
 
 // Joins the parts of the blocks that have several: D / 4 threads to a row of dk or dv.
@@ -457,10 +457,10 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   };
   const size_t nq = (size_t)s.B * s.H * s.Nq * p.d_head, nk = (size_t)s.B * s.Hkv * s.Nk * p.d_head, hk = (size_t)s.B * s.Hkv;
   if (p.dtype == HA_F32) {
-    f.off_q = take(4 * nq);
-    f.off_k = take(4 * nk);
-    f.off_v = take(4 * nk);
-    f.off_do = take(4 * nq);
+    f.off_q = take(6 * nq);
+    f.off_k = take(6 * nk);
+    f.off_v = take(6 * nk);
+    f.off_do = take(6 * nq);
   }
   f.off_lse2 = take((size_t)s.B * s.H * s.T * s.qb * 4);
   f.off_delta = take((size_t)s.B * s.H * s.T * s.qb * 4);
@@ -476,25 +476,25 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   return f;
 }
 
-template <int D, int NS>
+template <int D, bool F32>
 hipError_t launch_grad(const ha_sparse_problem &p, GradArgs &a, hipStream_t st) {
   const Sparse &s = a.s;
   hipError_t e;
   if (s.Nq > 0) {
     a.items = (unsigned)((int64_t)s.B * s.H * s.T);
     a.share = xcd_share(a.items);
-    if (s.qb == 128) sparse_dq_kernel<D, NS, 4><<<8 * a.share, 256, 0, st>>>(a);
-    else sparse_dq_kernel<D, NS, 2><<<8 * a.share, 128, 0, st>>>(a);
+    if (s.qb == 128) sparse_dq_kernel<D, F32, 4><<<8 * a.share, 256, 0, st>>>(a);
+    else sparse_dq_kernel<D, F32, 2><<<8 * a.share, 128, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (s.Nk > 0) {
     a.items = (unsigned)((int64_t)s.B * s.Hkv * a.max_items);
     a.share = xcd_share(a.items);
-    if (s.kb == 128) sparse_dkv_kernel<D, NS, 4><<<8 * a.share, 256, 0, st>>>(a);
-    else sparse_dkv_kernel<D, NS, 2><<<8 * a.share, 128, 0, st>>>(a);
+    if (s.kb == 128) sparse_dkv_kernel<D, F32, 4><<<8 * a.share, 256, 0, st>>>(a);
+    else sparse_dkv_kernel<D, F32, 2><<<8 * a.share, 128, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.max_slots > 0) {
-      sparse_dkv_join_kernel<D, NS == 2><<<(unsigned)((int64_t)s.B * s.Hkv * s.Tk), 256, 0, st>>>(a);
+      sparse_dkv_join_kernel<D, F32><<<(unsigned)((int64_t)s.B * s.Hkv * s.Tk), 256, 0, st>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -553,8 +553,8 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
     a.k = split_view(jobs[1], d);
     a.v = split_view(jobs[2], d);
     a.dout = split_view(jobs[3], d);
-    a.lo_q = (int64_t)s.B * s.H * s.Nq * d;
-    a.lo_k = (int64_t)s.B * s.Hkv * s.Nk * d;
+    a.piece_q = (int64_t)s.B * s.H * s.Nq * d;
+    a.piece_k = (int64_t)s.B * s.Hkv * s.Nk * d;
   }
   a.blocks = blocks;
   a.lse2 = lse2;
@@ -584,7 +584,7 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
       if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
     }
   }
-  if (d == 128) e = f32 ? launch_grad<128, 2>(*p, a, stream) : launch_grad<128, 1>(*p, a, stream);
-  else e = f32 ? launch_grad<64, 2>(*p, a, stream) : launch_grad<64, 1>(*p, a, stream);
+  if (d == 128) e = f32 ? launch_grad<128, true>(*p, a, stream) : launch_grad<128, false>(*p, a, stream);
+  else e = f32 ? launch_grad<64, true>(*p, a, stream) : launch_grad<64, false>(*p, a, stream);
   return e == hipSuccess ? HA_OK : device_error(e);
 }

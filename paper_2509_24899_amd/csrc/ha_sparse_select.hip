@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256) void choose_kernel(const uint64_t *keys, int T
   for (int i = at + threadIdx.x; i < sel; i += 256) out[i] = -1;
 }
 
-// ---- fp32 tensors as two bf16 images -----------------------------------------------------------------------------------
+// ---- fp32 tensors as three bf16 images -----------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void split_kernel(Sparse s, SplitJob j) {
   constexpr int TPR = D / 8, RPB = 256 / TPR;
@@ -274,13 +274,13 @@ __global__ __launch_bounds__(256) void split_kernel(Sparse s, SplitJob j) {
   const f32x4 *p = reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(j.in.p) + b * j.in.sb + h * j.in.sh + n * j.in.sn + c);
   const f32x4 a = p[0], d = p[1];
   const f32x8 x = {a.x, a.y, a.z, a.w, d.x, d.y, d.z, d.w};
-  bf16x8 out[2];
-  split8<2>(x, out);
+  bf16x8 out[3];
+  split8<3>(x, out);
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (!__builtin_isfinite(x[i])) out[1][i] = static_cast<__bf16>(0.f);      // (inf - inf)
-  *reinterpret_cast<bf16x8 *>(j.out + row * D + c) = out[0];
-  *reinterpret_cast<bf16x8 *>(j.out + (rows + row) * D + c) = out[1];
+    if (!__builtin_isfinite(x[i])) out[1][i] = out[2][i] = static_cast<__bf16>(0.f);      // (inf - inf)
+#pragma unroll
+  for (int p3 = 0; p3 < 3; ++p3) *reinterpret_cast<bf16x8 *>(j.out + (p3 * rows + row) * D + c) = out[p3];
 }
 
 size_t sums_bytes(const Sparse &s, int d) { return round256((size_t)s.B * s.Hkv * s.T * d * 8); }

@@ -1,8 +1,9 @@
 """Block-sparse attention against the definition in 64 bits (oracle/block_sparse_oracle.py), at the sizes, masks and layouts where it can go wrong.
 
 Tolerances.  bf16: products of bf16 values are exact in fp32, so a logit is off by the fp32 sum alone (d terms, d 2^-24 of the sum of absolute terms); a
-weight or a term of the gradients is rounded to bf16 (2^-8 of its value) before it is multiplied, and the result is (2^-8).  fp32: an operand as
-hi + lo is off by 2^-16 of its value and the lo lo products are left out (2^-16), 3 2^-16 a product; weights and terms in the gradients are split likewise.
+weight or a term of the gradients is rounded to bf16 (2^-8 of its value) before it is multiplied, and the result is (2^-8).  fp32: an operand in three
+pieces of 8 bits is off by 2^-24 of its value, and the three products left out are 2^-24, 2^-24 and 2^-32 of theirs: 5 2^-24 a product; weights and terms in the
+gradients are split likewise.
 The oracle adds these up over the terms of every single result."""
 import numpy as np
 import pytest
@@ -16,7 +17,7 @@ pytestmark = pytest.mark.gpu
 
 def units(dtype, d):
     return dict(u=2.0 ** -8, u_logit=(d + 8) * 2.0 ** -24, u_out=2.0 ** -8) if dtype == torch.bfloat16 else \
-        dict(u=3 * 2.0 ** -16, u_logit=3 * 2.0 ** -16 + (d + 8) * 2.0 ** -24, u_out=2.0 ** -24)
+        dict(u=5 * 2.0 ** -24, u_logit=(5 + d + 8) * 2.0 ** -24, u_out=2.0 ** -24)
 
 
 def tokens(gen, B, H, N, d, dtype, layout="bhnd", gain=1.0):
