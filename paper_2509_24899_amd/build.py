@@ -25,6 +25,7 @@ FILE_FLAGS = {"ha_grad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "ha_grad256
               "ha_query_alone.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "ha_state.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "ha_linear.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
               "ha_linear256.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
               "ha_state256.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+              "ha_sparse_grad.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
               "ha_wide_mlp.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

@@ -4,7 +4,7 @@
 #include <stdint.h>
 
 #include "../../include/hybrid_attn_sparse.h"
-#include "ha_device.h"
+#include "ha_mlp128.h"
 #include "ha_plan.h"
 
 namespace ha {
@@ -33,6 +33,7 @@ static __device__ __forceinline__ unsigned xcd_item(unsigned id, unsigned share)
 // both ways of reading a tile spread over all banks: 16 consecutive rows of one piece (the operand whose rows are the tile's) fall into 16
 // different pieces of 256 bytes, and so do four consecutive rows of four neighbouring pieces (the transposed operand).  The tile is filled
 // with direct-to-LDS loads, where a lane's place in LDS is fixed, so the permutation is in the addresses the lanes read.
+static __device__ __forceinline__ unsigned lds_offset(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 template <int D>
 struct Tile {
   static constexpr int PIECES = D / 8, PITCH = 2 * D, ROWS_PER_CHUNK = 64 / PIECES;
@@ -43,17 +44,25 @@ struct Tile {
     else return ((row << 1) & 4) | ((row >> 2) & 3);
   }
   // Operand with the tile's rows as its rows: rows row0 + r, contraction slots (g, t) = columns 16 ks + 8 g + t ("natural").
-  static __device__ __forceinline__ bf16x8 rows(const char *tile, int row0, int ks, int lane) {
-    const int row = row0 + (lane & 31);
-    return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(
-        (const __attribute__((address_space(3))) char *)tile + row * PITCH + (((2 * ks + (lane >> 5)) ^ swz(row)) << 4));
-  }
   // Operand with the tile's columns 32 cb .. as its rows and its rows row0 .. row0 + 15 as the contraction, "chained" order.
-  static __device__ __forceinline__ bf16x8 cols(const char *tile, int cb, int row0, int lane) {
-    const int r0 = row0 + 4 * (lane >> 5) + ((lane & 15) >> 2), r1 = r0 + 8;
-    const int piece = 4 * cb + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), within = (lane & 1) * 8;
-    return join(ds_read_tr(tile, r0 * PITCH + ((piece ^ swz(r0)) << 4) + within),
-                ds_read_tr(tile, r1 * PITCH + ((piece ^ swz(r1)) << 4) + within));
+  // Both from a lane's address that is formed once for a tile (whose place in LDS is a multiple of PITCH): the piece is the low bits of the address, so
+  // that one exclusive or gives any other; row0 is a multiple of 16 and, like a distance between tiles (`further`), goes into the instruction.
+  static __device__ __forceinline__ unsigned rows_base(const char *tile, int lane) {
+    const int row = lane & 31;
+    return lds_offset(tile) + row * PITCH + (((lane >> 5) ^ swz(row)) << 4);
+  }
+  static __device__ __forceinline__ bf16x8 rows_at(unsigned base, int row0, int ks, int further = 0) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(static_cast<uintptr_t>((base ^ (ks << 5)) + row0 * PITCH + further));
+  }
+  static __device__ __forceinline__ unsigned cols_base(const char *tile, int lane) {
+    const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    return lds_offset(tile) + row * PITCH + ((piece ^ swz(row)) << 4) + (lane & 1) * 8;
+  }
+  static __device__ __forceinline__ bf16x8 cols_at(unsigned base, int cb, int row0, int further = 0) {
+    // (eight rows further down the permutation differs in piece bit 1)
+    const unsigned at = base ^ (cb << 6);
+    return join(__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>(at + row0 * PITCH + further))),
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>((at ^ 32) + (row0 + 8) * PITCH + further))));
   }
 };
 
@@ -66,7 +75,6 @@ static __device__ __forceinline__ i32x4 rows_rsrc(const char *base, int rows, in
   return i32x4{(int)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (int)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32) & 0xffff),
                (int)__builtin_amdgcn_readfirstlane(n), 0x00020000};
 }
-static __device__ __forceinline__ unsigned lds_offset(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
 // Requests the tile of ROWS rows described by `rsrc` into `lds`: one instruction moves 64 lanes x 16 bytes, the chunks are dealt round-robin
 // to the NW waves.  Completion is awaited by the caller (vmcnt), which then synchronises the workgroup.

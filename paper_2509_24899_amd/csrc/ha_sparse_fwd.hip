@@ -76,11 +76,12 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_k
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
 
+  const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
   for (int stage = 0; key >= 0; stage ^= 1) {
     const int next = walk.next();
     landed();
     if (next >= 0) request(next, stage ^ 1);
-    const char *tk = lds + stage * (2 * NS * STAGE), *tv = tk + NS * STAGE;
+    const unsigned rows = rows0 + stage * (2 * NS * STAGE), cols = cols0 + stage * (2 * NS * STAGE);
     f32x16 sc[ROWS / 32];
 #pragma unroll
     for (int i = 0; i < ROWS / 32; ++i) {
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_k
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 kf[NS];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) kf[n] = T::rows(tk + n * STAGE, 32 * i, ks, lane);
+        for (int n = 0; n < NS; ++n) kf[n] = T::rows_at(rows, 32 * i, ks, n * STAGE);
         sc[i] = mfma_split<NS>(kf, qf[ks], sc[i]);
       }
     }
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_k
         for (int rb = 0; rb < RB; ++rb) {
           bf16x8 vf[NS];
 #pragma unroll
-          for (int n = 0; n < NS; ++n) vf[n] = T::cols(tv + n * STAGE, rb, 32 * i + 16 * u, lane);
+          for (int n = 0; n < NS; ++n) vf[n] = T::cols_at(cols, rb, 32 * i + 16 * u, (NS + n) * STAGE);
           o[rb] = mfma_split<NS>(vf, pb, o[rb]);
         }
       }

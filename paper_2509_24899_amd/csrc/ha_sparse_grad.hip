@@ -7,13 +7,15 @@
 // key blocks along the tiles that chose them.  S and dP are formed in both (seven products for five; writing dQ's terms from the second pass
 // instead would be fp32 atomics, or T x n_select partial tiles in memory).  The inverse lists are built on the way: tiles in rising order for every key
 // block, by counting in chunks of tiles.  Popular blocks (a first block that every tile keeps) would leave one workgroup with thousands of
-// tiles, so a list is cut into parts of kPart tiles whose sums a last kernel joins in order.
+// tiles, so a list is cut into parts whose sums a last kernel joins in order.
+#include <climits>
+
 #include "ha_sparse.h"
 
 namespace ha {
 namespace {
 
-constexpr int kPart = 64;        // tiles of an inverse list that one workgroup takes
+constexpr int kPart = 64;        // tiles of an inverse list that one workgroup takes, at most
 constexpr int kChunk = 16;       // tiles counted together while the inverse lists are built
 
 struct GradArgs {
@@ -21,20 +23,21 @@ struct GradArgs {
   View q, k, v, dout, dq, dk, dv;      // inputs bf16 (fp32 tensors: the first pieces; the next stand piece_* elements behind)
   int64_t piece_q, piece_k;
   const int32_t *blocks;
-  const float *lse2, *delta;           // [B H][T qb]: lse log2 e (+infinity for rows that take no part), delta
+  const float *stat;                   // [B H][T qb / 32][2][32]: -lse / scale (-infinity for rows that take no part), -delta
   int32_t *hist;                       // [B Hkv][n_chunks][Tk]
   int32_t *first, *item0, *slot0;      // [B Hkv][Tk + 1]: a block's first place in inv, its first item and its first slot
   int32_t *inv;                        // [B Hkv][T sel] tiles
-  int32_t *item_block;                 // [B Hkv][max_items] block of an item, -1 behind the last
+  int2 *work;                          // items in the order of their launch: {block of all heads' blocks, part}
+  int32_t *n_work;                     // how many
   float *part;                         // [B Hkv][max_slots][dk | dv][kb][D]
-  int n_chunks, max_items, max_slots;
+  int n_chunks, max_items, max_slots, part_tiles;
   float scale, scale_log2e;
   unsigned items, share;
 };
 
 // ---- row statistics ----------------------------------------------------------------------------------------------------
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void sparse_delta_kernel(Sparse s, View out, View dout, const float *lse, float *lse2, float *delta) {
+__global__ __launch_bounds__(256) void sparse_delta_kernel(Sparse s, View out, View dout, const float *lse, float inv_scale, float *stat) {
   constexpr int TPR = D / 8, RPB = 256 / TPR;
   const int rows = s.T * s.qb;
   const int64_t at = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
@@ -59,8 +62,9 @@ __global__ __launch_bounds__(256) void sparse_delta_kernel(Sparse s, View out, V
   for (int i = TPR / 2; i > 0; i >>= 1) sum += __shfl_xor(sum, i);
   if (c == 0) {
     const float l = n < s.Nq ? lse[(int64_t)bh * s.Nq + n] : -INFINITY;
-    lse2[at] = l == -INFINITY ? INFINITY : l * kLog2e;
-    delta[at] = l == -INFINITY ? 0.f : sum;
+    float *to = stat + (at >> 5) * 64 + (at & 31);
+    to[0] = l == -INFINITY ? -INFINITY : -l * inv_scale;
+    to[32] = l == -INFINITY ? 0.f : -sum;
   }
 }
 
@@ -90,7 +94,6 @@ __global__ __launch_bounds__(1024) void inverse_scan_kernel(GradArgs a) {
   const int bh = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int32_t *h = a.hist + (int64_t)bh * a.n_chunks * s.Tk;
   int32_t *first = a.first + (int64_t)bh * (s.Tk + 1), *item0 = a.item0 + (int64_t)bh * (s.Tk + 1), *slot0 = a.slot0 + (int64_t)bh * (s.Tk + 1);
-  int32_t *item_block = a.item_block + (int64_t)bh * a.max_items;
   int3 base = {0, 0, 0};
   for (int j0 = 0; j0 < s.Tk; j0 += 1024) {
     const int j = j0 + threadIdx.x;
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(1024) void inverse_scan_kernel(GradArgs a) {
         h[(int64_t)c * s.Tk + j] = n;
         n += x;
       }
-    const int parts = j < s.Tk ? max(1, (n + kPart - 1) / kPart) : 0;
+    const int parts = j < s.Tk ? max(1, (n + a.part_tiles - 1) / a.part_tiles) : 0;
     const int3 mine = {n, parts, parts > 1 ? parts : 0};
     int3 sum = mine;
 #pragma unroll
@@ -123,7 +126,6 @@ __global__ __launch_bounds__(1024) void inverse_scan_kernel(GradArgs a) {
       first[j] = at.x;
       item0[j] = at.y;
       slot0[j] = at.z;
-      for (int i = 0; i < parts; ++i) item_block[at.y + i] = j;
     }
     base = all;
   }
@@ -132,7 +134,49 @@ __global__ __launch_bounds__(1024) void inverse_scan_kernel(GradArgs a) {
     item0[s.Tk] = base.y;
     slot0[s.Tk] = base.z;
   }
-  for (int i = base.y + threadIdx.x; i < a.max_items; i += 1024) item_block[i] = -1;
+}
+
+// The order of the work: head by head, and in a head the parts with the most tiles first.  Workgroups that run at the same time then walk lists of one length
+// over one head's tiles and stay side by side, which is what lets them share the tiles through the L2 of their XCD (a head's queries and gradients are
+// several times its size).  Parts of one length stand in no particular order: it decides nothing but when they run.
+__global__ __launch_bounds__(1024) void inverse_order_kernel(GradArgs a) {
+  const Sparse &s = a.s;
+  const int bh = blockIdx.x, heads = gridDim.x;
+  __shared__ int before[16], bucket[kPart + 1];
+  int n = 0;
+  for (int i = threadIdx.x; i < bh; i += 1024) n += a.item0[(int64_t)i * (s.Tk + 1) + s.Tk];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) n += __shfl_down(n, d);
+  if ((threadIdx.x & 63) == 0) before[threadIdx.x >> 6] = n;
+  if (threadIdx.x <= kPart) bucket[threadIdx.x] = 0;
+  __syncthreads();
+  const int32_t *first = a.first + (int64_t)bh * (s.Tk + 1);
+  for (int j = threadIdx.x; j < s.Tk; j += 1024) {
+    const int len = first[j + 1] - first[j];
+    if (len >= a.part_tiles) atomicAdd(&bucket[0], len / a.part_tiles);
+    if (len % a.part_tiles || len == 0) atomicAdd(&bucket[a.part_tiles - len % a.part_tiles], 1);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int at = 0;
+    for (int w = 0; w < 16; ++w) at += before[w];
+    for (int i = 0; i <= a.part_tiles; ++i) {
+      const int c = bucket[i];
+      bucket[i] = at;
+      at += c;
+    }
+    if (bh == heads - 1) *a.n_work = at;
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < s.Tk; j += 1024) {
+    const int len = first[j + 1] - first[j];
+    const int full = len / a.part_tiles;
+    if (full) {
+      const int at = atomicAdd(&bucket[0], full);
+      for (int i = 0; i < full; ++i) a.work[at + i] = int2{bh * s.Tk + j, i};
+    }
+    if (len % a.part_tiles || len == 0) a.work[atomicAdd(&bucket[a.part_tiles - len % a.part_tiles], 1)] = int2{bh * s.Tk + j, full};
+  }
 }
 
 // The tiles of a chunk one after the other, so that every block's list rises; the entries of one tile side by side (one that stands twice takes two
@@ -192,18 +236,19 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
       qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (b * a.q.sb + h * a.q.sh + row * a.q.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
       df[ks][n] = *reinterpret_cast<const bf16x8 *>(a.dout.p + (b * a.dout.sb + h * a.dout.sh + row * a.dout.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
     }
-  const int64_t st = (int64_t)bh * s.T * s.qb + qi;
-  const float lse2 = a.lse2[st], delta = a.delta[st], c = a.scale_log2e;
+  const float *st = a.stat + ((int64_t)bh * s.T * s.qb + q0) * 2 + r;
+  const float c = a.scale_log2e, minus_lse2 = st[0] * c, minus_delta = st[32];
   f32x16 o[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
   for (int stage = 0; key >= 0; stage ^= 1) {
     const int next = walk.next();
     landed();
     if (next >= 0) request(next, stage ^ 1);
-    const char *tk = lds + stage * (2 * NS * STAGE), *tv = tk + NS * STAGE;
+    const unsigned rows = rows0 + stage * (2 * NS * STAGE), cols = cols0 + stage * (2 * NS * STAGE);
     const bool mask = key + ROWS > wave_limit;
 #pragma unroll
     for (int i = 0; i < ROWS / 32; ++i) {
@@ -215,14 +260,14 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
         bf16x8 kf[NS], vf[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          kf[n] = T::rows(tk + n * STAGE, 32 * i, ks, lane);
-          vf[n] = T::rows(tv + n * STAGE, 32 * i, ks, lane);
+          kf[n] = T::rows_at(rows, 32 * i, ks, n * STAGE);
+          vf[n] = T::rows_at(rows, 32 * i, ks, (NS + n) * STAGE);
         }
         sc = mfma_split<NS>(kf, qf[ks], sc);
         dp = mfma_split<NS>(vf, df[ks], dp);
       }
 #pragma unroll
-      for (int x = 0; x < 16; ++x) sc[x] = fast_exp2(__builtin_fmaf(sc[x], c, -lse2)) * (dp[x] - delta);
+      for (int x = 0; x < 16; ++x) sc[x] = fast_exp2(__builtin_fmaf(sc[x], c, minus_lse2)) * (dp[x] + minus_delta);
       if (mask) {
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = key + 32 * i + crow(x, g) < row_limit ? sc[x] : 0.f;
@@ -238,7 +283,7 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
         for (int rb = 0; rb < RB; ++rb) {
           bf16x8 kf[NS];
 #pragma unroll
-          for (int n = 0; n < NS; ++n) kf[n] = T::cols(tk + n * STAGE, rb, 32 * i + 16 * u, lane);
+          for (int n = 0; n < NS; ++n) kf[n] = T::cols_at(cols, rb, 32 * i + 16 * u, n * STAGE);
           o[rb] = mfma_split<NS>(kf, db, o[rb]);
         }
       }
@@ -252,28 +297,209 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
 }
 
 // ---- dK, dV ----------------------------------------------------------------------------------------------------------------
-// A workgroup takes one part of one key block's list: 32 keys to a wave, whose K and V stay in registers; 64 queries at a time lie in LDS, Q and dO,
-// read as rows for S = Q K^T and dP = dO V^T and as columns for dK^T += Q^T dS and dV^T += dO^T P.
-template <int D, bool F32, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
+// A workgroup takes 64 keys of a block and one part of its list, 32 queries ("a chunk") of one head at a time: S = Q K^T, dP = dO V^T, then
+// dV^T += dO^T P and dK^T += Q^T dS with P and dS straight from the registers of the first two products.  Q and dO lie in LDS and are read both ways.
+
+// The statistics of a chunk to LDS.
+__device__ __forceinline__ void request_stat(const float *src, char *to, int lane) {
+  const unsigned l = __builtin_amdgcn_readfirstlane(lds_offset(to));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l), "v"(lane * 4), "s"(src) : "memory");
+}
+
+// Four waves: the halves of the keys by two chunks at a time.  Two workgroups to a CU, so that one's loads, waits and exponentials run under the other's
+// products; that leaves 256 registers to a wave: 128 for dK and dV, 32 for S and dP, K and half of V; the other half of V lies in LDS.  S starts from
+// -lse / scale and dP from -delta, so that exp2(c S) is P and P dP is dS.
+template <int D>
+__global__ __launch_bounds__(256, 2) void sparse_dkv_kernel(GradArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS), STAT = 2 * 64 * 4;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), CHUNK = 2 * TILE + 256, VKEEP = KS / 2, VROW = 64 * (KS - VKEEP) * 16;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * CHUNK + 2 * VROW];      // [stage][chunk][q | dO | statistics], [half of the keys][ks][lane] of v
+  const Sparse &s = a.s;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5, kh = w & 1, cg = w >> 1;
+  // (workgroups go to the eight XCDs in turn: the two halves of a block of 128 keys to one of them)
+  const int subs = s.kb >> 6, within = blockIdx.x % (8 * subs), half = within >> 3, item = blockIdx.x / (8 * subs) * 8 + (within & 7);
+  if (item >= *a.n_work) return;
+  const int2 work = a.work[item];
+  const int bh = work.x / s.Tk, j = work.x - bh * s.Tk, part = work.y, b = bh / s.Hkv, hk = bh % s.Hkv;
+  const int64_t at_j = (int64_t)bh * (s.Tk + 1) + j;
+  const int parts = a.item0[at_j + 1] - a.item0[at_j];
+  const int held = s.held(b), start = s.start(b), Nq = s.Nq, qb = s.qb, G = s.G;
+  const int key0 = j * s.kb + 64 * half, k0 = key0 + 32 * kh, ki = k0 + r;
+  const int first = a.first[at_j] + part * a.part_tiles, n = key0 < held ? min(a.first[at_j + 1] - first, a.part_tiles) : 0;
+  const int tile = lane < n ? a.inv[(int64_t)bh * s.T * s.sel + first + lane] : 0;      // (a part has at most 64 tiles)
+  const int per_head = qb >> 5, steps = (n * G * per_head) >> 1;                         // (2 or 4 chunks of a head in a tile)
+  const int qsn = (int)a.q.sn * 2, dsn = (int)a.dout.sn * 2;
+  const int64_t qsh = a.q.sh * 2, dsh = a.dout.sh * 2, ssh = (int64_t)s.T * qb * 8;
+  const char *qhead = a.q.p + (b * a.q.sb + hk * G * a.q.sh) * 2, *dhead = a.dout.p + (b * a.dout.sb + hk * G * a.dout.sh) * 2;
+  const char *shead = reinterpret_cast<const char *>(a.stat) + ((int64_t)b * s.H + hk * G) * ssh;
+  const int first_seen = s.causal ? key0 - start : INT_MIN;         // the first query that sees one of the keys
+  int e = 0, hd = 0, sub = cg;                        // place in the list, head of the group, chunk of the tile: of the next request
+  // Requests this wave's half of its next chunk and returns the chunk's first row, or -1: rows behind the last query, and (causal) chunks all of whose
+  // rows stand before the keys, take no part.
+  auto request = [&](int stage) {
+    int row = __builtin_amdgcn_readlane(tile, e) * qb + 32 * sub;
+    const int rows = min(Nq - row, 32);
+    if (rows <= 0 || row + rows <= first_seen) {
+      row = -1;
+    } else {
+      char *to = lds + (stage * 2 + cg) * CHUNK;
+      request_rows<D, 32, 2>(rows_rsrc<D>(qhead + (int64_t)row * qsn, rows, qsn), qsn, to, kh, lane);
+      request_rows<D, 32, 2>(rows_rsrc<D>(dhead + (int64_t)row * dsn, rows, dsn), dsn, to + TILE, kh, lane);
+      if (kh == 0) request_stat(reinterpret_cast<const float *>(shead + (int64_t)row * 8), to + 2 * TILE, lane);
+    }
+    sub += 2;
+    if (sub >= per_head) {
+      sub = cg;
+      ++hd;
+      qhead += qsh;
+      dhead += dsh;
+      shead += ssh;
+      if (hd == G) {
+        hd = 0;
+        ++e;
+        qhead -= G * qsh;
+        dhead -= G * dsh;
+        shead -= G * ssh;
+      }
+    }
+    return row;
+  };
+  bf16x8 *vrest = reinterpret_cast<bf16x8 *>(lds + 2 * 2 * CHUNK) + kh * (VROW / 16) + lane;
+  bf16x8 kf[KS], vf[VKEEP];
+  int row = -1;
+  if (steps > 0) {
+    row = request(0);
+    const char *kp = a.k.p + (b * a.k.sb + hk * a.k.sh + min(ki, s.Nk - 1) * a.k.sn + 8 * g) * 2, *vp = a.v.p + (b * a.v.sb + hk * a.v.sh + min(ki, s.Nk - 1) * a.v.sn + 8 * g) * 2;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[ks] = *reinterpret_cast<const bf16x8 *>(kp + 32 * ks);
+      const bf16x8 x = *reinterpret_cast<const bf16x8 *>(vp + 32 * ks);
+      if (ks < VKEEP) vf[ks] = x;
+      else if (cg == 0) vrest[(ks - VKEEP) * 64] = x;
+    }
+  }
+  const float c = a.scale_log2e;
+  f32x16 dk[RB], dv[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) dk[rb][x] = dv[rb][x] = 0.f;
+  const unsigned rows0 = T::rows_base(lds + cg * CHUNK, lane), cols0 = T::cols_base(lds + cg * CHUNK, lane);
+
+  for (int step = 0, stage = 0; step < steps; ++step, stage ^= 1) {
+    landed();
+    const int cur = row;
+    if (step + 1 < steps) row = request(stage ^ 1);
+    if (cur < 0) continue;
+    const unsigned rows = rows0 + stage * (2 * CHUNK), cols = cols0 + stage * (2 * CHUNK);
+    const float *stat = reinterpret_cast<const float *>(lds + (stage * 2 + cg) * CHUNK + 2 * TILE) + 4 * g;
+    f32x16 sc, dp;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) {
+      const f32x4 l4 = *reinterpret_cast<const f32x4 *>(stat + 8 * x4), d4 = *reinterpret_cast<const f32x4 *>(stat + 32 + 8 * x4);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        sc[4 * x4 + x] = l4[x];
+        dp[4 * x4 + x] = d4[x];
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sc = mfma32(T::rows_at(rows, 0, ks), kf[ks], sc);
+      dp = mfma32(T::rows_at(rows, 0, ks, TILE), ks < VKEEP ? vf[ks < VKEEP ? ks : 0] : vrest[(ks - VKEEP) * 64], dp);
+    }
+    if (k0 + 32 > held || cur < first_seen + 32 * kh + 31) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        // (rows behind the last query see what it sees)
+        const bool seen = ki < held && ki - key0 + first_seen <= min(cur + crow(x, g), Nq - 1);
+        sc[x] = seen ? sc[x] : -INFINITY;
+        dp[x] = seen ? dp[x] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 p8, d8;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        p8[x] = fast_exp2(sc[8 * u + x] * c);
+        d8[x] = p8[x] * dp[8 * u + x];
+      }
+      const bf16x8 pb = __builtin_convertvector(p8, bf16x8), db = __builtin_convertvector(d8, bf16x8);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        dv[rb] = mfma32(T::cols_at(cols, rb, 16 * u, TILE), pb, dv[rb]);
+        dk[rb] = mfma32(T::cols_at(cols, rb, 16 * u), db, dk[rb]);
+      }
+    }
+  }
+  // the other chunk's sums to the first's, as register images [dk | dv][lane] of each wave
+  f32x4 *image = reinterpret_cast<f32x4 *>(lds);
+  constexpr int IMAGE = 2 * RB * 4 * 64;
+  __syncthreads();
+  if (cg == 1) {
+    f32x4 *to = image + kh * IMAGE + lane;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        to[(rb * 4 + x4) * 64] = f32x4{dk[rb][4 * x4], dk[rb][4 * x4 + 1], dk[rb][4 * x4 + 2], dk[rb][4 * x4 + 3]};
+        to[((RB + rb) * 4 + x4) * 64] = f32x4{dv[rb][4 * x4], dv[rb][4 * x4 + 1], dv[rb][4 * x4 + 2], dv[rb][4 * x4 + 3]};
+      }
+  }
+  __syncthreads();
+  if (cg == 1) return;
+  {
+    const f32x4 *of = image + kh * IMAGE + lane;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const f32x4 k4 = of[(rb * 4 + x4) * 64], v4 = of[((RB + rb) * 4 + x4) * 64];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          dk[rb][4 * x4 + x] += k4[x];
+          dv[rb][4 * x4 + x] += v4[x];
+        }
+      }
+  }
+  if (parts > 1) {
+    float *to = a.part + (((int64_t)bh * a.max_slots + a.slot0[at_j] + part) * 2 * s.kb + 64 * half + 32 * kh + r) * D;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        *reinterpret_cast<f32x4 *>(to + 32 * rb + 8 * x4 + 4 * g) = f32x4{dk[rb][4 * x4], dk[rb][4 * x4 + 1], dk[rb][4 * x4 + 2], dk[rb][4 * x4 + 3]};
+        *reinterpret_cast<f32x4 *>(to + s.kb * D + 32 * rb + 8 * x4 + 4 * g) = f32x4{dv[rb][4 * x4], dv[rb][4 * x4 + 1], dv[rb][4 * x4 + 2], dv[rb][4 * x4 + 3]};
+      }
+    return;
+  }
+  static_assert(2 * IMAGE * 16 <= 2 * 2 * CHUNK + 2 * VROW && store_bytes<D, false>() <= IMAGE * 16, "images, and the stores in a wave's own");
+  char *stage = lds + kh * (IMAGE * 16);
+  store_rows<D, false>(dk, a.scale, stage, a.dk.p + (b * a.dk.sb + hk * a.dk.sh) * 2, a.dk.sn * 2, k0, s.Nk, lane);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  store_rows<D, false>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * 2, a.dv.sn * 2, k0, s.Nk, lane);
+}
+
+// fp32 tensors: the keys' and values' pieces in registers, 32 keys to a wave, and every wave reads all queries.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS), STAT = 2 * 32 * 4;
   __shared__ __attribute__((aligned(1024))) char lds[2 * (2 * NS * STAGE + STAT)];      // [2 stages][q | dO][pieces][ROWS], lse2 | delta
-  const unsigned item = xcd_item(blockIdx.x, a.share);
-  if (item >= a.items) return;
   const Sparse &s = a.s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int bh = item / a.max_items, it = item % a.max_items, b = bh / s.Hkv, hk = bh % s.Hkv;
-  const int j = __builtin_amdgcn_readfirstlane(a.item_block[(int64_t)bh * a.max_items + it]);
-  if (j < 0) return;
-  const int part = it - a.item0[(int64_t)bh * (s.Tk + 1) + j], parts = a.item0[(int64_t)bh * (s.Tk + 1) + j + 1] - a.item0[(int64_t)bh * (s.Tk + 1) + j];
-  const int first = a.first[(int64_t)bh * (s.Tk + 1) + j], last = a.first[(int64_t)bh * (s.Tk + 1) + j + 1];
+  if ((int)blockIdx.x >= *a.n_work) return;
+  const int2 work = a.work[blockIdx.x];
+  const int bh = work.x / s.Tk, j = work.x - bh * s.Tk, part = work.y, b = bh / s.Hkv, hk = bh % s.Hkv;
+  const int64_t at_j = (int64_t)bh * (s.Tk + 1) + j;
+  const int parts = a.item0[at_j + 1] - a.item0[at_j], first = a.first[at_j], last = a.first[at_j + 1];
   const int32_t *list = a.inv + (int64_t)bh * s.T * s.sel;
   const int held = s.held(b), start = s.start(b);
   const int key0 = j * s.kb, k0 = key0 + 32 * w, ki = k0 + r;
   // steps: (place in the list, head of the group, ROWS queries of the tile)
   const int subs = s.qb / ROWS;
-  int at = first + part * kPart, end = min(at + kPart, last), head = 0, sub = 0;
+  int at = first + part * a.part_tiles, end = min(at + a.part_tiles, last), head = 0, sub = 0;
   if (key0 >= held) at = end;
   struct Step { int h, row; };        // row < 0: none left
   auto next_step = [&]() {
@@ -301,11 +527,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
       request_rows<D, ROWS, NW>(rows_rsrc<D>(a.dout.p + (b * a.dout.sb + st.h * a.dout.sh + st.row * a.dout.sn + n * a.piece_q) * 2, rows, dsn), dsn,
                               to + (NS + n) * STAGE, w, lane);
     }
-    if (w < 2) {
-      const float *src = (w == 0 ? a.lse2 : a.delta) + (int64_t)(b * s.H + st.h) * s.T * s.qb + st.row;
-      const unsigned l = __builtin_amdgcn_readfirstlane(lds_offset(to + 2 * NS * STAGE) + w * 256);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l), "v"(lane * 4), "s"(src) : "memory");
-    }
+    if (w == 0) request_stat(a.stat + ((int64_t)(b * s.H + st.h) * s.T * s.qb + st.row) * 2, to + 2 * NS * STAGE, lane);
   };
   Step cur = next_step();
   if (cur.row >= 0) request(cur, 0);
@@ -326,37 +548,42 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) dk[rb][x] = dv[rb][x] = 0.f;
 
+  const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
   for (int stage = 0; cur.row >= 0; stage ^= 1) {
     const Step next = next_step();
     landed();
     if (next.row >= 0) request(next, stage ^ 1);
-    const char *tq = lds + stage * (2 * NS * STAGE + STAT), *td = tq + NS * STAGE;
-    const float *lse2 = reinterpret_cast<const float *>(tq + 2 * NS * STAGE), *delta = lse2 + 64;
+    const char *tq = lds + stage * (2 * NS * STAGE + STAT);
+    const unsigned rows = rows0 + stage * (2 * NS * STAGE + STAT), cols = cols0 + stage * (2 * NS * STAGE + STAT);
+    const float *stat = reinterpret_cast<const float *>(tq + 2 * NS * STAGE);
     const bool mask = k0 + 32 > held || (s.causal && start + cur.row < k0 + 31);
 #pragma unroll
     for (int i = 0; i < ROWS / 32; ++i) {
       f32x16 sc, dp;
 #pragma unroll
-      for (int x = 0; x < 16; ++x) sc[x] = dp[x] = 0.f;
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(stat + 8 * x4 + 4 * g), d4 = *reinterpret_cast<const f32x4 *>(stat + 32 + 8 * x4 + 4 * g);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          sc[4 * x4 + x] = l4[x];
+          dp[4 * x4 + x] = d4[x];
+        }
+      }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 qf[NS], df[NS];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-          qf[n] = T::rows(tq + n * STAGE, 32 * i, ks, lane);
-          df[n] = T::rows(td + n * STAGE, 32 * i, ks, lane);
+          qf[n] = T::rows_at(rows, 32 * i, ks, n * STAGE);
+          df[n] = T::rows_at(rows, 32 * i, ks, (NS + n) * STAGE);
         }
         sc = mfma_split<NS>(qf, kf[ks], sc);
         dp = mfma_split<NS>(df, vf[ks], dp);
       }
 #pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(lse2 + 32 * i + 8 * x4 + 4 * g), d4 = *reinterpret_cast<const f32x4 *>(delta + 32 * i + 8 * x4 + 4 * g);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          sc[4 * x4 + x] = fast_exp2(__builtin_fmaf(sc[4 * x4 + x], c, -l4[x]));
-          dp[4 * x4 + x] = sc[4 * x4 + x] * (dp[4 * x4 + x] - d4[x]);
-        }
+      for (int x = 0; x < 16; ++x) {
+        sc[x] = fast_exp2(sc[x] * c);
+        dp[x] *= sc[x];
       }
       if (mask) {
 #pragma unroll
@@ -382,8 +609,8 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
           bf16x8 qf[NS], df[NS];
 #pragma unroll
           for (int n = 0; n < NS; ++n) {
-            df[n] = T::cols(td + n * STAGE, rb, 32 * i + 16 * u, lane);
-            qf[n] = T::cols(tq + n * STAGE, rb, 32 * i + 16 * u, lane);
+            df[n] = T::cols_at(cols, rb, 32 * i + 16 * u, (NS + n) * STAGE);
+            qf[n] = T::cols_at(cols, rb, 32 * i + 16 * u, n * STAGE);
           }
           dv[rb] = mfma_split<NS>(df, pb, dv[rb]);
           dk[rb] = mfma_split<NS>(qf, db, dk[rb]);
@@ -393,7 +620,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
     cur = next;
   }
   if (parts > 1) {
-    float *to = a.part + (((int64_t)bh * a.max_slots + a.slot0[(int64_t)bh * (s.Tk + 1) + j] + part) * 2 * s.kb + 32 * w + r) * D;
+    float *to = a.part + (((int64_t)bh * a.max_slots + a.slot0[at_j] + part) * 2 * s.kb + 32 * w + r) * D;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -404,51 +631,54 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_kernel(GradArgs a) {
     return;
   }
   __syncthreads();
-  constexpr int ESZ = F32 ? 4 : 2;
-  char *stage = lds + w * store_bytes<D, F32>();
-  store_rows<D, F32>(dk, a.scale, stage, a.dk.p + (b * a.dk.sb + hk * a.dk.sh) * ESZ, a.dk.sn * ESZ, k0, s.Nk, lane);
+  constexpr int ESZ = 4;
+  char *stage = lds + w * store_bytes<D, true>();
+  store_rows<D, true>(dk, a.scale, stage, a.dk.p + (b * a.dk.sb + hk * a.dk.sh) * ESZ, a.dk.sn * ESZ, k0, s.Nk, lane);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  store_rows<D, F32>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * ESZ, a.dv.sn * ESZ, k0, s.Nk, lane);
+  store_rows<D, true>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * ESZ, a.dv.sn * ESZ, k0, s.Nk, lane);
 }
 
-// Joins the parts of the blocks that have several: D / 4 threads to a row of dk or dv.
+// Joins the parts of the blocks that have several: D / 4 threads to a row of dk or dv, a workgroup to 256 / (D / 4) of a block's rows.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void sparse_dkv_join_kernel(GradArgs a) {
-  constexpr int TPR = D / 4;
+  constexpr int TPR = D / 4, RPB = 256 / TPR;
   const Sparse &s = a.s;
-  const int j = blockIdx.x % s.Tk, bh = blockIdx.x / s.Tk, b = bh / s.Hkv, hk = bh % s.Hkv;
-  const int64_t at = (int64_t)bh * (s.Tk + 1) + j;
-  const int parts = a.item0[at + 1] - a.item0[at];
+  const int pieces = 2 * s.kb / RPB, row = blockIdx.x % pieces * RPB + threadIdx.x / TPR, at = blockIdx.x / pieces;
+  const int j = at % s.Tk, bh = at / s.Tk, b = bh / s.Hkv, hk = bh % s.Hkv;
+  const int64_t at_j = (int64_t)bh * (s.Tk + 1) + j;
+  const int parts = a.item0[at_j + 1] - a.item0[at_j];
   if (parts <= 1) return;
-  const float *from = a.part + ((int64_t)bh * a.max_slots + a.slot0[at]) * 2 * s.kb * D;
   const int c = 4 * (threadIdx.x % TPR);
-  for (int row = threadIdx.x / TPR; row < 2 * s.kb; row += 256 / TPR) {
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < parts; ++i) sum += *reinterpret_cast<const f32x4 *>(from + ((int64_t)i * 2 * s.kb + row) * D + c);
-    const bool is_v = row >= s.kb;
-    const int n = j * s.kb + (is_v ? row - s.kb : row);
-    if (n >= s.Nk) continue;
-    const View &to = is_v ? a.dv : a.dk;
-    if (!is_v) sum *= a.scale;
-    const int64_t i = b * to.sb + hk * to.sh + n * to.sn + c;
-    if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(to.p) + i) = sum;
-    else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(to.p) + i) = __builtin_convertvector(sum, bf16x4);
-  }
+  const float *from = a.part + (((int64_t)bh * a.max_slots + a.slot0[at_j]) * 2 * s.kb + row) * D + c;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) sum += *reinterpret_cast<const f32x4 *>(from + (int64_t)i * 2 * s.kb * D);
+  const bool is_v = row >= s.kb;
+  const int n = j * s.kb + (is_v ? row - s.kb : row);
+  if (n >= s.Nk) return;
+  const View &to = is_v ? a.dv : a.dk;
+  if (!is_v) sum *= a.scale;
+  const int64_t i = b * to.sb + hk * to.sh + n * to.sn + c;
+  if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(to.p) + i) = sum;
+  else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(to.p) + i) = __builtin_convertvector(sum, bf16x4);
 }
 
 struct GradPlanS {
-  int n_chunks, max_items, max_slots;
-  size_t off_q, off_k, off_v, off_do, off_lse2, off_delta, off_hist, off_first, off_item0, off_slot0, off_inv, off_item, off_part, total;
+  int n_chunks, max_items, max_slots, part_tiles;
+  size_t off_q, off_k, off_v, off_do, off_stat, off_hist, off_first, off_item0, off_slot0, off_inv, off_work, off_n_work, off_part, total;
 };
 
 GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   GradPlanS f{};
   const int64_t entries = (int64_t)s.T * s.sel;
   f.n_chunks = (s.T + kChunk - 1) / kChunk;
-  // ceil(n_j / kPart) parts of block j: over all blocks at most entries / kPart + Tk; those of blocks with several, of which there are
-  // fewer than entries / kPart, at most 2 entries / kPart
-  f.max_items = (int)(entries / kPart) + s.Tk;
-  f.max_slots = (int)(2 * (entries / kPart));
+  // parts of 64 tiles, shorter ones where the lists of all heads would not fill the chip twice
+  const int64_t fill = (int64_t)s.B * s.Hkv * entries / 512;
+  f.part_tiles = (int)(fill < 8 ? 8 : fill > kPart ? kPart : fill);
+  // ceil(n_j / part) parts of block j: over all blocks at most entries / part + Tk; those of blocks with several, of which there are
+  // fewer than entries / part, at most 2 entries / part
+  f.max_items = (int)(entries / f.part_tiles) + s.Tk;
+  f.max_slots = (int)(2 * (entries / f.part_tiles));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -462,14 +692,14 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
     f.off_v = take(6 * nk);
     f.off_do = take(6 * nq);
   }
-  f.off_lse2 = take((size_t)s.B * s.H * s.T * s.qb * 4);
-  f.off_delta = take((size_t)s.B * s.H * s.T * s.qb * 4);
+  f.off_stat = take((size_t)s.B * s.H * s.T * s.qb * 8);
   f.off_hist = take(hk * f.n_chunks * s.Tk * 4);
   f.off_first = take(hk * (s.Tk + 1) * 4);
   f.off_item0 = take(hk * (s.Tk + 1) * 4);
   f.off_slot0 = take(hk * (s.Tk + 1) * 4);
   f.off_inv = take(hk * entries * 4);
-  f.off_item = take(hk * f.max_items * 4);
+  f.off_work = take(hk * f.max_items * 8);
+  f.off_n_work = take(4);
   f.off_part = take(hk * f.max_slots * 2 * s.kb * p.d_head * 4);
   f.total = at;
   if ((int64_t)hk * f.max_items > (1 << 30)) f.total = 0;      // (more workgroups than a launch is given)
@@ -488,13 +718,13 @@ hipError_t launch_grad(const ha_sparse_problem &p, GradArgs &a, hipStream_t st) 
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (s.Nk > 0) {
-    a.items = (unsigned)((int64_t)s.B * s.Hkv * a.max_items);
-    a.share = xcd_share(a.items);
-    if (s.kb == 128) sparse_dkv_kernel<D, F32, 4><<<8 * a.share, 256, 0, st>>>(a);
-    else sparse_dkv_kernel<D, F32, 2><<<8 * a.share, 128, 0, st>>>(a);
+    const unsigned items = (unsigned)((int64_t)s.B * s.Hkv * a.max_items);
+    if constexpr (!F32) sparse_dkv_kernel<D><<<(items + 7) / 8 * 8 * (s.kb >> 6), 256, 0, st>>>(a);
+    else if (s.kb == 128) sparse_dkv_f32_kernel<D, 4><<<items, 256, 0, st>>>(a);
+    else sparse_dkv_f32_kernel<D, 2><<<items, 128, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.max_slots > 0) {
-      sparse_dkv_join_kernel<D, F32><<<(unsigned)((int64_t)s.B * s.Hkv * s.Tk), 256, 0, st>>>(a);
+      sparse_dkv_join_kernel<D, F32><<<(unsigned)((int64_t)s.B * s.Hkv * s.Tk) * (2 * s.kb / (1024 / D)), 256, 0, st>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -536,13 +766,13 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
   char *ws = static_cast<char *>(workspace);
   const int d = p->d_head;
   const bool f32 = p->dtype == HA_F32;
-  float *lse2 = reinterpret_cast<float *>(ws + f.off_lse2), *delta = reinterpret_cast<float *>(ws + f.off_delta);
+  float *stat = reinterpret_cast<float *>(ws + f.off_stat);
   hipError_t e;
   if (s.Nq > 0) {
     const int rpb = 256 / (d / 8);
     const unsigned n = (unsigned)(((int64_t)s.B * s.H * s.T * s.qb + rpb - 1) / rpb);
-    if (d == 128) { if (f32) sparse_delta_kernel<128, true><<<n, 256, 0, stream>>>(s, o, a.dout, lse, lse2, delta); else sparse_delta_kernel<128, false><<<n, 256, 0, stream>>>(s, o, a.dout, lse, lse2, delta); }
-    else { if (f32) sparse_delta_kernel<64, true><<<n, 256, 0, stream>>>(s, o, a.dout, lse, lse2, delta); else sparse_delta_kernel<64, false><<<n, 256, 0, stream>>>(s, o, a.dout, lse, lse2, delta); }
+    if (d == 128) { if (f32) sparse_delta_kernel<128, true><<<n, 256, 0, stream>>>(s, o, a.dout, lse, 1.f / p->softmax_scale, stat); else sparse_delta_kernel<128, false><<<n, 256, 0, stream>>>(s, o, a.dout, lse, 1.f / p->softmax_scale, stat); }
+    else { if (f32) sparse_delta_kernel<64, true><<<n, 256, 0, stream>>>(s, o, a.dout, lse, 1.f / p->softmax_scale, stat); else sparse_delta_kernel<64, false><<<n, 256, 0, stream>>>(s, o, a.dout, lse, 1.f / p->softmax_scale, stat); }
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
   }
   if (f32) {
@@ -557,18 +787,19 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
     a.piece_k = (int64_t)s.B * s.Hkv * s.Nk * d;
   }
   a.blocks = blocks;
-  a.lse2 = lse2;
-  a.delta = delta;
+  a.stat = stat;
   a.hist = reinterpret_cast<int32_t *>(ws + f.off_hist);
   a.first = reinterpret_cast<int32_t *>(ws + f.off_first);
   a.item0 = reinterpret_cast<int32_t *>(ws + f.off_item0);
   a.slot0 = reinterpret_cast<int32_t *>(ws + f.off_slot0);
   a.inv = reinterpret_cast<int32_t *>(ws + f.off_inv);
-  a.item_block = reinterpret_cast<int32_t *>(ws + f.off_item);
+  a.work = reinterpret_cast<int2 *>(ws + f.off_work);
+  a.n_work = reinterpret_cast<int32_t *>(ws + f.off_n_work);
   a.part = reinterpret_cast<float *>(ws + f.off_part);
   a.n_chunks = f.n_chunks;
   a.max_items = f.max_items;
   a.max_slots = f.max_slots;
+  a.part_tiles = f.part_tiles;
   a.scale = p->softmax_scale;
   a.scale_log2e = p->softmax_scale * kLog2e;
   if (s.Nk > 0) {
@@ -578,6 +809,8 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
       if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
     }
     inverse_scan_kernel<<<heads, 1024, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+    inverse_order_kernel<<<heads, 1024, 0, stream>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
     if (f.n_chunks > 0) {
       inverse_fill_kernel<<<dim3(f.n_chunks, heads), 256, 0, stream>>>(a);

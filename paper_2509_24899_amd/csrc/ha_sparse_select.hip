@@ -24,7 +24,7 @@ ha_status check_sparse(const ha_sparse_problem *p) {
   if ((int64_t)p->B * p->H > 65535 || p->N_q > (1 << 24) || p->N_k > (1 << 29) || p->n_select > (1 << 20) || p->near_tokens > (1 << 29)) return HA_ERR_UNSUPPORTED;
   const int64_t T = (p->N_q + p->q_block - 1) / p->q_block, Tk = (p->N_k + p->k_block - 1) / p->k_block, BH = (int64_t)p->B * p->H;
   // (a launch takes 2^31 - 1 workgroups, and an index into one head's lists 31 bits)
-  if (BH * T > (1 << 24) || BH * Tk > (1 << 28) || T * p->n_select > (1 << 30)) return HA_ERR_UNSUPPORTED;
+  if (BH * T > (1 << 24) || BH * Tk > (1 << 25) || T * p->n_select > (1 << 30)) return HA_ERR_UNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(p->q_start) & 3u || reinterpret_cast<uintptr_t>(p->key_len) & 3u) return HA_ERR_ALIGN;
   return HA_OK;
 }
