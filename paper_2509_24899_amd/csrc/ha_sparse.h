@@ -51,18 +51,20 @@ struct Tile {
     const int row = lane & 31;
     return lds_offset(tile) + row * PITCH + (((lane >> 5) ^ swz(row)) << 4);
   }
-  static __device__ __forceinline__ bf16x8 rows_at(unsigned base, int row0, int ks, int further = 0) {
-    return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(static_cast<uintptr_t>((base ^ (ks << 5)) + row0 * PITCH + further));
-  }
+  static __device__ __forceinline__ bf16x8 row_piece(unsigned at) { return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(static_cast<uintptr_t>(at)); }
+  static __device__ __forceinline__ bf16x8 rows_at(unsigned base, int row0, int ks, int further = 0) { return row_piece((base ^ (ks << 5)) + row0 * PITCH + further); }
   static __device__ __forceinline__ unsigned cols_base(const char *tile, int lane) {
     const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     return lds_offset(tile) + row * PITCH + ((piece ^ swz(row)) << 4) + (lane & 1) * 8;
   }
+  static __device__ __forceinline__ bf16x8 col_piece(unsigned at0, unsigned at8) {
+    return join(__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>(at0))),
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>(at8))));
+  }
   static __device__ __forceinline__ bf16x8 cols_at(unsigned base, int cb, int row0, int further = 0) {
     // (eight rows further down the permutation differs in piece bit 1)
     const unsigned at = base ^ (cb << 6);
-    return join(__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>(at + row0 * PITCH + further))),
-                __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4_ptr>(static_cast<uintptr_t>((at ^ 32) + (row0 + 8) * PITCH + further))));
+    return col_piece(at + row0 * PITCH + further, (at ^ 32) + (row0 + 8) * PITCH + further);
   }
 };
 

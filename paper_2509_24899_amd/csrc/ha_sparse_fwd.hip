@@ -9,6 +9,7 @@
 // the second product only (fp32 tensors: all operands are three bf16 pieces, six products each).
 // Few tiles: the list is cut into ranges, a workgroup each, whose sums a second kernel joins.
 #include <cmath>
+#include <type_traits>
 
 #include "ha_sparse.h"
 
@@ -27,10 +28,179 @@ struct FwdArgs {
   unsigned items, share;
 };
 
-template <int D, bool F32, int NW>
-__global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
+// bf16 tensors: 32 keys to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next keys under the
+// exponentials of its own, then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work
+// of one wave at the same time, and of two with two workgroups to a CU.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, SLOTS = 4;
+  __shared__ __attribute__((aligned(1024))) char lds[SLOTS * SLOT];      // [step][k | v]
+  const unsigned item = xcd_item(blockIdx.x, a.share);
+  if (item >= a.items) return;
+  const Sparse &s = a.s;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = item % a.n_split, t = item / a.n_split % s.T, bh = item / a.n_split / s.T, b = bh / s.H, h = bh % s.H, hk = h / s.G;
+  const int held = s.held(b), start = s.start(b);
+  const int q0 = t * s.qb + 32 * w, qi = q0 + r;      // this wave's first query, this lane's
+  const int tile_last = min((t + 1) * s.qb, s.Nq) - 1;
+  // keys that the tile, this wave's first query and this lane's query see
+  const int limit = s.causal ? min(held, start + tile_last + 1) : held;
+  const int wave_limit = s.causal ? min(held, start + q0 + 1) : held, row_limit = s.causal ? min(held, start + qi + 1) : held;
+  const int32_t *list = a.blocks + ((int64_t)(b * s.Hkv + hk) * s.T + t) * s.sel;
+  ListWalk<32> walk(list, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
+
+  const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
+  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  constexpr int REQUESTS = 2 * T::chunks(32) / NW;
+  // (behind the list's last key zeros are requested: every step has as many requests, which is what the waits count)
+  auto request = [&](int key, int slot) {
+    char *to = lds + slot * SLOT;
+    const int rows = key < 0 ? 0 : min(limit - key, 32), at = max(key, 0);
+    request_rows<D, 32, NW>(rows_rsrc<D>(kbase + (int64_t)at * ksn, rows, ksn), ksn, to, w, lane);
+    request_rows<D, 32, NW>(rows_rsrc<D>(vbase + (int64_t)at * vsn, rows, vsn), vsn, to + TILE, w, lane);
+  };
+  int key0 = walk.next(), key1 = walk.next(), key2 = walk.next();
+  const float c = a.scale_log2e;
+  float m = -INFINITY, top = -INFINITY, l = 0.f;      // what the sums are expressed against, the largest logit and the sum of weights (this lane's keys)
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  if (key0 >= 0) {
+    request(key0, 0);
+    request(key1, 1);
+    request(key2, 2);
+    bf16x8 qf[KS];
+    const char *qp = a.q.p + (b * a.q.sb + h * a.q.sh + (int64_t)min(qi, s.Nq - 1) * a.q.sn + 8 * g) * 2;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+    // addresses of all operands of a step; the slot goes into the instruction
+    unsigned rows[KS], cols[RB][2];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) rows[ks] = T::rows_base(lds, lane) ^ (ks << 5);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) cols[rb][i] = T::cols_base(lds, lane) ^ (rb << 6) ^ (i << 5);
+    auto read_k = [&](int slot, int ks) { return T::row_piece(rows[ks] + slot * SLOT); };
+    auto read_v = [&](int slot, int rb, int u) { return T::col_piece(cols[rb][0] + slot * SLOT + TILE + 16 * u * T::PITCH, cols[rb][1] + slot * SLOT + TILE + (16 * u + 8) * T::PITCH); };
+    const float gap = 8.f / c;
+    float mc = 0.f;
+    // logits of keys that this wave's queries do not all see (a key of -1: of none), then the running maximum.  What has been summed follows it when
+    // some query's has moved by 8 in the exponent (weights stay below 2^8).
+    auto mask = [&](f32x16 &sc, int key) {
+      if (key < 0 || key + 32 > wave_limit) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = key >= 0 && key + crow(x, g) < row_limit ? sc[x] : -INFINITY;
+      }
+    };
+    auto follow = [&](const f32x16 &sc) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+      if (__any(top - m > gap)) {
+        top = xhalf_max(top);
+        const float f = top == m ? 1.f : fast_exp2((m - top) * c);      // (neither may have seen a key)
+        l *= f;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+        m = top;
+        mc = m == -INFINITY ? 0.f : m * c;
+      }
+    };
+    const f32x16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    f32x16 s_a, s_b;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * REQUESTS) : "memory");
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s_a = mfma32(read_k(0, ks), qf[ks], ks == 0 ? none : s_a);
+    mask(s_a, key0);
+    follow(s_a);
+    auto step = [&](f32x16 &sc, f32x16 &sn, auto slot_c) {
+      constexpr int slot = decltype(slot_c)::value, next = (slot + 1) & (SLOTS - 1);
+      // the next keys have landed, and no wave reads those of the step before any more
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
+      __syncthreads();
+      bf16x8 kf[KS], vf[2 * RB], pb[2];
+      kf[0] = read_k(next, 0);
+      kf[1] = read_k(next, 1);
+      const int key3 = walk.next();
+      request(key3, (slot + 3) & (SLOTS - 1));
+      constexpr int PER = 16 / KS;         // logits to a product: 2 at d = 128, 4 at d = 64
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 2 < KS) kf[ks + 2] = read_k(next, ks + 2);
+        else vf[ks + 2 - KS] = read_v(slot, ks + 2 - KS, 0);
+        HA_FENCE();
+        sn = mfma32(kf[ks], qf[ks], ks == 0 ? none : sn);
+#pragma unroll
+        for (int y = 0; y < PER; ++y) {
+          const int x = ks * PER + y;
+          sc[x] = fast_exp2(__builtin_fmaf(sc[x], c, -mc));
+          l += sc[x];
+          if (x % 8 == 7) {
+            f32x8 p;
+#pragma unroll
+            for (int z = 0; z < 8; ++z) p[z] = sc[x - 7 + z];
+            pb[x / 8] = __builtin_convertvector(p, bf16x8);
+          }
+        }
+        HA_FENCE();
+      }
+#pragma unroll
+      for (int n = 0; n < 2 * RB; ++n) {   // n = RB u + rb
+        if (n + 2 < 2 * RB) vf[n + 2] = read_v(slot, (n + 2) % RB, (n + 2) / RB);
+        HA_FENCE();
+        o[n % RB] = mfma32(vf[n], pb[n / RB], o[n % RB]);
+      }
+      mask(sn, key1);
+      follow(sn);
+      key0 = key1;
+      key1 = key2;
+      key2 = key3;
+    };
+    while (true) {
+      step(s_a, s_b, std::integral_constant<int, 0>{});
+      if (key0 < 0) break;
+      step(s_b, s_a, std::integral_constant<int, 1>{});
+      if (key0 < 0) break;
+      step(s_a, s_b, std::integral_constant<int, 2>{});
+      if (key0 < 0) break;
+      step(s_b, s_a, std::integral_constant<int, 3>{});
+      if (key0 < 0) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  l = xhalf_sum(l);
+  if (a.n_split > 1) {
+    const int64_t row = ((int64_t)range * s.B * s.H + bh) * s.Nq + qi;
+    if (qi < s.Nq) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int x4 = 0; x4 < 4; ++x4)
+          *reinterpret_cast<f32x4 *>(a.po + row * D + 32 * rb + 8 * x4 + 4 * g) = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+      if (g == 0) {
+        a.pm[row] = m;
+        a.pl[row] = l;
+      }
+    }
+    return;
+  }
+  if (a.lse && g == 0 && qi < s.Nq) a.lse[(int64_t)bh * s.Nq + qi] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
+  __syncthreads();                                    // the slots become the staging area of the stores
+  store_rows<D, false>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, false>(), a.out.p + (b * a.out.sb + h * a.out.sh) * 2, a.out.sn * 2,
+                       q0, min((t + 1) * s.qb, s.Nq), lane);
+}
+
+// fp32 tensors: 32 keys at a time in three pieces.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void sparse_fwd_f32_kernel(FwdArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS);
   __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];      // [2 stages][k | v][pieces][ROWS]
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
@@ -158,8 +328,7 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_fwd_k
   }
   if (a.lse && g == 0 && qi < s.Nq) a.lse[(int64_t)bh * s.Nq + qi] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
   __syncthreads();                                    // the stages become the staging area of the stores
-  constexpr int ESZ = F32 ? 4 : 2;
-  store_rows<D, F32>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, F32>(), a.out.p + (b * a.out.sb + h * a.out.sh) * ESZ, a.out.sn * ESZ,
+  store_rows<D, true>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, true>(), a.out.p + (b * a.out.sb + h * a.out.sh) * 4, a.out.sn * 4,
                          q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
@@ -228,7 +397,8 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
 
 template <int D, bool F32, int NW>
 hipError_t launch_fwd(const FwdArgs &a, hipStream_t st) {
-  sparse_fwd_kernel<D, F32, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  if constexpr (F32) sparse_fwd_f32_kernel<D, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  else sparse_fwd_kernel<D, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
   return hipGetLastError();
 }
 
