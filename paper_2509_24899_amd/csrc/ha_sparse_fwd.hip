@@ -332,28 +332,173 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_fwd_f32_kernel(FwdArgs a) {
                          q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
-// Joins the ranges of a row: D / 4 threads to a row.
+// Few queries (a decoding step): all queries of all heads of a key head, 32 at most, are the columns of one product, so that keys and values are read once
+// for the group.  What bounds it is memory, so every wave walks keys of its own, every fourth step of the range, with its own two stages in LDS and no
+// barrier; the four waves' sums are joined behind the list.
+template <int D>
+__global__ __launch_bounds__(256) void sparse_few_kernel(FwdArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, REQUESTS = 2 * T::chunks(32), IMAGE = RB * 4 * 64;
+  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * SLOT];      // [wave][stage][k | v]; then [wave][register image]
+  __shared__ float stats[2][4][32];
+  const Sparse &s = a.s;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / s.Hkv, hk = bh % s.Hkv;
+  const int held = s.held(b), start = s.start(b), rows = s.G * s.Nq, col = min(r, rows - 1), h = hk * s.G + col / s.Nq, n = col % s.Nq;
+  const int limit = s.causal ? min(held, start + s.Nq) : held, all_see = s.causal ? min(held, start + 1) : held, row_limit = s.causal ? min(held, start + n + 1) : held;
+  ListWalk<32> walk(a.blocks + (int64_t)bh * s.sel, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
+  const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
+  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  char *mine = lds + w * (2 * SLOT);
+  auto request = [&](int key, int stage) {
+    const int n_keys = min(limit - key, 32);
+    request_rows<D, 32, 1>(rows_rsrc<D>(kbase + (int64_t)key * ksn, n_keys, ksn), ksn, mine + stage * SLOT, 0, lane);
+    request_rows<D, 32, 1>(rows_rsrc<D>(vbase + (int64_t)key * vsn, n_keys, vsn), vsn, mine + stage * SLOT + TILE, 0, lane);
+  };
+  int key = -1;
+  for (int i = 0; i <= w; ++i) key = walk.next();
+  if (key >= 0) request(key, 0);
+  bf16x8 qf[KS];
+  const char *qp = a.q.p + (b * a.q.sb + h * a.q.sh + n * a.q.sn + 8 * g) * 2;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+  const unsigned rows0 = T::rows_base(mine, lane), cols0 = T::cols_base(mine, lane);
+  const float c = a.scale_log2e;
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  for (int stage = 0; key >= 0; stage ^= 1) {
+    int next = -1;
+    for (int i = 0; i < 4; ++i) next = walk.next();
+    if (next >= 0) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the last step's reads of that stage are done)
+      request(next, stage ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    const unsigned kt = rows0 + stage * SLOT, vt = cols0 + stage * SLOT;
+    f32x16 sc;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sc = mfma32(T::rows_at(kt, 0, ks), qf[ks], sc);
+    if (key + 32 > all_see) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sc[x] = key + crow(x, g) < row_limit ? sc[x] : -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+    top = xhalf_max(top);
+    const float f = top == m ? 1.f : fast_exp2((m - top) * c), mc = top == -INFINITY ? 0.f : top * c;
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 p;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        p[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
+        l += p[x];
+      }
+      const bf16x8 pb = __builtin_convertvector(p, bf16x8);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb] = mfma32(T::cols_at(vt, rb, 16 * u, TILE), pb, o[rb]);
+    }
+    key = next;
+  }
+  l = xhalf_sum(l);
+  __syncthreads();
+  f32x4 *image = reinterpret_cast<f32x4 *>(lds);
+  static_assert(4 * IMAGE * 16 <= 4 * 2 * SLOT, "the images fit the stages");
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4)
+      image[w * IMAGE + (rb * 4 + x4) * 64 + lane] = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+  if (g == 0) {
+    stats[0][w][r] = m;
+    stats[1][w][r] = l;
+  }
+  __syncthreads();
+  if (w >= RB || r >= rows) return;
+  // wave w: columns 32 w .. of the joined rows
+  float top = stats[0][0][r], total = 0.f;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) top = fmaxf(top, stats[0][i][r]);
+  f32x4 y[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float mi = stats[0][i][r], f = mi == top ? 1.f : fast_exp2((mi - top) * c);
+    total += stats[1][i][r] * f;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) y[x4] += image[i * IMAGE + (w * 4 + x4) * 64 + lane] * f;
+  }
+  const int64_t row = ((int64_t)b * s.H + h) * s.Nq + n;
+  if (a.n_split > 1) {
+    const int64_t at = (int64_t)range * s.B * s.H * s.Nq + row;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) *reinterpret_cast<f32x4 *>(a.po + at * D + 32 * w + 8 * x4 + 4 * g) = y[x4];
+    if (w == 0 && g == 0) {
+      a.pm[at] = top;
+      a.pl[at] = total;
+    }
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int x4 = 0; x4 < 4; ++x4)
+    *reinterpret_cast<bf16x4 *>(a.out.p + (b * a.out.sb + h * a.out.sh + n * a.out.sn + 32 * w + 8 * x4 + 4 * g) * 2) = __builtin_convertvector(y[x4] * inv, bf16x4);
+  if (a.lse && w == 0 && g == 0) a.lse[row] = total > 0.f ? top * a.scale + logf(total) : total == 0.f ? -INFINITY : total;
+}
+
+// Joins the ranges of a row, at most 64: a wave to a row.  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void sparse_join_kernel(FwdArgs a) {
-  constexpr int TPR = D / 4;
+  constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
   const Sparse &s = a.s;
-  const int64_t rows = (int64_t)s.B * s.H * s.Nq, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int64_t rows = (int64_t)s.B * s.H * s.Nq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= rows) return;
-  const int c4 = 4 * (threadIdx.x % TPR);
-  float m = -INFINITY;
-  for (int i = 0; i < a.n_split; ++i) m = fmaxf(m, a.pm[i * rows + row]);
-  float l = 0.f;
+  const int lane = threadIdx.x & 63, c4 = 4 * (lane % LPR);
+  const bool has = lane < a.n_split;
+  const float mi = has ? a.pm[lane * rows + row] : -INFINITY;
+  float m = mi;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  const float f = mi == m ? 1.f : fast_exp2((mi - m) * a.scale_log2e);
+  float l = has ? a.pl[lane * rows + row] * f : 0.f;          // (a range that saw nothing has 0, or the NaN that has to show)
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < a.n_split; ++i) {
-    const float mi = a.pm[i * rows + row];
-    const float f = mi == -INFINITY ? 0.f : fast_exp2((mi - m) * a.scale_log2e);
-    const float li = a.pl[i * rows + row];
-    // (a range that saw nothing has l = 0; a NaN in it has to show)
-    l += mi == -INFINITY ? li : li * f;
-    o += *reinterpret_cast<const f32x4 *>(a.po + (i * rows + row) * D + c4) * f;
+  for (int i0 = 0; i0 < a.n_split; i0 += 4 * AT_ONCE) {
+    f32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + u * AT_ONCE + lane / LPR, a.n_split - 1);
+      x[u] = *reinterpret_cast<const f32x4 *>(a.po + (i * rows + row) * D + c4);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * AT_ONCE + lane / LPR;
+      const float fi = __shfl(f, min(i, 63));
+      if (i < a.n_split) o += x[u] * fi;
+    }
   }
+#pragma unroll
+  for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] += __shfl_xor(o[u], d);
+  if (lane >= LPR) return;
   const int b = (int)(row / s.Nq / s.H), h = (int)(row / s.Nq % s.H), n = (int)(row % s.Nq);
-  if (a.lse && c4 == 0) a.lse[row] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
+  if (a.lse && lane == 0) a.lse[row] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
   o *= l == 0.f ? 0.f : 1.f / l;
   const int64_t at = b * a.out.sb + h * a.out.sh + n * a.out.sn + c4;
   if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out.p) + at) = o;
@@ -361,19 +506,20 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(FwdArgs a) {
 }
 
 struct FwdPlan {
+  bool few;
   int n_split;
   size_t off_q, off_k, off_v, off_po, off_pm, off_pl, total;
 };
 
 FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
   FwdPlan f{};
-  const int64_t tiles = (int64_t)s.B * s.H * s.T;
-  f.n_split = 1;
-  if (tiles > 0 && tiles < 512) {
-    const int64_t want = (512 + tiles - 1) / tiles, most = (s.sel + 1) / 2;
-    f.n_split = (int)(want < most ? want : most);
-    if (f.n_split > 32) f.n_split = 32;
-  }
+  // Workgroups: a tile of a head each, or all queries of a key head's group where they are few; the list is cut where that leaves CUs without one.
+  f.few = p.dtype == HA_BF16 && s.T == 1 && s.G * (int64_t)s.Nq <= 32;
+  const int64_t groups = (int64_t)s.B * (f.few ? s.Hkv : s.H * (int64_t)s.T), steps = (int64_t)s.sel * s.kb / 32;
+  const int64_t most = f.few ? (steps + 3) / 4 : (steps + 15) / 16, want = groups > 0 ? 256 / groups : 1;      // (a step to a wave, or 16 to a workgroup)
+  f.n_split = (int)(want < 1 || s.Nq == 0 ? 1 : want < most ? want : most);
+  if (f.n_split > s.sel) f.n_split = s.sel;
+  if (f.n_split > 64) f.n_split = 64;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -451,7 +597,12 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   a.scale_log2e = p->softmax_scale * kLog2e;
   a.items = (unsigned)((int64_t)s.B * s.H * s.T * f.n_split);
   a.share = xcd_share(a.items);
-  if (d == 128) {
+  if (f.few) {
+    const unsigned n = (unsigned)s.B * s.Hkv * f.n_split;
+    if (d == 128) sparse_few_kernel<128><<<n, 256, 0, stream>>>(a);
+    else sparse_few_kernel<64><<<n, 256, 0, stream>>>(a);
+    e = hipGetLastError();
+  } else if (d == 128) {
     if (f32) e = s.qb == 128 ? launch_fwd<128, true, 4>(a, stream) : launch_fwd<128, true, 2>(a, stream);
     else e = s.qb == 128 ? launch_fwd<128, false, 4>(a, stream) : launch_fwd<128, false, 2>(a, stream);
   } else {
@@ -460,7 +611,7 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   }
   if (e != hipSuccess) return device_error(e);
   if (f.n_split > 1) {
-    const unsigned blocks_j = (unsigned)(((int64_t)s.B * s.H * s.Nq + 256 / (d / 4) - 1) / (256 / (d / 4)));
+    const unsigned blocks_j = (unsigned)(((int64_t)s.B * s.H * s.Nq + 3) / 4);
     if (d == 128) { if (f32) sparse_join_kernel<128, true><<<blocks_j, 256, 0, stream>>>(a); else sparse_join_kernel<128, false><<<blocks_j, 256, 0, stream>>>(a); }
     else { if (f32) sparse_join_kernel<64, true><<<blocks_j, 256, 0, stream>>>(a); else sparse_join_kernel<64, false><<<blocks_j, 256, 0, stream>>>(a); }
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);

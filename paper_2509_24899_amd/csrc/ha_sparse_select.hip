@@ -5,8 +5,8 @@
 // Everything that decides is formed in double: the sums of 64 or 128 bf16 values are exact there, and two scores that differ at all are in the
 // right order, whatever the order of summation (in fp32 about one list in ten thousand changed with it).  The sums over q and k are bound by
 // memory; the scores of 128 queries against a block of 64 keys take one product of d values.
+#include <climits>
 #include <cmath>
-#include <limits>
 
 #include "ha_sparse.h"
 
@@ -125,98 +125,280 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   return (u >> 63) ? ~u : u | ((uint64_t)1 << 63);
 }
 
-// Scores of TILES tiles against 256 blocks, a block a thread, as ordered integers [rows][Tk].
 struct ScoreArgs {
   Sparse s;
-  const double *sums;
+  View q;
+  double *sums;
   const float *means;
   uint64_t *keys;
+  int32_t *blocks;
   int keep_first, near_tokens;
 };
-template <int D, int TILES>
-__global__ __launch_bounds__(256) void scores_kernel(ScoreArgs a) {
+// Key of block j for tile t: its score's order, all ones where the block is always kept, 0 where it may not be chosen.
+__device__ __forceinline__ uint64_t rank_key(const ScoreArgs &a, int held, int start, int t, int j, double score) {
   const Sparse &s = a.s;
-  __shared__ double q[TILES][D];
-  const int bh = blockIdx.z, b = bh / s.Hkv, t0 = blockIdx.y * TILES, j = blockIdx.x * 256 + threadIdx.x;
-  for (int i = threadIdx.x; i < TILES * D; i += 256) q[i / D][i % D] = t0 + i / D < s.T ? a.sums[((int64_t)bh * s.T + t0) * D + i] : 0.;
-  __syncthreads();
-  if (j >= s.Tk) return;
-  const f32x4 *m = reinterpret_cast<const f32x4 *>(a.means + ((int64_t)bh * s.Tk + j) * D);
-  double acc[TILES];
+  const int lo_key = j * s.kb, hi_key = lo_key + s.kb - 1, lo = start + t * s.qb, hi = start + min((t + 1) * s.qb, s.Nq) - 1;
+  uint64_t key = ordered(score);
+  if (j < a.keep_first || (a.near_tokens >= 0 && hi_key >= lo - a.near_tokens && lo_key <= hi + (s.causal ? 0 : a.near_tokens))) key = ~(uint64_t)0;
+  if (lo_key >= held || (s.causal && lo_key > hi)) key = 0;
+  return key;
+}
+
+// Scores of kTiles tiles against 16 blocks by one wave on the fp64 matrix cores: lane l holds the sums of tile l % 16 (rows) and the mean of block l % 16
+// (columns) at columns 16 i + 4 (l / 16) + u of every 16, the contraction's k of product (i, u); register v of the result is tile 4 v + l / 16,
+// block l % 16.  (As vector products the sums came from LDS for every block, and that bound it: 22 us for 15 at 256 tiles by 512 blocks of 12 heads.)
+constexpr int kTiles = 16;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+template <int D>
+__device__ __forceinline__ void load_sums(const ScoreArgs &a, int bh, int t0, int lane, f64x4 (&q)[D / 16]) {
+  const int t = min(t0 + (lane & 15), a.s.T - 1);
+  const f64x4 *p = reinterpret_cast<const f64x4 *>(a.sums + ((int64_t)bh * a.s.T + t) * D) + (lane >> 4);
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) acc[i] = 0.;
-#pragma unroll 2
-  for (int c = 0; c < D / 4; ++c) {
-    const f32x4 x = m[c];
+  for (int i = 0; i < D / 16; ++i) q[i] = p[4 * i];
+}
+template <int D>
+__device__ __forceinline__ void load_means(const ScoreArgs &a, int bh, int j0, int lane, f32x4 (&m)[D / 16]) {
+  const f32x4 *p = reinterpret_cast<const f32x4 *>(a.means + ((int64_t)bh * a.s.Tk + min(j0 + (lane & 15), a.s.Tk - 1)) * D) + (lane >> 4);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+  for (int i = 0; i < D / 16; ++i) m[i] = p[4 * i];
+}
+template <int D>
+__device__ __forceinline__ f64x4 scores_of_blocks(const f32x4 (&m)[D / 16], const f64x4 (&q)[D / 16]) {
+  f64x4 c[2] = {{0., 0., 0., 0.}, {0., 0., 0., 0.}};
 #pragma unroll
-      for (int i = 0; i < TILES; ++i) acc[i] = __builtin_fma((double)x[u], q[i][4 * c + u], acc[i]);
-  }
-  const int held = s.held(b), lo_key = j * s.kb, hi_key = lo_key + s.kb - 1, start = s.start(b);
+  for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    const int t = t0 + i;
-    if (t >= s.T) break;
-    const int lo = start + t * s.qb, hi = start + min((t + 1) * s.qb, s.Nq) - 1;
-    uint64_t key = ordered(acc[i]);
-    if (j < a.keep_first || (a.near_tokens >= 0 && hi_key >= lo - a.near_tokens && lo_key <= hi + (s.causal ? 0 : a.near_tokens))) key = ~(uint64_t)0;
-    if (lo_key >= held || (s.causal && lo_key > hi)) key = 0;
-    a.keys[((int64_t)bh * s.T + t) * s.Tk + j] = key;
+    for (int u = 0; u < 4; ++u) c[u & 1] = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i][u], (double)m[i][u], c[u & 1], 0, 0, 0);
+  return c[0] + c[1];
+}
+// Every wave of WAVES its groups of 16 blocks of [lo, hi); done(j0, scores).
+template <int D, int WAVES, typename Done>
+__device__ __forceinline__ void score_range(const ScoreArgs &a, int bh, int lo, int hi, int w, int lane, const f64x4 (&q)[D / 16], Done done) {
+  for (int j0 = lo + 16 * w; j0 < hi; j0 += 16 * WAVES) {
+    f32x4 m[D / 16];
+    load_means<D>(a, bh, j0, lane, m);
+    done(j0, scores_of_blocks<D>(m, q));
   }
 }
 
-// ---- the choice ------------------------------------------------------------------------------------------------------
-// One workgroup to a list: the largest threshold that at least n_select keys reach is found bit by bit, then the blocks are written in rising order.
-// V > 0: thread t holds blocks t, t + 256, ..; V = 0: any number, read again for every bit.
-template <int V>
-struct Keys {
-  uint64_t k[V];
-  int n;
-  __device__ __forceinline__ Keys(const uint64_t *keys, int n_) : n(n_) {
+// Very many blocks: the keys go through memory, [rows][Tk].
+template <int D>
+__global__ __launch_bounds__(512) void scores_kernel(ScoreArgs a) {
+  const Sparse &s = a.s;
+  const int bh = blockIdx.z, b = bh / s.Hkv, t0 = blockIdx.x * kTiles, lane = threadIdx.x & 63, held = s.held(b), start = s.start(b);
+  f64x4 q[D / 16];
+  load_sums<D>(a, bh, t0, lane, q);
+  score_range<D, 8>(a, bh, blockIdx.y * 1024, min(s.Tk, (int)(blockIdx.y + 1) * 1024), threadIdx.x >> 6, lane, q, [&](int j0, f64x4 score) {
+    const int j = j0 + (lane & 15);
 #pragma unroll
-    for (int i = 0; i < V; ++i) k[i] = i * 256 + (int)threadIdx.x < n ? keys[i * 256 + threadIdx.x] : 0;
-  }
-  __device__ __forceinline__ int rounds() const { return V; }
-  __device__ __forceinline__ uint64_t at(int i) const { return k[i]; }
-};
-template <>
-struct Keys<0> {
-  const uint64_t *p;
-  int n;
-  __device__ __forceinline__ Keys(const uint64_t *keys, int n_) : p(keys), n(n_) {}
-  __device__ __forceinline__ int rounds() const { return (n + 255) / 256; }
-  __device__ __forceinline__ uint64_t at(int i) const { return i * 256 + (int)threadIdx.x < n ? p[i * 256 + threadIdx.x] : 0; }
-};
+    for (int v = 0; v < 4; ++v) {
+      const int t = t0 + 4 * v + (lane >> 4);
+      if (t < s.T && j < s.Tk) a.keys[((int64_t)bh * s.T + t) * s.Tk + j] = rank_key(a, held, start, t, j, score[v]);
+    }
+  });
+}
 
+// ---- the choice ------------------------------------------------------------------------------------------------------
+// A list is the blocks whose keys reach a threshold: the largest that at least n_select keys reach is found bit by bit from the top (the search ends as
+// soon as exactly n_select do), then the blocks are written in rising order.  If more reach it, it is the n_select-th largest key itself, and of
+// the blocks whose keys equal it the first are taken.
+// One wave, with the keys of blocks l, l + 64, .. in lane l.  The upper halves of the keys decide almost always; the lower ones are looked at where they do not.
 template <int V>
-__global__ __launch_bounds__(256) void choose_kernel(const uint64_t *keys, int Tk, int sel, int32_t *blocks) {
-  __shared__ int count[2][4];
+__device__ __forceinline__ void choose_wave(const uint64_t *keys, int sel, int32_t *out, int lane) {
+  uint32_t hi[V], lo[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint64_t k = keys[64 * i + lane];
+    hi[i] = (uint32_t)(k >> 32);
+    lo[i] = (uint32_t)k;
+  }
+  auto reach = [&](uint32_t y) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) c += __popcll(__ballot(hi[i] >= y));
+    return c;
+  };
+  uint32_t x = 1, y = 0;                // the threshold's halves (a key that may be chosen has an upper half of 1 or more)
+  int n = reach(1);                     // keys that reach it
+  if (n > sel) {
+    x = 0;
+    for (int bit = 31; bit >= 0 && n != sel; --bit) {
+      const int c = reach(x | 1u << bit);
+      if (c >= sel) {
+        x |= 1u << bit;
+        n = c;
+      }
+    }
+    if (n > sel) {
+      const int above = x == ~0u ? 0 : reach(x + 1);
+      for (int bit = 31; bit >= 0 && n != sel; --bit) {
+        int c = above;
+#pragma unroll
+        for (int i = 0; i < V; ++i) c += __popcll(__ballot(hi[i] == x && lo[i] >= (y | 1u << bit)));
+        if (c >= sel) {
+          y |= 1u << bit;
+          n = c;
+        }
+      }
+    }
+  }
+  // more than sel reach it: it is the sel-th largest key itself, and of the blocks whose keys equal it the first are taken
+  const bool ties = n > sel;
+  const uint64_t cut = (uint64_t)x << 32 | y;
+  int equal_left = 0, at = 0;
+  if (ties) {
+    equal_left = sel;
+#pragma unroll
+    for (int i = 0; i < V; ++i) equal_left -= __popcll(__ballot(((uint64_t)hi[i] << 32 | lo[i]) > cut));
+  }
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint64_t k = (uint64_t)hi[i] << 32 | lo[i];
+    const bool eq = ties && k == cut, over = ties ? k > cut : k >= cut;
+    const uint64_t m_eq = __ballot(eq), m_over = __ballot(over);
+    const int eq_before = __popcll(m_eq & below), place = at + __popcll(m_over & below) + min(eq_before, equal_left);
+    if (over || (eq && eq_before < equal_left)) out[place] = i * 64 + lane;
+    const int taken = min((int)__popcll(m_eq), equal_left);
+    at += __popcll(m_over) + taken;
+    equal_left -= taken;
+  }
+  for (int i = at + lane; i < sel; i += 64) out[i] = -1;
+}
+
+// Many tiles: a workgroup scores kTiles of them against all blocks (at most 64 V), then every wave makes one tile's choice.
+template <int D, int V>
+__global__ __launch_bounds__(1024) void score_and_choose_kernel(ScoreArgs a) {
+  const Sparse &s = a.s;
+  __shared__ uint64_t keys[kTiles][64 * V];
+  const int bh = blockIdx.y, b = bh / s.Hkv, t0 = blockIdx.x * kTiles, lane = threadIdx.x & 63, w = threadIdx.x >> 6, held = s.held(b), start = s.start(b);
+  {
+    f64x4 q[D / 16];
+    load_sums<D>(a, bh, t0, lane, q);
+    const int last = (s.Tk + 15) & ~15;
+    score_range<D, 16>(a, bh, 0, last, w, lane, q, [&](int j0, f64x4 score) {
+      const int j = j0 + (lane & 15);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) keys[4 * v + (lane >> 4)][j] = j < s.Tk ? rank_key(a, held, start, t0 + 4 * v + (lane >> 4), j, score[v]) : 0;
+    });
+    for (int i = threadIdx.x; i < kTiles * (64 * V - last); i += 1024) keys[i % kTiles][last + i / kTiles] = 0;
+  }
+  __syncthreads();
+  if (t0 + w < s.T) choose_wave<V>(keys[w], s.sel, a.blocks + ((int64_t)bh * s.T + t0 + w) * s.sel, lane);
+}
+
+// Few tiles.  A workgroup of WAVES waves forms the keys of one tile for blocks [lo, hi) from its queries on: their sum, then the scores, a block's mean to
+// eight lanes.  `part` is WAVES rows of D doubles.
+template <int D, bool F32, int WAVES>
+__device__ __forceinline__ void keys_of_tile(const ScoreArgs &a, int row, int lo, int hi, double (*part)[D], uint64_t *keys) {
+  const Sparse &s = a.s;
+  constexpr int TPR = D / 8, LPM = 8, PER = D / 32, ESZ = F32 ? 4 : 2, AT_ONCE = WAVES * 64 / LPM;
+  const int t = row % s.T, bh = row / s.T, b = bh / s.Hkv, h = bh % s.Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int held = s.held(b), start = s.start(b), n_rows = min(s.Nq - t * s.qb, s.qb);
+  double acc[8] = {0., 0., 0., 0., 0., 0., 0., 0.};
+  {
+    const int c = threadIdx.x % TPR, total = s.G * n_rows;
+    for (int i = threadIdx.x / TPR; i < total; i += WAVES * 64 / TPR) {
+      const int hd = i / n_rows;
+      const char *p = a.q.p + (b * a.q.sb + (int64_t)(h * s.G + hd) * a.q.sh + (int64_t)(t * s.qb + i - hd * n_rows) * a.q.sn + 8 * c) * ESZ;
+      if constexpr (F32) {
+        const f32x4 x = reinterpret_cast<const f32x4 *>(p)[0], y = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          acc[u] += (double)x[u];
+          acc[4 + u] += (double)y[u];
+        }
+      } else {
+        const bf16x8 x = *reinterpret_cast<const bf16x8 *>(p);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[u] += (double)static_cast<float>(x[u]);
+      }
+    }
+#pragma unroll
+    for (int d = TPR; d < 64; d <<= 1)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[u] += __shfl_xor(acc[u], d);
+    if (lane < TPR)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) part[w][8 * c + u] = acc[u];
+    __syncthreads();
+    if (threadIdx.x < D) {
+      double sum = part[0][threadIdx.x];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) sum += part[i][threadIdx.x];
+      part[0][threadIdx.x] = sum;       // (its own column: nobody else reads it before the barrier)
+    }
+    __syncthreads();
+  }
+  const int c = lane % LPM;
+  double q[PER][4];
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[i][u] = part[0][32 * i + 4 * c + u];
+  for (int j0 = lo; j0 < hi; j0 += AT_ONCE) {
+    const int j = j0 + (int)threadIdx.x / LPM;
+    const float *mean = a.means + ((int64_t)bh * s.Tk + min(j, s.Tk - 1)) * D + 4 * c;
+    f32x4 x[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = *reinterpret_cast<const f32x4 *>(mean + 32 * i);
+    double score = 0.;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) score = __builtin_fma((double)x[i][u], q[i][u], score);
+#pragma unroll
+    for (int d = 1; d < LPM; d <<= 1) score += __shfl_xor(score, d);
+    if (c == 0 && j < hi) keys[j] = rank_key(a, held, start, t, j, score);
+  }
+}
+
+// Up to 256 blocks: the whole choice of a tile in one launch.
+template <int D, bool F32>
+__global__ __launch_bounds__(512) void choose_row_kernel(ScoreArgs a) {
+  __shared__ double part[8][D];
+  __shared__ uint64_t keys[256];
+  if (threadIdx.x < 256 && (int)threadIdx.x >= a.s.Tk) keys[threadIdx.x] = 0;
+  keys_of_tile<D, F32, 8>(a, blockIdx.x, 0, a.s.Tk, part, keys);
+  __syncthreads();
+  if (threadIdx.x < 64) choose_wave<4>(keys, a.s.sel, a.blocks + (int64_t)blockIdx.x * a.s.sel, threadIdx.x);
+}
+
+// More: the means are many, so that a workgroup takes 128 of them, and a second launch makes the choice.
+template <int D, bool F32>
+__global__ __launch_bounds__(1024) void keys_kernel(ScoreArgs a) {
+  __shared__ double part[16][D];
+  keys_of_tile<D, F32, 16>(a, blockIdx.y, blockIdx.x * 128, min(a.s.Tk, (int)(blockIdx.x + 1) * 128), part, a.keys + (int64_t)blockIdx.y * a.s.Tk);
+}
+__global__ __launch_bounds__(64) void choose_1k_kernel(const uint64_t *keys, int Tk, int sel, int32_t *blocks) {
+  __shared__ uint64_t k[1024];
   const int64_t row = blockIdx.x;
-  const Keys<V> k(keys + row * Tk, Tk);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) k[64 * i + threadIdx.x] = 64 * i + (int)threadIdx.x < Tk ? keys[row * Tk + 64 * i + threadIdx.x] : 0;
+  choose_wave<16>(k, sel, blocks + row * sel, threadIdx.x);      // (every lane reads what it wrote)
+}
+
+// Very many blocks: 256 threads to a list, keys read from memory for every bit.
+__global__ __launch_bounds__(256) void choose_kernel(const uint64_t *all_keys, int Tk, int sel, int32_t *blocks) {
+  __shared__ int count[2][4], chosen[2][2][4];
+  const int64_t row = blockIdx.x;
+  const uint64_t *keys = all_keys + row * Tk;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, rounds = (Tk + 255) / 256;
+  auto key = [&](int i) { return i * 256 + (int)threadIdx.x < Tk ? keys[i * 256 + threadIdx.x] : 0; };
   int turn = 0;
-  // keys that are >= x, of the whole workgroup
   auto reach = [&](uint64_t x) {
     int c = 0;
-    if constexpr (V > 0) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) c += __popcll(__ballot(k.at(i) >= x));
-    } else {
-      for (int i = 0; i < k.rounds(); ++i) c += __popcll(__ballot(k.at(i) >= x));
-    }
+    for (int i = 0; i < rounds; ++i) c += __popcll(__ballot(key(i) >= x));
     if (lane == 0) count[turn][w] = c;
     __syncthreads();
     c = count[turn][0] + count[turn][1] + count[turn][2] + count[turn][3];
     turn ^= 1;
     return c;
   };
-  // x: reached by at least sel keys (or 1: by all that may be chosen), with as many bits decided as it takes
-  uint64_t x = 0;
+  uint64_t x = 1;
   int n = reach(1);
-  if (n <= sel) {
-    x = 1;
-  } else {
+  if (n > sel) {
+    x = 0;
     for (int bit = 63; bit >= 0 && n != sel; --bit) {
       const uint64_t y = x | (uint64_t)1 << bit;
       const int c = reach(y);
@@ -226,18 +408,14 @@ __global__ __launch_bounds__(256) void choose_kernel(const uint64_t *keys, int T
       }
     }
   }
-  // n keys reach x.  If they are more than sel, x is the sel-th largest key itself: of those equal to it the first are taken
-  int equal_left = sel;
-  if (n > sel) equal_left = sel - (x == ~(uint64_t)0 ? 0 : reach(x + 1));
-  else equal_left = n;
   const bool ties = n > sel;
+  int equal_left = ties ? sel - (x == ~(uint64_t)0 ? 0 : reach(x + 1)) : 0, at = 0;
   int32_t *out = blocks + row * sel;
-  int at = 0;
-  __shared__ int chosen[2][2][4];
-  for (int i = 0; i < k.rounds(); ++i) {
-    const uint64_t v = k.at(i);
-    const bool eq = ties && v == x, over = ties ? v > x : v >= x;
-    const uint64_t m_eq = __ballot(eq), m_over = __ballot(over), below = ((uint64_t)1 << lane) - 1;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int i = 0; i < rounds; ++i) {
+    const uint64_t k = key(i);
+    const bool eq = ties && k == x, over = ties ? k > x : k >= x;
+    const uint64_t m_eq = __ballot(eq), m_over = __ballot(over);
     if (lane == 0) {
       chosen[i & 1][0][w] = __popcll(m_eq);
       chosen[i & 1][1][w] = __popcll(m_over);
@@ -256,10 +434,10 @@ __global__ __launch_bounds__(256) void choose_kernel(const uint64_t *keys, int T
     }
     eq_before += __popcll(m_eq & below);
     over_before += __popcll(m_over & below);
-    const int taken_before = over_before + (ties ? min(eq_before, equal_left) : 0);
-    if (over || (eq && eq_before < equal_left)) out[at + taken_before] = i * 256 + threadIdx.x;
-    at += over_all + (ties ? min(eq_all, equal_left) : 0);
-    equal_left -= ties ? min(eq_all, equal_left) : 0;
+    if (over || (eq && eq_before < equal_left)) out[at + over_before + min(eq_before, equal_left)] = i * 256 + threadIdx.x;
+    const int taken = min(eq_all, equal_left);
+    at += over_all + taken;
+    equal_left -= taken;
   }
   for (int i = at + threadIdx.x; i < sel; i += 256) out[i] = -1;
 }
@@ -284,6 +462,10 @@ __global__ __launch_bounds__(256) void split_kernel(Sparse s, SplitJob j) {
 }
 
 size_t sums_bytes(const Sparse &s, int d) { return round256((size_t)s.B * s.Hkv * s.T * d * 8); }
+
+constexpr int kFusedBlocks = 1024;     // keys of kTiles tiles that fit LDS
+// Few tiles make their choice from the queries on, a workgroup or several each; many share passes over the means.
+bool few_tiles(const Sparse &s) { return (int64_t)s.B * s.Hkv * s.T <= 256; }
 
 // Blocks that are always kept, at most.
 int64_t forced_blocks(const ha_sparse_problem &p) {
@@ -340,7 +522,8 @@ extern "C" ha_status hybrid_attn_key_means(const ha_sparse_problem *p, const ha_
 extern "C" size_t hybrid_attn_select_workspace_bytes(const ha_sparse_problem *p) {
   if (check_sparse(p) != HA_OK) return 0;
   const Sparse s = sparse_of(*p);
-  return sums_bytes(s, p->d_head) + round256((size_t)s.B * s.Hkv * s.T * s.Tk * 8);
+  if (few_tiles(s) && s.Tk <= 256) return 0;
+  return sums_bytes(s, p->d_head) + (!few_tiles(s) && s.Tk <= kFusedBlocks ? 0 : round256((size_t)s.B * s.Hkv * s.T * s.Tk * 8));
 }
 
 extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const ha_view *q, const float *means, int32_t *blocks, void *workspace,
@@ -355,32 +538,51 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
   if (p->N_q == 0) return HA_OK;
   if (!blocks || (p->N_k > 0 && !means)) return HA_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(means) & 15u || reinterpret_cast<uintptr_t>(blocks) & 3u) return HA_ERR_ALIGN;
-  if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < hybrid_attn_select_workspace_bytes(p)) return HA_ERR_WORKSPACE;
+  const size_t need = hybrid_attn_select_workspace_bytes(p);
+  if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < need)) return HA_ERR_WORKSPACE;
   double *sums = static_cast<double *>(workspace);
   uint64_t *keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + sums_bytes(s, p->d_head));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const unsigned rows = (unsigned)s.B * s.Hkv * s.T;
+  const ScoreArgs a{s, qv, sums, means, keys, blocks, p->keep_first, p->near_tokens};
   hipError_t e;
-  if (s.Tk > 0) {
-#define HA_SUMS(D, F) query_sums_kernel<D, F><<<rows, 256, 0, stream>>>(s, qv, sums)
-    if (p->d_head == 128) { if (p->dtype == HA_F32) HA_SUMS(128, true); else HA_SUMS(128, false); }
-    else { if (p->dtype == HA_F32) HA_SUMS(64, true); else HA_SUMS(64, false); }
-#undef HA_SUMS
-    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
-    constexpr int TILES = 8;
-    const ScoreArgs a{s, sums, means, keys, p->keep_first, p->near_tokens};
-    const dim3 grid((s.Tk + 255) / 256, (s.T + TILES - 1) / TILES, s.B * s.Hkv);
-    if (p->d_head == 128) scores_kernel<128, TILES><<<grid, 256, 0, stream>>>(a);
-    else scores_kernel<64, TILES><<<grid, 256, 0, stream>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+  if (few_tiles(s)) {
+#define HA_ROW(K, ...) do { \
+    if (p->d_head == 128) { if (p->dtype == HA_F32) K<128, true>__VA_ARGS__(a); else K<128, false>__VA_ARGS__(a); } \
+    else { if (p->dtype == HA_F32) K<64, true>__VA_ARGS__(a); else K<64, false>__VA_ARGS__(a); } } while (0)
+    if (s.Tk <= 256) {
+      HA_ROW(choose_row_kernel, <<<rows, 512, 0, stream>>>);
+    } else {
+      HA_ROW(keys_kernel, <<<dim3((s.Tk + 127) / 128, rows), 1024, 0, stream>>>);
+      if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+      if (s.Tk <= 1024) choose_1k_kernel<<<rows, 64, 0, stream>>>(keys, s.Tk, s.sel, blocks);
+      else choose_kernel<<<rows, 256, 0, stream>>>(keys, s.Tk, s.sel, blocks);
+    }
+#undef HA_ROW
+    e = hipGetLastError();
+    return e == hipSuccess ? HA_OK : device_error(e);
   }
-#define HA_CHOOSE(V) choose_kernel<V><<<rows, 256, 0, stream>>>(keys, s.Tk, s.sel, blocks)
-  if (s.Tk <= 256) HA_CHOOSE(1);
-  else if (s.Tk <= 512) HA_CHOOSE(2);
-  else if (s.Tk <= 1024) HA_CHOOSE(4);
-  else if (s.Tk <= 2048) HA_CHOOSE(8);
-  else HA_CHOOSE(0);
-#undef HA_CHOOSE
+#define HA_SUMS(D, F) query_sums_kernel<D, F><<<rows, 256, 0, stream>>>(s, qv, sums)
+  if (p->d_head == 128) { if (p->dtype == HA_F32) HA_SUMS(128, true); else HA_SUMS(128, false); }
+  else { if (p->dtype == HA_F32) HA_SUMS(64, true); else HA_SUMS(64, false); }
+#undef HA_SUMS
+  if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+  const unsigned groups = (s.T + kTiles - 1) / kTiles, heads = (unsigned)s.B * s.Hkv;
+  if (s.Tk <= kFusedBlocks) {
+#define HA_FUSED(V) (p->d_head == 128 ? score_and_choose_kernel<128, V><<<dim3(groups, heads), 1024, 0, stream>>>(a) \
+                                      : score_and_choose_kernel<64, V><<<dim3(groups, heads), 1024, 0, stream>>>(a))
+    if (s.Tk <= 256) HA_FUSED(4);
+    else if (s.Tk <= 512) HA_FUSED(8);
+    else if (s.Tk <= 640) HA_FUSED(10);
+    else HA_FUSED(16);
+#undef HA_FUSED
+  } else {
+    const dim3 grid(groups, (s.Tk + 1023) / 1024, heads);
+    if (p->d_head == 128) scores_kernel<128><<<grid, 512, 0, stream>>>(a);
+    else scores_kernel<64><<<grid, 512, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+    choose_kernel<<<rows, 256, 0, stream>>>(keys, s.Tk, s.sel, blocks);
+  }
   e = hipGetLastError();
   return e == hipSuccess ? HA_OK : device_error(e);
 }

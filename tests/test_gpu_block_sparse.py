@@ -154,6 +154,21 @@ def test_long_lists(dtype):
     check(problem(14, H=1, Hkv=1, Nq=70, Nk=9000, dtype=dtype, d=64, qb=64, kb=64, sel=140))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,Nq", [(1, 1), (3, 1), (8, 4), (32, 1), (5, 6), (1, 32), (33, 1), (11, 3)])
+def test_few_queries(dtype, d, G, Nq):
+    # one list for all queries of a group: up to 32 of them, and one more
+    for sel, kb in ((1, 64), (7, 128), (40, 64)):
+        check(problem(23, B=2, H=2 * G, Hkv=2, Nq=Nq, Nk=2777, d=d, dtype=dtype, kb=kb, sel=sel, causal=True, ragged=[2777, 1500], starts=[2777 - Nq, 1500 - Nq]), grad=False)
+    check(problem(24, H=G, Hkv=1, Nq=Nq, Nk=200, d=d, dtype=dtype, sel=3, layout="bnhd"))
+
+
+def test_many_heads_of_few_queries():
+    check(problem(25, B=70, H=4, Hkv=4, Nq=1, Nk=300, d=64, sel=4), grad=False)            # lists that are not cut
+    check(problem(26, B=3, H=2, Hkv=1, Nq=9, Nk=20000, d=64, sel=200, kb=64), grad=False)   # and ones that are, into many ranges
+
+
 def test_popular_blocks_are_joined_from_parts():
     p = problem(15, H=2, Hkv=1, Nq=64 * 150 + 3, Nk=200, d=64, qb=64, kb=64, sel=2)       # 151 tiles on four blocks: parts of 64
     check(p)
@@ -292,6 +307,17 @@ def test_choice_of_many_blocks_for_one_query(Nk, sel):
     q, k = tokens(gen, 2, 2, 1, 64, BF16), tokens(gen, 2, 1, Nk, 64, BF16)
     got, want = chosen(q, k, sel, 128, 64, causal=True, near=0)
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("N,Nk,H,sel,kb", [(64 * 300, 64 * 200, 1, 5, 64), (64 * 130, 64 * 600, 2, 16, 64), (64 * 100, 64 * 1000, 3, 9, 64), (64 * 260, 128 * 1100, 1, 64, 128)])
+def test_choice_of_many_tiles(N, Nk, H, sel, kb):
+    gen = torch.Generator().manual_seed(36)
+    q, k = tokens(gen, 1, H, N - 7, 64, BF16), tokens(gen, 1, H, Nk - 1, 64, BF16)
+    means = ha.hybrid_attn_key_means(k, kb)
+    got = ha.hybrid_attn_select_blocks(q, means, Nk - 1, sel, 64, kb)
+    rows = torch.nn.functional.pad(q.double(), (0, 0, 0, 7)).view(1, H, N // 64, 64, 64).sum(3)
+    best = torch.sort(rows @ means.double().transpose(2, 3).contiguous(), dim=3, descending=True, stable=True).indices[..., :sel]
+    assert torch.equal(got, best.sort(dim=3).values.to(torch.int32))
 
 
 def test_choice_of_ragged_batches():

@@ -115,10 +115,12 @@ def test_pointers_and_workspaces(lib):
     for ws, size in ((None, need), (aligned, need - 1), (aligned + 128, need)):
         assert grad(lib, ws=ws, size=size) == WORKSPACE
     assert grad(lib, blocks=None) == NULL and grad(lib, lse=None) == NULL and grad(lib, lse=FAKE + 1) == ALIGN
-    need = lib.hybrid_attn_select_workspace_bytes(problem())
+    many = problem(N_q=128 * 100)                       # (few tiles need none)
+    need = lib.hybrid_attn_select_workspace_bytes(many)
+    assert need > 0
 
     def select(p=None, means=FAKE, out=FAKE, ws=aligned, size=need):
-        return lib.hybrid_attn_select_blocks(p or problem(), view(), means, out, ws, size, None)
+        return lib.hybrid_attn_select_blocks(p or many, view(n=128 * 100), means, out, ws, size, None)
     assert select(means=None) == NULL and select(out=None) == NULL and select(means=FAKE + 4) == ALIGN and select(out=FAKE + 1) == ALIGN
     assert select(ws=None) == WORKSPACE and select(size=need - 1) == WORKSPACE and select(ws=aligned + 64) == WORKSPACE
     # a causal choice without the tile's own blocks would look at later keys; kept blocks have to fit the list
