@@ -6,7 +6,8 @@
     dq, dk, dv = hybrid_attn_sparse_grad(q, k, v, blocks, out, lse, grad_out)
 
 q is a [B, H, N_q, d] view, k and v are [B, H_kv, N_k, d] views (H a multiple of H_kv), each with strides of its own and a contiguous last dimension.
-Argument marshalling only, as in hybrid_attn; everything is public there.
+Argument marshalling only, as in hybrid_attn; everything is public there.  Plain calls are marshalled by compiled code (csrc/ha_binding_calls.h), all others, and
+every error, here.
 """
 from __future__ import annotations
 
@@ -125,10 +126,17 @@ def hybrid_attn_sparse_grad_workspace_bytes(problem: ha_sparse_problem) -> int:
     return _ha._lib().hybrid_attn_sparse_grad_workspace_bytes(problem)
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_key_means(k, k_block: int = 64, key_len=None, only_last: int = 0, out=None, stream=None):
     """Mean of the keys of every block (those below key_len, int32 [B] or None: all): fp32 [B, H_kv, ceil(N_k / k_block), d].  only_last = m > 0 writes only
     the last m blocks of every batch entry that hold a key, into `out`, which then has to be given.  Does not synchronise."""
+    native = _ha._CALLS or _ha._calls()
+    if native and (means := native.key_means(k, k_block, key_len, only_last, out, stream)) is not None:
+        return means
+    return _key_means(k, k_block, key_len, only_last, out, stream)
+
+
+@_ha._allocations_follow_stream
+def _key_means(k, k_block, key_len, only_last, out, stream):
     _ha._require_gpu(k, out)
     if k.dim() != 4:
         raise ValueError("k must be a [B, H_kv, N_k, d] view")
@@ -146,12 +154,19 @@ def hybrid_attn_key_means(k, k_block: int = 64, key_len=None, only_last: int = 0
     return out
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_select_blocks(q, means, n_keys: int, n_select: int, q_block: int = 128, k_block: int = 64, causal: bool = False, q_start=None, key_len=None,
                               keep_first: int = 0, near: int = -1, out=None, workspace=None, stream=None):
     """The n_select key blocks of highest score (sum of the tile's queries times the block's mean) for every tile of q_block queries: int32
     [B, H_kv, ceil(N_q / q_block), n_select] in rising order, -1 behind the last.  n_keys: N_k.  keep_first leading blocks and, with near >= 0, those
     within `near` tokens of the tile's positions are always among them.  Does not synchronise."""
+    native = _ha._CALLS or _ha._calls()
+    if native and (blocks := native.select_blocks(q, means, n_keys, n_select, q_block, k_block, causal, q_start, key_len, keep_first, near, out, workspace, stream)) is not None:
+        return blocks
+    return _select_blocks(q, means, n_keys, n_select, q_block, k_block, causal, q_start, key_len, keep_first, near, out, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _select_blocks(q, means, n_keys, n_select, q_block, k_block, causal, q_start, key_len, keep_first, near, out, workspace, stream):
     _ha._require_gpu(q, means, out, workspace)
     if q.dim() != 4 or means.dim() != 4:
         raise ValueError("q must be a [B, H, N_q, d] view and means [B, H_kv, blocks, d]")
@@ -182,12 +197,19 @@ def _attention_problem(q, k, v, blocks, q_block, k_block, causal, q_start, key_l
     return prob
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_sparse_forward(q, k, v, blocks, q_block: int = 128, k_block: int = 64, causal: bool = False, q_start=None, key_len=None,
                                softmax_scale: Optional[float] = None, with_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """Softmax attention of every query over the keys of its tile's blocks; returns (out, lse): out like q, lse fp32 [B, H, N_q] (the logarithm of every
     row's sum of weights, what the gradients take) or None without with_lse.  causal: query i, at position q_start[b] + i (int32 [B], or None:
     N_k - N_q + i), sees the keys up to its own position; keys at and behind key_len (int32 [B], or None) are never seen.  Does not synchronise."""
+    native = _ha._CALLS or _ha._calls()
+    if native and (pair := native.sparse_forward(q, k, v, blocks, q_block, k_block, causal, q_start, key_len, softmax_scale, with_lse, out, lse, workspace, stream)) is not None:
+        return pair
+    return _sparse_forward(q, k, v, blocks, q_block, k_block, causal, q_start, key_len, softmax_scale, with_lse, out, lse, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _sparse_forward(q, k, v, blocks, q_block, k_block, causal, q_start, key_len, softmax_scale, with_lse, out, lse, workspace, stream):
     _ha._require_gpu(q, k, v, blocks, out, lse, workspace)
     with _ha._on_device_of(q):
         prob = _attention_problem(q, k, v, blocks, q_block, k_block, causal, q_start, key_len, softmax_scale)
@@ -207,11 +229,19 @@ def hybrid_attn_sparse_forward(q, k, v, blocks, q_block: int = 128, k_block: int
     return out, lse
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_sparse_grad(q, k, v, blocks, out, lse, grad_out, q_block: int = 128, k_block: int = 64, causal: bool = False, q_start=None, key_len=None,
                             softmax_scale: Optional[float] = None, grad_q=None, grad_k=None, grad_v=None, workspace=None, stream=None):
     """Gradients of q, k and v (in their dtype) from that of `out`; out and lse as hybrid_attn_sparse_forward returned them for the same
     arguments.  Returns (grad_q, grad_k, grad_v).  Does not synchronise."""
+    native = _ha._CALLS or _ha._calls()
+    if native and (grads := native.sparse_grad(q, k, v, blocks, out, lse, grad_out, q_block, k_block, causal, q_start, key_len, softmax_scale, grad_q, grad_k, grad_v,
+                                               workspace, stream)) is not None:
+        return grads
+    return _sparse_grad(q, k, v, blocks, out, lse, grad_out, q_block, k_block, causal, q_start, key_len, softmax_scale, grad_q, grad_k, grad_v, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _sparse_grad(q, k, v, blocks, out, lse, grad_out, q_block, k_block, causal, q_start, key_len, softmax_scale, grad_q, grad_k, grad_v, workspace, stream):
     _ha._require_gpu(q, k, v, blocks, out, lse, grad_out, grad_q, grad_k, grad_v, workspace)
     with _ha._on_device_of(q):
         prob = _attention_problem(q, k, v, blocks, q_block, k_block, causal, q_start, key_len, softmax_scale)

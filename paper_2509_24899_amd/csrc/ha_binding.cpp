@@ -7,10 +7,16 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
+
+#include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <limits>
 
-#include "../../include/hybrid_attn.h"
+#include "../../include/hybrid_attn_optim.h"
+#include "../../include/hybrid_attn_sparse.h"
 
 namespace {
 
@@ -234,7 +240,16 @@ PyObject *bind(PyObject *, PyObject *args) {
   Py_RETURN_NONE;
 }
 
-PyMethodDef methods[] = {{"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr},
+}  // namespace
+
+#include "ha_binding_calls.h"
+
+namespace {
+
+#define HA_FAST(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {HA_FAST(key_means), HA_FAST(select_blocks), HA_FAST(sparse_forward), HA_FAST(sparse_grad), HA_FAST(grad_norm), HA_FAST(grad_clip),
+                         HA_FAST(update_many), {"bind_calls", bind_calls, METH_VARARGS, nullptr},
+                         {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr},
                          {"param_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(param_update)), METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
@@ -254,6 +269,13 @@ PyMODINIT_FUNC PyInit_hybridattn_binding() {
                                 static_cast<Py_ssize_t>(sizeof(ha_optimizer)));
   if (!abi || PyModule_AddObject(m, "abi", abi) < 0) {
     Py_XDECREF(abi);
+    Py_DECREF(m);
+    return nullptr;
+  }
+  PyObject *calls_abi = Py_BuildValue("(nnnn)", static_cast<Py_ssize_t>(sizeof(ha_sparse_problem)), static_cast<Py_ssize_t>(sizeof(ha_view)),
+                                      static_cast<Py_ssize_t>(sizeof(ha_tensor)), static_cast<Py_ssize_t>(sizeof(ha_param)));
+  if (!calls_abi || PyModule_AddObject(m, "calls_abi", calls_abi) < 0) {
+    Py_XDECREF(calls_abi);
     Py_DECREF(m);
     return nullptr;
   }

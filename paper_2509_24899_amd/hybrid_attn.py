@@ -175,6 +175,32 @@ def _binding():
     return _BINDING
 
 
+_CALLS = None
+
+
+def _calls():
+    """The same module, bound to the calls of block_sparse and optim as well, or False.  Looked for once, like _binding's result."""
+    global _CALLS
+    if _CALLS is None:
+        native = _binding()
+        if native is None:
+            return False                                  # (no library yet, which the call will report)
+        if native:
+            from . import block_sparse, optim
+            sizes = tuple(ctypes.sizeof(s) for s in (block_sparse.ha_sparse_problem, block_sparse.ha_view, optim.ha_tensor, optim.ha_param))
+            current = getattr(torch._C, "_cuda_getDevice", None)
+            if native.calls_abi != sizes or current is None:
+                native = False
+            else:
+                lib = _lib()
+                native.bind_calls(tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+                    "hybrid_attn_key_means", "hybrid_attn_select_workspace_bytes", "hybrid_attn_select_blocks", "hybrid_attn_sparse_workspace_bytes",
+                    "hybrid_attn_sparse_forward", "hybrid_attn_sparse_grad_workspace_bytes", "hybrid_attn_sparse_grad", "hybrid_attn_grad_norm",
+                    "hybrid_attn_grad_clip", "hybrid_attn_param_update_many")), current)
+        _CALLS = native
+    return _CALLS
+
+
 def _mismatch(what):
     raise ValueError(f"feature map does not match the problem: {what}")
 

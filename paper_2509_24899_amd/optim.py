@@ -4,7 +4,7 @@
     result = hybrid_attn_grad_norm(grads, max_norm)                                     # device (norm, factor)
     hybrid_attn_param_update_many(params, lr, kind=HA_OPT_ADAMW, step=step, clip=result)
 
-Argument marshalling only, as in hybrid_attn; everything is public there.
+Argument marshalling only, as in hybrid_attn; everything is public there.  Plain calls are marshalled by compiled code (csrc/ha_binding_calls.h).
 """
 from __future__ import annotations
 
@@ -45,6 +45,11 @@ def _one_device(tensors):
     return devices.pop() if devices else None
 
 
+def _native(c, n, workspace_bytes, device):
+    """What the compiled marshalling reads of a list."""
+    return ctypes.addressof(c), n, workspace_bytes, -1 if device is None else device.index
+
+
 class TensorList:
     """Contiguous bf16 or fp32 tensors on one GPU, with their descriptors for the C ABI.  It holds the tensors; a program whose gradients keep their
     memory over its steps builds it once, one whose gradients are new tensors every step builds it every step."""
@@ -53,7 +58,9 @@ class TensorList:
         self.tensors = list(tensors)
         self.device = _one_device(self.tensors)
         self.c = (ha_tensor * len(self.tensors))(*[(t.data_ptr(), t.numel(), _ha._dtype_code(t), 0) for t in self.tensors])
+        self.sizes = [t.numel() for t in self.tensors]
         self.workspace_bytes = _ha._lib().hybrid_attn_grad_norm_workspace_bytes(len(self.tensors), self.c)
+        self.native = _native(self.c, len(self.tensors), self.workspace_bytes, self.device)
 
     def __len__(self):
         return len(self.tensors)
@@ -81,6 +88,7 @@ class ParamList:
             return None if t is None else t.data_ptr()
         self.c = (ha_param * n)(*[(at(p), at(g), at(a), at(b), at(c), p.numel(), _ha._dtype_code(g), _ha.HA_BF16 if c is None else _ha._dtype_code(c))
                                   for p, g, a, b, c in zip(*self.tensors)])
+        self.native = _native(self.c, n, 0, self.device)
 
     def __len__(self):
         return len(self.tensors[0])
@@ -100,11 +108,18 @@ def hybrid_attn_grad_norm_workspace_bytes(grads) -> int:
     return _tensor_list(grads).workspace_bytes
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_grad_norm(grads, max_norm: float = float("inf"), result=None, workspace=None, stream=None):
     """Enqueue the global 2-norm of a TensorList (or a list of tensors) and the factor min(1, max_norm / norm) that brings it down to max_norm: returns
     a device fp32 tensor (norm, factor).  The factor is NaN where the norm is not finite.  Does not synchronise."""
     grads = _tensor_list(grads)
+    native = _ha._CALLS or _ha._calls()
+    if native and (done := native.grad_norm(grads, max_norm, result, workspace, stream)) is not None:
+        return done
+    return _grad_norm(grads, max_norm, result, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _grad_norm(grads, max_norm, result, workspace, stream):
     device = grads.device if grads.device is not None else result.device if result is not None else torch.device("cuda", torch.cuda.current_device())
     with _ha._on_device(device):
         if result is None:
@@ -127,8 +142,11 @@ def hybrid_attn_grad_clip(grads, result, out=None, stream=None):
     leaves out as it was.  Does not synchronise."""
     grads = _tensor_list(grads)
     out = grads if out is None else _tensor_list(out)
-    if len(out) != len(grads) or any(a.numel() != b.numel() for a, b in zip(grads.tensors, out.tensors)):
+    if out.sizes != grads.sizes:
         raise ValueError("out must be a list of tensors of the gradients' sizes")
+    native = _ha._CALLS or _ha._calls()
+    if native and native.grad_clip(grads, result, out, stream) is not None:
+        return
     _ha._require_gpu(result)
     if grads.device is not None and out.device != grads.device:
         raise ValueError(f"out must be on {grads.device}")
@@ -143,6 +161,9 @@ def hybrid_attn_param_update_many(params: ParamList, lr: float, kind: int = 0, s
                                   beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01, clip=None, stream=None):
     """One update of all parameters of a ParamList in place, as hybrid_attn_param_update makes it of one.  clip: hybrid_attn_grad_norm's result, whose factor
     multiplies the gradients besides grad_scale; where it is not finite, nothing changes.  Does not synchronise."""
+    native = _ha._CALLS or _ha._calls()
+    if native and native.update_many(params, lr, kind, step, grad_scale, beta1, beta2, eps, weight_decay, clip, stream) is not None:
+        return
     if clip is not None:
         _ha._require_gpu(clip)
         _result(clip, params.device)
