@@ -196,12 +196,13 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
                        q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
-// fp32 tensors: 32 keys at a time in three pieces.
+// fp32 tensors: 32 keys at a time in three pieces.  Two waves (tiles of 64 queries) take one stage of LDS and leave room for two more workgroups, whose
+// work covers the loads; two stages would leave the CU with these two waves.
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void sparse_fwd_f32_kernel(FwdArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS);
-  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];      // [2 stages][k | v][pieces][ROWS]
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS), STAGES = NW == 2 ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * NS * STAGE];      // [stage][k | v][pieces][ROWS]
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -247,10 +248,10 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_fwd_f32_kernel(FwdArgs a) {
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
 
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
-  for (int stage = 0; key >= 0; stage ^= 1) {
+  for (int stage = 0; key >= 0; stage ^= STAGES - 1) {
     const int next = walk.next();
     landed();
-    if (next >= 0) request(next, stage ^ 1);
+    if (STAGES == 2 && next >= 0) request(next, stage ^ 1);
     const unsigned rows = rows0 + stage * (2 * NS * STAGE), cols = cols0 + stage * (2 * NS * STAGE);
     f32x16 sc[ROWS / 32];
 #pragma unroll
@@ -308,6 +309,10 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_fwd_f32_kernel(FwdArgs a) {
           o[rb] = mfma_split<NS>(vf, pb, o[rb]);
         }
       }
+    if (STAGES == 1) {
+      __syncthreads();                                // every wave is done with the stage
+      if (next >= 0) request(next, 0);
+    }
     key = next;
   }
   l = xhalf_sum(l);

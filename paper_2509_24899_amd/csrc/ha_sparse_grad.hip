@@ -16,7 +16,7 @@ namespace ha {
 namespace {
 
 constexpr int kPart = 64;        // tiles of an inverse list that one workgroup takes, at most
-constexpr int kChunk = 16;       // tiles counted together while the inverse lists are built
+constexpr int kChunk = 8;        // tiles counted together while the inverse lists are built
 
 struct GradArgs {
   Sparse s;
@@ -99,10 +99,15 @@ __global__ __launch_bounds__(1024) void inverse_scan_kernel(GradArgs a) {
     const int j = j0 + threadIdx.x;
     int n = 0;
     if (j < s.Tk)
-      for (int c = 0; c < a.n_chunks; ++c) {
-        const int x = h[(int64_t)c * s.Tk + j];
-        h[(int64_t)c * s.Tk + j] = n;
-        n += x;
+      for (int c = 0; c < a.n_chunks; c += 8) {
+        int x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = c + i < a.n_chunks ? h[(int64_t)(c + i) * s.Tk + j] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (c + i < a.n_chunks) h[(int64_t)(c + i) * s.Tk + j] = n;
+          n += x[i];
+        }
       }
     const int parts = j < s.Tk ? max(1, (n + a.part_tiles - 1) / a.part_tiles) : 0;
     const int3 mine = {n, parts, parts > 1 ? parts : 0};
@@ -199,10 +204,11 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 template <int D, bool F32, int NW>
-__global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
+__global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW == 4 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
   typedef Tile<D> T;
   constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
-  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * NS * STAGE];
+  constexpr int STAGES = F32 && NW == 2 ? 1 : 2;      // (as in the forward)
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * NS * STAGE];
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -244,10 +250,10 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
-  for (int stage = 0; key >= 0; stage ^= 1) {
+  for (int stage = 0; key >= 0; stage ^= STAGES - 1) {
     const int next = walk.next();
     landed();
-    if (next >= 0) request(next, stage ^ 1);
+    if (STAGES == 2 && next >= 0) request(next, stage ^ 1);
     const unsigned rows = rows0 + stage * (2 * NS * STAGE), cols = cols0 + stage * (2 * NS * STAGE);
     const bool mask = key + ROWS > wave_limit;
 #pragma unroll
@@ -287,6 +293,10 @@ __global__ __launch_bounds__(64 * NW, !F32 && NW == 4 ? 2 : 1) void sparse_dq_ke
           o[rb] = mfma_split<NS>(kf, db, o[rb]);
         }
       }
+    }
+    if (STAGES == 1) {
+      __syncthreads();
+      if (next >= 0) request(next, 0);
     }
     key = next;
   }
@@ -486,7 +496,8 @@ template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) {
   typedef Tile<D> T;
   constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS), STAT = 2 * 32 * 4;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * (2 * NS * STAGE + STAT)];      // [2 stages][q | dO][pieces][ROWS], lse2 | delta
+  constexpr int STAGES = NW == 2 ? 1 : 2;             // (as in the forward)
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * (2 * NS * STAGE + STAT)];      // [stage][q | dO][pieces][ROWS], lse2 | delta
   const Sparse &s = a.s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
   if ((int)blockIdx.x >= *a.n_work) return;
@@ -549,10 +560,10 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
     for (int x = 0; x < 16; ++x) dk[rb][x] = dv[rb][x] = 0.f;
 
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
-  for (int stage = 0; cur.row >= 0; stage ^= 1) {
+  for (int stage = 0; cur.row >= 0; stage ^= STAGES - 1) {
     const Step next = next_step();
     landed();
-    if (next.row >= 0) request(next, stage ^ 1);
+    if (STAGES == 2 && next.row >= 0) request(next, stage ^ 1);
     const char *tq = lds + stage * (2 * NS * STAGE + STAT);
     const unsigned rows = rows0 + stage * (2 * NS * STAGE + STAT), cols = cols0 + stage * (2 * NS * STAGE + STAT);
     const float *stat = reinterpret_cast<const float *>(tq + 2 * NS * STAGE);
@@ -616,6 +627,10 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
           dk[rb] = mfma_split<NS>(qf, db, dk[rb]);
         }
       }
+    }
+    if (STAGES == 1) {
+      __syncthreads();
+      if (next.row >= 0) request(next, 0);
     }
     cur = next;
   }

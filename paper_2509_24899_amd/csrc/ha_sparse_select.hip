@@ -221,14 +221,30 @@ __device__ __forceinline__ void choose_wave(const uint64_t *keys, int sel, int32
   uint32_t x = 1, y = 0;                // the threshold's halves (a key that may be chosen has an upper half of 1 or more)
   int n = reach(1);                     // keys that reach it
   if (n > sel) {
-    x = 0;
-    for (int bit = 31; bit >= 0 && n != sel; --bit) {
+    // Every lane's largest key reaches the smallest of these, so that at least 64 keys do: the threshold lies between it and the largest key of all, and what
+    // the two have in common (sign and most of the exponent, as a rule) need not be searched.
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) most = max(most, hi[i]);
+    uint32_t least = sel <= 64 ? most : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      most = max(most, (uint32_t)__shfl_xor(most, d));
+      least = min(least, (uint32_t)__shfl_xor(least, d));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+    const int bits = most == least ? 0 : 32 - __builtin_clz(most ^ least);
+    x = bits == 32 ? 0 : most >> bits << bits;
+    n = INT_MAX;
+    for (int bit = bits - 1; bit >= 0 && n != sel; --bit) {
       const int c = reach(x | 1u << bit);
       if (c >= sel) {
         x |= 1u << bit;
         n = c;
       }
     }
+    if (n == INT_MAX) n = reach(x);
     if (n > sel) {
       const int above = x == ~0u ? 0 : reach(x + 1);
       for (int bit = 31; bit >= 0 && n != sel; --bit) {
