@@ -248,7 +248,7 @@ namespace {
 
 #define HA_FAST(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HA_FAST(key_means), HA_FAST(select_blocks), HA_FAST(sparse_forward), HA_FAST(sparse_grad), HA_FAST(grad_norm), HA_FAST(grad_clip),
-                         HA_FAST(update_many), {"bind_calls", bind_calls, METH_VARARGS, nullptr},
+                         HA_FAST(update_many), HA_FAST(describe_tensors), HA_FAST(describe_params), {"bind_calls", bind_calls, METH_VARARGS, nullptr},
                          {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr},
                          {"param_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(param_update)), METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},

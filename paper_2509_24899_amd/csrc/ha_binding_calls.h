@@ -372,6 +372,81 @@ PyObject *update_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 #undef HA_CALL
 
+// One tensor of a list: contiguous, on the GPU that *device names (-1: none yet), of a type that the library has.
+bool listed(PyObject *o, int64_t *device, const at::Tensor **t, int32_t *type) {
+  *t = tensor(o);
+  if (!*t || !(*t)->is_cuda() || !(*t)->is_contiguous() || (*device >= 0 && (*t)->get_device() != *device)) return false;
+  if ((*t)->scalar_type() != at::kFloat && (*t)->scalar_type() != at::kBFloat16) return false;
+  *device = (*t)->get_device();
+  *type = (*t)->scalar_type() == at::kFloat ? HA_F32 : HA_BF16;
+  return true;
+}
+
+// describe_tensors(list, address of as many ha_tensor) -> (device index, sizes), or None
+PyObject *describe_tensors(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 2 || !PyList_CheckExact(args[0])) Py_RETURN_NONE;
+  try {
+    ha_tensor *to = static_cast<ha_tensor *>(PyLong_AsVoidPtr(args[1]));
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    const Ref sizes(PyList_New(count));
+    if (!to || !sizes.p) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    int64_t device = -1;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const at::Tensor *t;
+      int32_t type;
+      if (!listed(PyList_GET_ITEM(args[0], i), &device, &t, &type)) Py_RETURN_NONE;
+      to[i] = ha_tensor{t->data_ptr(), static_cast<uint64_t>(t->numel()), type, 0};
+      PyObject *size = PyLong_FromLongLong(t->numel());
+      if (!size) return nullptr;
+      PyList_SET_ITEM(sizes.p, i, size);
+    }
+    return Py_BuildValue("(LO)", static_cast<long long>(device), sizes.p);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// describe_params((masters, grads, m, v, copies), address of as many ha_param) -> device index, or None
+PyObject *describe_params(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 2 || !PyTuple_CheckExact(args[0]) || PyTuple_GET_SIZE(args[0]) != 5) Py_RETURN_NONE;
+  try {
+    ha_param *to = static_cast<ha_param *>(PyLong_AsVoidPtr(args[1]));
+    PyObject *list[5];
+    for (int f = 0; f < 5; ++f) {
+      list[f] = PyTuple_GET_ITEM(args[0], f);
+      if (!PyList_CheckExact(list[f]) || PyList_GET_SIZE(list[f]) != PyList_GET_SIZE(list[0])) Py_RETURN_NONE;
+    }
+    if (!to) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    int64_t device = -1;
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list[0]); ++i) {
+      void *at[5];
+      int32_t type[5] = {HA_F32, HA_F32, HA_F32, HA_F32, HA_BF16};
+      int64_t size = 0;
+      for (int f = 0; f < 5; ++f) {
+        PyObject *o = PyList_GET_ITEM(list[f], i);
+        at[f] = nullptr;
+        if (f >= 2 && o == Py_None) continue;
+        const at::Tensor *t;
+        if (!listed(o, &device, &t, &type[f]) || (f != 1 && f != 4 && type[f] != HA_F32) || (f > 0 && t->numel() != size)) Py_RETURN_NONE;
+        size = t->numel();
+        at[f] = t->data_ptr();
+      }
+      to[i] = ha_param{static_cast<float *>(at[0]), at[1], static_cast<float *>(at[2]), static_cast<float *>(at[3]), at[4], static_cast<uint64_t>(size), type[1], type[4]};
+    }
+    return PyLong_FromLongLong(device);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
 // bind_calls(addresses of the ten functions in the order of Calls, current-device function)
 PyObject *bind_calls(PyObject *, PyObject *args) {
   PyObject *list, *get_device;

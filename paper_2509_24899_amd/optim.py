@@ -56,9 +56,14 @@ class TensorList:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        self.device = _one_device(self.tensors)
-        self.c = (ha_tensor * len(self.tensors))(*[(t.data_ptr(), t.numel(), _ha._dtype_code(t), 0) for t in self.tensors])
-        self.sizes = [t.numel() for t in self.tensors]
+        self.c = (ha_tensor * len(self.tensors))()
+        native = _ha._CALLS or _ha._calls()
+        if native and self.tensors and (done := native.describe_tensors(self.tensors, ctypes.addressof(self.c))) is not None:
+            self.device, self.sizes = torch.device("cuda", done[0]), done[1]
+        else:
+            self.device = _one_device(self.tensors)
+            self.c[:] = [ha_tensor(t.data_ptr(), t.numel(), _ha._dtype_code(t), 0) for t in self.tensors]
+            self.sizes = [t.numel() for t in self.tensors]
         self.workspace_bytes = _ha._lib().hybrid_attn_grad_norm_workspace_bytes(len(self.tensors), self.c)
         self.native = _native(self.c, len(self.tensors), self.workspace_bytes, self.device)
 
@@ -77,6 +82,15 @@ class ParamList:
         if not len(grads) == len(m) == len(v) == len(io) == n:
             raise ValueError("masters, grads, m, v and param_io must be lists of one length")
         self.tensors = (masters, grads, m, v, io)
+        self.c = (ha_param * n)()
+        native = _ha._CALLS or _ha._calls()
+        if native and n and (device := native.describe_params(self.tensors, ctypes.addressof(self.c))) is not None:
+            self.device = torch.device("cuda", device)
+        else:
+            self._describe()
+        self.native = _native(self.c, n, 0, self.device)
+
+    def _describe(self):
         self.device = _one_device([t for x in self.tensors for t in x])
         for p, g, a, b, c in zip(*self.tensors):
             if any(t is not None and t.dtype != torch.float32 for t in (p, a, b)):
@@ -86,9 +100,8 @@ class ParamList:
 
         def at(t):
             return None if t is None else t.data_ptr()
-        self.c = (ha_param * n)(*[(at(p), at(g), at(a), at(b), at(c), p.numel(), _ha._dtype_code(g), _ha.HA_BF16 if c is None else _ha._dtype_code(c))
-                                  for p, g, a, b, c in zip(*self.tensors)])
-        self.native = _native(self.c, n, 0, self.device)
+        self.c[:] = [ha_param(at(p), at(g), at(a), at(b), at(c), p.numel(), _ha._dtype_code(g), _ha.HA_BF16 if c is None else _ha._dtype_code(c))
+                     for p, g, a, b, c in zip(*self.tensors)]
 
     def __len__(self):
         return len(self.tensors[0])

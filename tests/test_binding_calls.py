@@ -16,6 +16,8 @@ def test_is_built_and_leaves_host_tensors_alone():
     assert native.sparse_grad(t, t, t, i, t, t[..., 0], t, 128, 64, False, None, None, None, None, None, None, None, None) is None
     assert native.grad_norm([t], 1.0, None, None, None) is None and native.grad_clip([t], t, [t], None) is None
     assert native.update_many([t], 1e-3, 0, 1, 1.0, 0.9, 0.999, 1e-8, 0.01, None, None) is None
+    assert native.describe_tensors([t], 0) is None and native.describe_tensors((t,), 1) is None and native.describe_tensors([None], 1) is None
+    assert native.describe_params(([t], [t], [None], [None], [None]), 0) is None and native.describe_params(([t], [], [None], [None], [None]), 1) is None
     with pytest.raises(ValueError, match="another number"):
         native.bind_calls((1, 2), None)
 
@@ -43,7 +45,7 @@ def test_same_results_as_the_python_code(dtype, layout, causal, monkeypatch):
     n, s = torch.tensor([500, 300], dtype=torch.int32, device="cuda"), torch.tensor([200, 10], dtype=torch.int32, device="cuda")
     mask = dict(causal=causal, q_start=s, key_len=n)
     grads = [torch.randn(m, generator=gen).cuda() for m in (1000, 7)]
-    names = ("key_means", "select_blocks", "sparse_forward", "sparse_grad", "grad_norm", "grad_clip", "update_many")
+    names = ("key_means", "select_blocks", "sparse_forward", "sparse_grad", "grad_norm", "grad_clip", "update_many", "describe_tensors", "describe_params")
 
     def run(native):
         took = []
@@ -79,6 +81,33 @@ def test_same_results_as_the_python_code(dtype, layout, causal, monkeypatch):
     without, _ = run(False)
     for a, b in zip(with_native, without):
         assert torch.equal(a, b) and a.stride() == b.stride()
+
+
+@pytest.mark.gpu
+def test_lists_are_described_alike(monkeypatch):
+    def field(x, name):
+        return [getattr(e, name) for e in x.c]
+    f = [torch.zeros(n, device="cuda") for n in (5, 0, 300)]
+    half = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for n in (5, 0, 300)]
+    made = []
+    for native in (ha._calls(), False):
+        monkeypatch.setattr(ha, "_CALLS", native)
+        monkeypatch.setattr(ha, "_calls", lambda: native)
+        made.append((ha.TensorList(f + half), ha.ParamList(f, half, f, f, [half[0], None, f[2]]), ha.ParamList(f, f)))
+    from paper_2509_24899_amd import optim
+    for a, b in zip(*made):
+        struct = optim.ha_tensor if isinstance(a, ha.TensorList) else optim.ha_param
+        assert len(a) == len(b) and a.device == b.device and a.native[1:] == b.native[1:]
+        for name, _ in struct._fields_:
+            assert field(a, name) == field(b, name), name
+    assert made[0][0].sizes == made[1][0].sizes
+    monkeypatch.undo()
+    for wrong in ([f[2], half[2].cpu()], [f[2].view(30, 10).t()], [f[2].double()]):
+        with pytest.raises((RuntimeError, ValueError, TypeError)):
+            ha.TensorList(wrong)
+    for masters, grads, m in ((half, f, None), (f, f[::-1], None), (f, f, half), (f, f[:2], None)):
+        with pytest.raises(ValueError):
+            ha.ParamList(masters, grads, m, m)
 
 
 @pytest.mark.gpu
