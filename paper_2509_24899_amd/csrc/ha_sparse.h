@@ -108,6 +108,14 @@ static __device__ __forceinline__ void split8(f32x8 x, bf16x8 (&out)[NS]) {
       for (int i = 0; i < 8; ++i) x[i] -= static_cast<float>(out[n][i]);
   }
 }
+// Values that may be infinite: those have one piece (infinity less infinity is none).
+static __device__ __forceinline__ void split8_any(f32x4 lo, f32x4 hi, bf16x8 (&out)[3]) {
+  const f32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  split8<3>(x, out);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (!__builtin_isfinite(x[i])) out[1][i] = out[2][i] = static_cast<__bf16>(0.f);
+}
 // a b with both in pieces, small terms first; of three pieces the products that stay below the last bit are left out (six of nine are formed).
 template <int NS>
 static __device__ __forceinline__ f32x16 mfma_split(const bf16x8 (&a)[NS], const bf16x8 (&b)[NS], f32x16 c) {

@@ -18,8 +18,8 @@ namespace {
 
 struct FwdArgs {
   Sparse s;
-  View q, k, v, out;          // bf16 (fp32 tensors: the first pieces; the next stand piece_* elements behind)
-  int64_t piece_q, piece_k;
+  View q, k, v, out;          // as they are (fp32 tensors: k and v are the first bf16 pieces, the next stand piece_k elements behind)
+  int64_t piece_k;
   const int32_t *blocks;
   float *lse;
   int n_split;                // ranges of the list
@@ -196,13 +196,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
                        q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
-// fp32 tensors: 32 keys at a time in three pieces.  Two waves (tiles of 64 queries) take one stage of LDS and leave room for two more workgroups, whose
-// work covers the loads; two stages would leave the CU with these two waves.
+// fp32 tensors: 32 keys at a time in three pieces, six products for one.  One stage of LDS, so that other workgroups of the CU cover the loads: 32 heads of
+// 8192 tokens (d = 128, tiles of 128 x 16 blocks of 64) take 675 us (204 TFLOP/s, 1.2 PFLOP/s of the matrix cores) and 807 with two stages and one
+// workgroup to a CU; four heads, which leave a CU with one, 132 and 130.
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kernel(FwdArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void sparse_fwd_f32_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS), STAGES = NW == 2 ? 1 : 2;
-  __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * NS * STAGE];      // [stage][k | v][pieces][ROWS]
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS);
+  __shared__ __attribute__((aligned(1024))) char lds[2 * NS * STAGE];      // [k | v][pieces][ROWS]
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -219,25 +220,22 @@ __global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kerne
 
   const char *kbase = a.k.p + (b * a.k.sb + hk * a.k.sh) * 2, *vbase = a.v.p + (b * a.v.sb + hk * a.v.sh) * 2;
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
-  auto request = [&](int key, int stage) {
-    char *to = lds + stage * (2 * NS * STAGE);
+  auto request = [&](int key) {
     const int rows = min(limit - key, ROWS);
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      request_rows<D, ROWS, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.piece_k) * 2, rows, ksn), ksn, to + n * STAGE, w, lane);
-      request_rows<D, ROWS, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.piece_k) * 2, rows, vsn), vsn, to + (NS + n) * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(kbase + (key * a.k.sn + n * a.piece_k) * 2, rows, ksn), ksn, lds + n * STAGE, w, lane);
+      request_rows<D, ROWS, NW>(rows_rsrc<D>(vbase + (key * a.v.sn + n * a.piece_k) * 2, rows, vsn), vsn, lds + (NS + n) * STAGE, w, lane);
     }
   };
   int key = walk.next();
-  if (key >= 0) request(key, 0);
+  if (key >= 0) request(key);
 
   bf16x8 qf[KS][NS];
   {
-    const int64_t at = b * a.q.sb + h * a.q.sh + (int64_t)min(qi, s.Nq - 1) * a.q.sn + 8 * g;
+    const float *at = reinterpret_cast<const float *>(a.q.p) + b * a.q.sb + h * a.q.sh + (int64_t)min(qi, s.Nq - 1) * a.q.sn + 8 * g;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int n = 0; n < NS; ++n) qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (at + n * a.piece_q + 16 * ks) * 2);
+    for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(at + 16 * ks), *reinterpret_cast<const f32x4 *>(at + 16 * ks + 4), qf[ks]);
   }
   const float c = a.scale_log2e;
   float m = -INFINITY, l = 0.f;                       // this query's largest logit (lagging, see below), its sum of weights (this lane's keys)
@@ -247,12 +245,9 @@ __global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kerne
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
 
-  const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
-  for (int stage = 0; key >= 0; stage ^= STAGES - 1) {
-    const int next = walk.next();
+  const unsigned rows = T::rows_base(lds, lane), cols = T::cols_base(lds, lane);
+  while (key >= 0) {
     landed();
-    if (STAGES == 2 && next >= 0) request(next, stage ^ 1);
-    const unsigned rows = rows0 + stage * (2 * NS * STAGE), cols = cols0 + stage * (2 * NS * STAGE);
     f32x16 sc[ROWS / 32];
 #pragma unroll
     for (int i = 0; i < ROWS / 32; ++i) {
@@ -309,11 +304,9 @@ __global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kerne
           o[rb] = mfma_split<NS>(vf, pb, o[rb]);
         }
       }
-    if (STAGES == 1) {
-      __syncthreads();                                // every wave is done with the stage
-      if (next >= 0) request(next, 0);
-    }
-    key = next;
+    __syncthreads();                                  // every wave is done with the stage
+    key = walk.next();
+    if (key >= 0) request(key);
   }
   l = xhalf_sum(l);
   if (a.n_split > 1) {
@@ -332,7 +325,7 @@ __global__ __launch_bounds__(64 * NW, NW == 2 ? 2 : 1) void sparse_fwd_f32_kerne
     return;
   }
   if (a.lse && g == 0 && qi < s.Nq) a.lse[(int64_t)bh * s.Nq + qi] = l > 0.f ? m * a.scale + logf(l) : l == 0.f ? -INFINITY : l;
-  __syncthreads();                                    // the stages become the staging area of the stores
+  __syncthreads();                                    // the stage becomes the staging area of the stores
   store_rows<D, true>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, true>(), a.out.p + (b * a.out.sb + h * a.out.sh) * 4, a.out.sn * 4,
                          q0, min((t + 1) * s.qb, s.Nq), lane);
 }
@@ -513,7 +506,7 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(FwdArgs a) {
 struct FwdPlan {
   bool few;
   int n_split;
-  size_t off_q, off_k, off_v, off_po, off_pm, off_pl, total;
+  size_t off_k, off_v, off_po, off_pm, off_pl, total;
 };
 
 FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
@@ -532,7 +525,6 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
     return here;
   };
   if (p.dtype == HA_F32) {
-    f.off_q = take((size_t)6 * s.B * s.H * s.Nq * p.d_head);
     f.off_k = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
     f.off_v = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
   }
@@ -583,13 +575,10 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   const int d = p->d_head;
   const bool f32 = p->dtype == HA_F32;
   if (f32) {
-    const SplitJob jobs[3] = {{a.q, reinterpret_cast<__bf16 *>(ws + f.off_q), s.H, s.Nq}, {a.k, reinterpret_cast<__bf16 *>(ws + f.off_k), s.Hkv, s.Nk},
-                              {a.v, reinterpret_cast<__bf16 *>(ws + f.off_v), s.Hkv, s.Nk}};
-    if ((e = launch_split(s, d, jobs, 3, stream)) != hipSuccess) return device_error(e);
-    a.q = split_view(jobs[0], d);
-    a.k = split_view(jobs[1], d);
-    a.v = split_view(jobs[2], d);
-    a.piece_q = (int64_t)s.B * s.H * s.Nq * d;
+    const SplitJob jobs[2] = {{a.k, reinterpret_cast<__bf16 *>(ws + f.off_k), s.Hkv, s.Nk}, {a.v, reinterpret_cast<__bf16 *>(ws + f.off_v), s.Hkv, s.Nk}};
+    if ((e = launch_split(s, d, jobs, 2, stream)) != hipSuccess) return device_error(e);
+    a.k = split_view(jobs[0], d);
+    a.v = split_view(jobs[1], d);
     a.piece_k = (int64_t)s.B * s.Hkv * s.Nk * d;
   }
   a.blocks = blocks;

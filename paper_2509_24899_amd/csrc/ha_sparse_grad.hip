@@ -23,7 +23,7 @@ struct GradArgs {
   View q, k, v, dout, dq, dk, dv;      // inputs bf16 (fp32 tensors: the first pieces; the next stand piece_* elements behind)
   int64_t piece_q, piece_k;
   const int32_t *blocks;
-  const float *stat;                   // [B H][T qb / 32][2][32]: -lse / scale (-infinity for rows that take no part), -delta
+  float *stat;                         // [B H][T qb / 32][2][32]: -lse / scale (-infinity for rows that take no part), -delta
   int32_t *hist;                       // [B Hkv][n_chunks][Tk]
   int32_t *first, *item0, *slot0;      // [B Hkv][Tk + 1]: a block's first place in inv, its first item and its first slot
   int32_t *inv;                        // [B Hkv][T sel] tiles
@@ -205,7 +205,8 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 // dS is rounded to bf16 for the matrix cores, and delta stems from an output that was rounded, so a row's dS no longer add up to nothing, and what is left
 // over goes with the mean key: to be seen where few keys share a row (of rounding apart, dQ is 0.18 % off at 1024 keys, 0.19 at 512, 0.25 at 64 and 0.3 at 16;
-// rounding dQ itself adds 0.17 %).  Tiles of up to kFewKeys keys go along their list again and take sum(dS) P K away: 0.16 % off at all of these.
+// rounding dQ itself adds 0.17 %).  Tiles of up to kFewKeys keys go along their list again and take sum(dS) P K away: 0.16 % off at all of these.  They also
+// put delta right for dK.
 constexpr int kFewKeys = 512;
 
 template <int D, bool F32, int NW>
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
   typedef Tile<D> T;
   enum { ONLY, FIRST, SECOND };
   constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
-  constexpr int STAGES = F32 && NW == 2 ? 1 : 2;      // (as in the forward)
+  constexpr int STAGES = F32 && NW == 2 ? 1 : 2;      // (two waves: one stage, and more workgroups to a CU)
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * NS * STAGE];
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
       qf[ks][n] = *reinterpret_cast<const bf16x8 *>(a.q.p + (b * a.q.sb + h * a.q.sh + row * a.q.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
       df[ks][n] = *reinterpret_cast<const bf16x8 *>(a.dout.p + (b * a.dout.sb + h * a.dout.sh + row * a.dout.sn + n * a.piece_q + 16 * ks + 8 * g) * 2);
     }
-  const float *st = a.stat + ((int64_t)bh * s.T * s.qb + q0) * 2 + r;
+  float *st = a.stat + ((int64_t)bh * s.T * s.qb + q0) * 2 + r;
   const float c = a.scale_log2e, minus_lse2 = st[0] * c, minus_delta = st[32];
   f32x16 o[RB];
 #pragma unroll
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
-  float total = 0.f;                   // FIRST: of the rounded dS of this lane's keys
+  float total = 0.f, unrounded = 0.f;  // FIRST: of this lane's keys' dS, as the product takes them and before
   // One walk along the list: o += dS K, or (SECOND) o += (-total P) K.
   auto add = [&](auto pass) {
     constexpr int PASS = decltype(pass)::value;
@@ -297,7 +298,10 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
           split8<NS>(ds, db);
           if constexpr (PASS == FIRST) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x) total += static_cast<float>(db[0][x]);
+            for (int x = 0; x < 8; ++x) {
+            total += static_cast<float>(db[0][x]);
+            unrounded += ds[x];
+          }
           }
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
@@ -320,6 +324,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
   } else if (min(s.sel * s.kb, limit) <= kFewKeys) {
     add(std::integral_constant<int, FIRST>());
     total = xhalf_sum(total);
+    st[32] = minus_delta - xhalf_sum(unrounded);      // for dK (both lanes of a row write the same)
     __syncthreads();
     walk = ListWalk<ROWS>(list, 0, s.sel, s, limit, lane);
     key = walk.next();
@@ -524,7 +529,7 @@ template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) {
   typedef Tile<D> T;
   constexpr int KS = D / 16, RB = D / 32, NS = Pieces<true>::N, ROWS = Pieces<true>::ROWS, STAGE = T::bytes(ROWS), STAT = 2 * 32 * 4;
-  constexpr int STAGES = NW == 2 ? 1 : 2;             // (as in the forward)
+  constexpr int STAGES = NW == 2 ? 1 : 2;             // (as for dQ)
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * (2 * NS * STAGE + STAT)];      // [stage][q | dO][pieces][ROWS], lse2 | delta
   const Sparse &s = a.s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
@@ -600,14 +605,7 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
     for (int i = 0; i < ROWS / 32; ++i) {
       f32x16 sc, dp;
 #pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(stat + 8 * x4 + 4 * g), d4 = *reinterpret_cast<const f32x4 *>(stat + 32 + 8 * x4 + 4 * g);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          sc[4 * x4 + x] = l4[x];
-          dp[4 * x4 + x] = d4[x];
-        }
-      }
+      for (int x = 0; x < 16; ++x) sc[x] = dp[x] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 qf[NS], df[NS];
@@ -619,10 +617,16 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
         sc = mfma_split<NS>(qf, kf[ks], sc);
         dp = mfma_split<NS>(df, vf[ks], dp);
       }
+      // (the statistics come last: a sum that starts from -lse / scale rounds at its size, and P is 1.4e-6 off)
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        sc[x] = fast_exp2(sc[x] * c);
-        dp[x] *= sc[x];
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(stat + 8 * x4 + 4 * g), d4 = *reinterpret_cast<const f32x4 *>(stat + 32 + 8 * x4 + 4 * g);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float p = fast_exp2(__builtin_fmaf(sc[4 * x4 + x], c, l4[x] * c));
+          sc[4 * x4 + x] = p;
+          dp[4 * x4 + x] = p * (dp[4 * x4 + x] + d4[x]);
+        }
       }
       if (mask) {
 #pragma unroll
@@ -651,8 +655,9 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
             df[n] = T::cols_at(cols, rb, 32 * i + 16 * u, (NS + n) * STAGE);
             qf[n] = T::cols_at(cols, rb, 32 * i + 16 * u, n * STAGE);
           }
-          dv[rb] = mfma_split<NS>(df, pb, dv[rb]);
-          dk[rb] = mfma_split<NS>(qf, db, dk[rb]);
+          // (a sum of six products rounds at its own size, not at that of the sum over thousands of queries)
+          dv[rb] += mfma_split<NS>(df, pb, f32x16{});
+          dk[rb] += mfma_split<NS>(qf, db, f32x16{});
         }
       }
     }
@@ -718,6 +723,9 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   // parts of 64 tiles, shorter ones where the lists of all heads would not fill the chip twice
   const int64_t fill = (int64_t)s.B * s.Hkv * entries / 512;
   f.part_tiles = (int)(fill < 8 ? 8 : fill > kPart ? kPart : fill);
+  // fp32: a sum over R queries in 16s is 2.4e-8 sqrt(R / 32) off by its roundings; parts of up to 8192 queries hold that under 4e-7
+  const int rows = s.G * s.qb;
+  if (p.dtype == HA_F32 && f.part_tiles * rows > 8192) f.part_tiles = rows >= 8192 ? 1 : 8192 / rows;
   // ceil(n_j / part) parts of block j: over all blocks at most entries / part + Tk; those of blocks with several, of which there are
   // fewer than entries / part, at most 2 entries / part
   f.max_items = (int)(entries / f.part_tiles) + s.Tk;
