@@ -330,14 +330,72 @@ __global__ __launch_bounds__(64 * NW, 2) void sparse_fwd_f32_kernel(FwdArgs a) {
                          q0, min((t + 1) * s.qb, s.Nq), lane);
 }
 
+// The sums of four waves that walked keys of one group's range: joined through LDS (`image`: 4 x 32 D values) and stored.
+template <int D>
+static constexpr int image_bytes() { return 4 * 32 * D * 4; }
+template <int D, bool F32>
+__device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D / 32], float m, float l, char *lds, float (&stats)[2][4][32], int range, int b, int hk, int w, int lane) {
+  constexpr int RB = D / 32, IMAGE = RB * 4 * 64;
+  const Sparse &s = a.s;
+  const int r = lane & 31, g = lane >> 5, rows = s.G * s.Nq;
+  const float c = a.scale_log2e;
+  l = xhalf_sum(l);
+  __syncthreads();
+  f32x4 *image = reinterpret_cast<f32x4 *>(lds);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4)
+      image[w * IMAGE + (rb * 4 + x4) * 64 + lane] = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+  if (g == 0) {
+    stats[0][w][r] = m;
+    stats[1][w][r] = l;
+  }
+  __syncthreads();
+  if (w >= RB || r >= rows) return;
+  const int h = hk * s.G + r / s.Nq, n = r % s.Nq;
+  // wave w: columns 32 w .. of the joined rows
+  float top = stats[0][0][r], total = 0.f;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) top = fmaxf(top, stats[0][i][r]);
+  f32x4 y[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float mi = stats[0][i][r], f = mi == top ? 1.f : fast_exp2((mi - top) * c);
+    total += stats[1][i][r] * f;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) y[x4] += image[i * IMAGE + (w * 4 + x4) * 64 + lane] * f;
+  }
+  const int64_t row = ((int64_t)b * s.H + h) * s.Nq + n;
+  if (a.n_split > 1) {
+    const int64_t at = (int64_t)range * s.B * s.H * s.Nq + row;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) *reinterpret_cast<f32x4 *>(a.po + at * D + 32 * w + 8 * x4 + 4 * g) = y[x4];
+    if (w == 0 && g == 0) {
+      a.pm[at] = top;
+      a.pl[at] = total;
+    }
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int x4 = 0; x4 < 4; ++x4) {
+    char *to = a.out.p + (b * a.out.sb + h * a.out.sh + n * a.out.sn + 32 * w + 8 * x4 + 4 * g) * (F32 ? 4 : 2);
+    if constexpr (F32) *reinterpret_cast<f32x4 *>(to) = y[x4] * inv;
+    else *reinterpret_cast<bf16x4 *>(to) = __builtin_convertvector(y[x4] * inv, bf16x4);
+  }
+  if (a.lse && w == 0 && g == 0) a.lse[row] = total > 0.f ? top * a.scale + logf(total) : total == 0.f ? -INFINITY : total;
+}
+
 // Few queries (a decoding step): all queries of all heads of a key head, 32 at most, are the columns of one product, so that keys and values are read once
 // for the group.  What bounds it is memory, so every wave walks keys of its own, every fourth step of the range, with its own two stages in LDS and no
 // barrier; the four waves' sums are joined behind the list.
 template <int D>
 __global__ __launch_bounds__(256) void sparse_few_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, REQUESTS = 2 * T::chunks(32), IMAGE = RB * 4 * 64;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, REQUESTS = 2 * T::chunks(32);
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * SLOT];      // [wave][stage][k | v]; then [wave][register image]
+  static_assert(image_bytes<D>() <= 4 * 2 * SLOT, "the images fit the stages");
   __shared__ float stats[2][4][32];
   const Sparse &s = a.s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
@@ -413,49 +471,103 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(FwdArgs a) {
     }
     key = next;
   }
-  l = xhalf_sum(l);
-  __syncthreads();
-  f32x4 *image = reinterpret_cast<f32x4 *>(lds);
-  static_assert(4 * IMAGE * 16 <= 4 * 2 * SLOT, "the images fit the stages");
+  join_waves<D, false>(a, o, m, l, lds, stats, range, b, hk, w, lane);
+}
+
+// The same of fp32 tensors, whose chosen rows are split on the way: each wave takes them from memory to registers (a row of keys to a lane, eight rows of a
+// column of the values), so that a step reads the chosen rows once and not the whole cache.  Keys are requested a step ahead.
+template <int D>
+__global__ __launch_bounds__(256, 1) void sparse_few_f32_kernel(FwdArgs a) {
+  constexpr int KS = D / 16, RB = D / 32;
+  __shared__ __attribute__((aligned(1024))) char lds[image_bytes<D>()];
+  __shared__ float stats[2][4][32];
+  const Sparse &s = a.s;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / s.Hkv, hk = bh % s.Hkv;
+  const int held = s.held(b), start = s.start(b), rows = s.G * s.Nq, col = min(r, rows - 1), h = hk * s.G + col / s.Nq, n = col % s.Nq;
+  const int limit = s.causal ? min(held, start + s.Nq) : held, all_see = s.causal ? min(held, start + 1) : held, row_limit = s.causal ? min(held, start + n + 1) : held;
+  ListWalk<32> walk(a.blocks + (int64_t)bh * s.sel, (int)((int64_t)range * s.sel / a.n_split), (int)((int64_t)(range + 1) * s.sel / a.n_split), s, limit, lane);
+  const float *kbase = reinterpret_cast<const float *>(a.k.p) + b * a.k.sb + hk * a.k.sh + 8 * g, *vbase = reinterpret_cast<const float *>(a.v.p) + b * a.v.sb + hk * a.v.sh + r;
+  f32x4 kr[KS][2];
+  // (rows behind the last visible key are that key's: their weights are zero)
+  auto request = [&](int key) {
+    const float *p = kbase + min(key + r, limit - 1) * a.k.sn;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) kr[ks][i] = *reinterpret_cast<const f32x4 *>(p + 16 * ks + 4 * i);
+  };
+  int key = -1;
+  for (int i = 0; i <= w; ++i) key = walk.next();
+  if (key >= 0) request(key);
+  bf16x8 qf[KS][3];
+  const float *qp = reinterpret_cast<const float *>(a.q.p) + b * a.q.sb + h * a.q.sh + n * a.q.sn + 8 * g;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(qp + 16 * ks), *reinterpret_cast<const f32x4 *>(qp + 16 * ks + 4), qf[ks]);
+  const float c = a.scale_log2e;
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int x4 = 0; x4 < 4; ++x4)
-      image[w * IMAGE + (rb * 4 + x4) * 64 + lane] = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
-  if (g == 0) {
-    stats[0][w][r] = m;
-    stats[1][w][r] = l;
-  }
-  __syncthreads();
-  if (w >= RB || r >= rows) return;
-  // wave w: columns 32 w .. of the joined rows
-  float top = stats[0][0][r], total = 0.f;
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  while (key >= 0) {
+    float vr[2][RB][8];
 #pragma unroll
-  for (int i = 1; i < 4; ++i) top = fmaxf(top, stats[0][i][r]);
-  f32x4 y[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float mi = stats[0][i][r], f = mi == top ? 1.f : fast_exp2((mi - top) * c);
-    total += stats[1][i][r] * f;
+      for (int x = 0; x < 8; ++x) {
+        const float *p = vbase + min(key + crow(8 * u + x, g), limit - 1) * a.v.sn;
 #pragma unroll
-    for (int x4 = 0; x4 < 4; ++x4) y[x4] += image[i * IMAGE + (w * 4 + x4) * 64 + lane] * f;
-  }
-  const int64_t row = ((int64_t)b * s.H + h) * s.Nq + n;
-  if (a.n_split > 1) {
-    const int64_t at = (int64_t)range * s.B * s.H * s.Nq + row;
+        for (int rb = 0; rb < RB; ++rb) vr[u][rb][x] = p[32 * rb];
+      }
+    f32x16 sc;
 #pragma unroll
-    for (int x4 = 0; x4 < 4; ++x4) *reinterpret_cast<f32x4 *>(a.po + at * D + 32 * w + 8 * x4 + 4 * g) = y[x4];
-    if (w == 0 && g == 0) {
-      a.pm[at] = top;
-      a.pl[at] = total;
+    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 kf[3];
+      split8_any(kr[ks][0], kr[ks][1], kf);
+      sc = mfma_split<3>(kf, qf[ks], sc);
     }
-    return;
-  }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int at = key;
+    for (int i = 0; i < 4; ++i) key = walk.next();
+    if (key >= 0) request(key);
+    if (at + 32 > all_see) {
 #pragma unroll
-  for (int x4 = 0; x4 < 4; ++x4)
-    *reinterpret_cast<bf16x4 *>(a.out.p + (b * a.out.sb + h * a.out.sh + n * a.out.sn + 32 * w + 8 * x4 + 4 * g) * 2) = __builtin_convertvector(y[x4] * inv, bf16x4);
-  if (a.lse && w == 0 && g == 0) a.lse[row] = total > 0.f ? top * a.scale + logf(total) : total == 0.f ? -INFINITY : total;
+      for (int x = 0; x < 16; ++x) sc[x] = at + crow(x, g) < row_limit ? sc[x] : -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+    top = xhalf_max(top);
+    const float f = top == m ? 1.f : fast_exp2((m - top) * c), mc = top == -INFINITY ? 0.f : top * c;
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 p;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        p[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
+        l += p[x];
+      }
+      bf16x8 pb[3];
+      split8<3>(p, pb);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float(&v)[8] = vr[u][rb];
+        bf16x8 vf[3];
+        split8_any(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]}, vf);
+        o[rb] = mfma_split<3>(vf, pb, o[rb]);
+      }
+    }
+  }
+  join_waves<D, true>(a, o, m, l, lds, stats, range, b, hk, w, lane);
 }
 
 // Joins the ranges of a row, at most 64: a wave to a row.  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
@@ -512,7 +624,7 @@ struct FwdPlan {
 FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
   FwdPlan f{};
   // Workgroups: a tile of a head each, or all queries of a key head's group where they are few; the list is cut where that leaves CUs without one.
-  f.few = p.dtype == HA_BF16 && s.T == 1 && s.G * (int64_t)s.Nq <= 32;
+  f.few = s.T == 1 && s.G * (int64_t)s.Nq <= 32;
   const int64_t groups = (int64_t)s.B * (f.few ? s.Hkv : s.H * (int64_t)s.T), steps = (int64_t)s.sel * s.kb / 32;
   const int64_t most = f.few ? (steps + 3) / 4 : (steps + 15) / 16, want = groups > 0 ? 256 / groups : 1;      // (a step to a wave, or 16 to a workgroup)
   f.n_split = (int)(want < 1 || s.Nq == 0 ? 1 : want < most ? want : most);
@@ -524,7 +636,7 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
     at += round256(bytes);
     return here;
   };
-  if (p.dtype == HA_F32) {
+  if (p.dtype == HA_F32 && !f.few) {
     f.off_k = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
     f.off_v = take((size_t)6 * s.B * s.Hkv * s.Nk * p.d_head);
   }
@@ -574,7 +686,7 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   hipError_t e;
   const int d = p->d_head;
   const bool f32 = p->dtype == HA_F32;
-  if (f32) {
+  if (f32 && !f.few) {
     const SplitJob jobs[2] = {{a.k, reinterpret_cast<__bf16 *>(ws + f.off_k), s.Hkv, s.Nk}, {a.v, reinterpret_cast<__bf16 *>(ws + f.off_v), s.Hkv, s.Nk}};
     if ((e = launch_split(s, d, jobs, 2, stream)) != hipSuccess) return device_error(e);
     a.k = split_view(jobs[0], d);
@@ -593,8 +705,14 @@ extern "C" ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, cons
   a.share = xcd_share(a.items);
   if (f.few) {
     const unsigned n = (unsigned)s.B * s.Hkv * f.n_split;
-    if (d == 128) sparse_few_kernel<128><<<n, 256, 0, stream>>>(a);
-    else sparse_few_kernel<64><<<n, 256, 0, stream>>>(a);
+    if (f32) {
+      if (d == 128) sparse_few_f32_kernel<128><<<n, 256, 0, stream>>>(a);
+      else sparse_few_f32_kernel<64><<<n, 256, 0, stream>>>(a);
+    } else if (d == 128) {
+      sparse_few_kernel<128><<<n, 256, 0, stream>>>(a);
+    } else {
+      sparse_few_kernel<64><<<n, 256, 0, stream>>>(a);
+    }
     e = hipGetLastError();
   } else if (d == 128) {
     if (f32) e = s.qb == 128 ? launch_fwd<128, true, 4>(a, stream) : launch_fwd<128, true, 2>(a, stream);

@@ -12,6 +12,8 @@
 
 #include "ha_sparse.h"
 
+#include <algorithm>
+
 namespace ha {
 namespace {
 
@@ -720,12 +722,15 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   GradPlanS f{};
   const int64_t entries = (int64_t)s.T * s.sel;
   f.n_chunks = (s.T + kChunk - 1) / kChunk;
-  // parts of 64 tiles, shorter ones where the lists of all heads would not fill the chip twice
-  const int64_t fill = (int64_t)s.B * s.Hkv * entries / 512;
-  f.part_tiles = (int)(fill < 8 ? 8 : fill > kPart ? kPart : fill);
+  // Parts of 64 tiles, shorter ones where the lists of all heads would not fill the chip twice, but at least some queries to a part, whose sums pass through
+  // memory: 512 in bf16, 256 in fp32, where a query takes four times as long.  Passes (forward and gradients) with at least 8 tiles / 256 / 512 / 1024 queries
+  // to a part, us: [2, 12 : 4, 1819] bf16 138 / 102 / 102 / 106, [1, 16 : 2, 411] 141 / 84 / 83 / 90, [2, 3 : 1, 3724] causal 126 / 142 / 129 / 123;
+  // [2, 2 : 1, 4810] fp32 261 / 138 / 156 / 198, [2, 6 : 3, 305] 210 / 147 / 189 / 209.
+  const int64_t rows = (int64_t)s.G * s.qb, fill = (int64_t)s.B * s.Hkv * entries / 512;
+  int64_t part = std::max<int64_t>({fill, (p.dtype == HA_F32 ? 256 : 512) / rows, 1});
   // fp32: a sum over R queries in 16s is 2.4e-8 sqrt(R / 32) off by its roundings; parts of up to 8192 queries hold that under 4e-7
-  const int rows = s.G * s.qb;
-  if (p.dtype == HA_F32 && f.part_tiles * rows > 8192) f.part_tiles = rows >= 8192 ? 1 : 8192 / rows;
+  if (p.dtype == HA_F32) part = std::min<int64_t>(part, std::max<int64_t>(8192 / rows, 1));
+  f.part_tiles = (int)std::min<int64_t>(part, kPart);
   // ceil(n_j / part) parts of block j: over all blocks at most entries / part + Tk; those of blocks with several, of which there are
   // fewer than entries / part, at most 2 entries / part
   f.max_items = (int)(entries / f.part_tiles) + s.Tk;
