@@ -39,6 +39,20 @@ def test_norm_and_factor(sizes, max_norm):
     assert abs(factor - f) <= f * (2.0 ** -23 + 1e-12) and (f < 1 or factor == 1.0)
 
 
+@pytest.mark.parametrize("sizes", [[1], [1024 * 47, 1024], [1024 * 47 + 1, 1024], [1024 * 48, 1], [1] * 48, [1] * 49, [1000, 0, 1025, 5, 0, 7000, 33], [0] * 127 + [9], [0] * 128 + [9]])
+def test_norm_of_few_values(sizes):
+    """On both sides of the sizes that one workgroup takes, alone and with what an earlier call left in the workspace."""
+    g = grads_of(7, sizes)
+    ws = torch.full((ha.hybrid_attn_grad_norm_workspace_bytes(g) + 8,), 255, dtype=torch.uint8, device="cuda")
+    want = norm_of(g)
+    for workspace in (None, ws):
+        norm, factor = ha.hybrid_attn_grad_norm(g, want / 3, workspace=workspace).tolist()
+        assert abs(norm - want) <= want * (2.0 ** -24 + 1e-12) and abs(factor - 1 / 3) <= (2.0 ** -23 + 1e-12) / 3
+    first = next(x for x in g if x.numel())
+    first[-1] = math.nan
+    assert all(math.isnan(x) for x in ha.hybrid_attn_grad_norm(g, 1.0).tolist())
+
+
 def test_large_and_small_values():
     for x, n in ((3e38, 1000), (1e-38, 1000), (1e-45, 5)):
         g = [torch.full((n,), x, device="cuda")]
