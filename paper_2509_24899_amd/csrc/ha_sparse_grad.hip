@@ -18,7 +18,7 @@ namespace ha {
 namespace {
 
 constexpr int kPart = 64;        // tiles of an inverse list that one workgroup takes, at most
-constexpr int kChunk = 8;        // tiles counted together while the inverse lists are built
+constexpr int kChunk = 8;        // tiles counted together while the inverse lists are built (training at 480p 3.66 ms with 8 and 16, 3.69 with 4; 4096 causal tokens 180, 182 and 183 us)
 
 struct GradArgs {
   Sparse s;
@@ -38,6 +38,7 @@ struct GradArgs {
 };
 
 // ---- row statistics ----------------------------------------------------------------------------------------------------
+// Bound by memory: 41 us for out and its gradient at 12 heads of 32760 x 128, 4.9 TB/s.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void sparse_delta_kernel(Sparse s, View out, View dout, const float *lse, float inv_scale, float *stat) {
   constexpr int TPR = D / 8, RPB = 256 / TPR;
@@ -71,19 +72,27 @@ __global__ __launch_bounds__(256) void sparse_delta_kernel(Sparse s, View out, V
 }
 
 // ---- inverse lists -----------------------------------------------------------------------------------------------------
+// Four small launches, 25 us of 3.6 ms at 480p (256 tiles of 64 entries, 512 blocks, 12 heads), 12 us for the smallest problems.  (Counted in memory instead of
+// LDS, the first alone took 34.)
 // hist[chunk][j]: how many times the chunk's tiles list block j.
+constexpr int kCounted = 2048;   // blocks counted in LDS at a time
 __global__ __launch_bounds__(256) void inverse_count_kernel(GradArgs a) {
   const Sparse &s = a.s;
   const int chunk = blockIdx.x, bh = blockIdx.y;
   int32_t *h = a.hist + ((int64_t)bh * a.n_chunks + chunk) * s.Tk;
-  for (int j = threadIdx.x; j < s.Tk; j += 256) h[j] = 0;
-  __threadfence();
-  __syncthreads();
   const int lo = chunk * kChunk * s.sel, hi = min((chunk + 1) * kChunk, s.T) * s.sel;
   const int32_t *list = a.blocks + (int64_t)bh * s.T * s.sel;
-  for (int i = lo + threadIdx.x; i < hi; i += 256) {
-    const int j = list[i];
-    if ((unsigned)j < (unsigned)s.Tk) atomicAdd(h + j, 1);
+  __shared__ int n[kCounted];
+  for (int j0 = 0; j0 < s.Tk; j0 += kCounted) {
+    for (int j = threadIdx.x; j < kCounted; j += 256) n[j] = 0;
+    __syncthreads();
+    for (int i = lo + threadIdx.x; i < hi; i += 256) {
+      const int j = list[i];
+      if ((unsigned)j < (unsigned)s.Tk && (unsigned)(j - j0) < (unsigned)kCounted) atomicAdd(n + j - j0, 1);
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < min(kCounted, s.Tk - j0); j += 256) h[j0 + j] = n[j];
+    __syncthreads();
   }
 }
 
@@ -205,6 +214,8 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
+// The forward's walk with three products, S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  1.10 ms at 480p (1.1 PFLOP/s), matrix cores busy 64 % of the cycles.
+//
 // dS is rounded to bf16 for the matrix cores, and delta stems from an output that was rounded, so a row's dS no longer add up to nothing, and what is left
 // over goes with the mean key: to be seen where few keys share a row (of rounding apart, dQ is 0.18 % off at 1024 keys, 0.19 at 512, 0.25 at 64 and 0.3 at 16;
 // rounding dQ itself adds 0.17 %).  Tiles of up to kFewKeys keys go along their list again and take sum(dS) P K away: 0.16 % off at all of these.  They also
@@ -353,7 +364,8 @@ __device__ __forceinline__ void request_stat(const float *src, char *to, int lan
 
 // Four waves: the halves of the keys by two chunks at a time.  Two workgroups to a CU, so that one's loads, waits and exponentials run under the other's
 // products; that leaves 256 registers to a wave: 128 for dK and dV, 32 for S and dP, K and half of V; the other half of V lies in LDS.  S starts from
-// -lse / scale and dP from -delta, so that exp2(c S) is P and P dP is dS.
+// -lse / scale and dP from -delta, so that exp2(c S) is P and P dP is dS.  1.65 ms at 480p for four products (1.0 PFLOP/s), matrix cores busy 57 %.  It is
+// bound by how little of one workgroup's loads and vector work the other one covers, and by the L2 (items in another order miss it almost twice as often).
 template <int D>
 __global__ __launch_bounds__(256, 2) void sparse_dkv_kernel(GradArgs a) {
   typedef Tile<D> T;
@@ -526,7 +538,8 @@ __global__ __launch_bounds__(256, 2) void sparse_dkv_kernel(GradArgs a) {
   store_rows<D, false>(dv, 1.f, stage, a.dv.p + (b * a.dv.sb + hk * a.dv.sh) * 2, a.dv.sn * 2, k0, s.Nk, lane);
 }
 
-// fp32 tensors: the keys' and values' pieces in registers, 32 keys to a wave, and every wave reads all queries.
+// fp32 tensors: the keys' and values' pieces in registers, 32 keys to a wave, and every wave reads all queries.  All gradients of 32 heads of 8192 tokens
+// (d = 128, tiles of 128 x 16 blocks of 64) take 3.5 ms, 97 TFLOP/s, 0.6 PFLOP/s of the matrix cores: the pieces fill the registers of one wave to a SIMD.
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) {
   typedef Tile<D> T;
@@ -689,11 +702,12 @@ __global__ __launch_bounds__(64 * NW, 1) void sparse_dkv_f32_kernel(GradArgs a) 
 }
 
 // Joins the parts of the blocks that have several: D / 4 threads to a row of dk or dv, a workgroup to 256 / (D / 4) of a block's rows.
+// Bound by memory, 36 us at 480p.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void sparse_dkv_join_kernel(GradArgs a) {
   constexpr int TPR = D / 4, RPB = 256 / TPR;
   const Sparse &s = a.s;
-  const int pieces = 2 * s.kb / RPB, row = blockIdx.x % pieces * RPB + threadIdx.x / TPR, at = blockIdx.x / pieces;
+  const int row = blockIdx.y * RPB + threadIdx.x / TPR, at = blockIdx.x;
   const int j = at % s.Tk, bh = at / s.Tk, b = bh / s.Hkv, hk = bh % s.Hkv;
   const int64_t at_j = (int64_t)bh * (s.Tk + 1) + j;
   const int parts = a.item0[at_j + 1] - a.item0[at_j];
@@ -758,7 +772,7 @@ GradPlanS plan_grad(const ha_sparse_problem &p, const Sparse &s) {
   f.off_n_work = take(4);
   f.off_part = take(hk * f.max_slots * 2 * s.kb * p.d_head * 4);
   f.total = at;
-  if ((int64_t)hk * f.max_items > (1 << 30)) f.total = 0;      // (more workgroups than a launch is given)
+  if ((int64_t)hk * f.max_items > (1 << 22)) f.total = 0;      // (twice 256 threads to an item: more than a launch takes)
   return f;
 }
 
@@ -780,7 +794,7 @@ hipError_t launch_grad(const ha_sparse_problem &p, GradArgs &a, hipStream_t st) 
     else sparse_dkv_f32_kernel<D, 2><<<items, 128, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.max_slots > 0) {
-      sparse_dkv_join_kernel<D, F32><<<(unsigned)((int64_t)s.B * s.Hkv * s.Tk) * (2 * s.kb / (1024 / D)), 256, 0, st>>>(a);
+      sparse_dkv_join_kernel<D, F32><<<dim3((unsigned)((int64_t)s.B * s.Hkv * s.Tk), 2 * s.kb / (1024 / D)), 256, 0, st>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }

@@ -4,7 +4,8 @@
 //
 // Everything that decides is formed in double: the sums of 64 or 128 bf16 values are exact there, and two scores that differ at all are in the
 // right order, whatever the order of summation (in fp32 about one list in ten thousand changed with it).  The sums over q and k are bound by
-// memory; the scores of 128 queries against a block of 64 keys take one product of d values.
+// memory (12 heads of 32760 x 128 bf16, 100 MB: 20 us for keys and 20 for queries, 5 TB/s); the scores of 128 queries against a block of 64 keys take one
+// product of d values.
 #include <climits>
 #include <cmath>
 
@@ -17,14 +18,14 @@ ha_status check_sparse(const ha_sparse_problem *p) {
   if (p->B <= 0 || p->H <= 0 || p->H_kv <= 0 || p->N_q < 0 || p->N_k < 0 || p->d_head <= 0) return HA_ERR_SHAPE;
   if (p->H % p->H_kv || p->n_select < 1 || p->keep_first < 0 || p->near_tokens < -1) return HA_ERR_SHAPE;
   if (p->causal != 0 && p->causal != 1) return HA_ERR_SHAPE;
-  if (!(p->softmax_scale > 0.f) || !std::isfinite(p->softmax_scale)) return HA_ERR_SHAPE;
+  if (!(p->softmax_scale >= 1e-30f && p->softmax_scale <= 1e30f)) return HA_ERR_SHAPE;      // (its reciprocal, and logits times it, are finite)
   if (p->dtype != HA_BF16 && p->dtype != HA_F32) return HA_ERR_UNSUPPORTED;
   if (p->d_head != 64 && p->d_head != 128) return HA_ERR_UNSUPPORTED;
   if ((p->q_block != 64 && p->q_block != 128) || (p->k_block != 64 && p->k_block != 128)) return HA_ERR_UNSUPPORTED;
   if ((int64_t)p->B * p->H > 65535 || p->N_q > (1 << 24) || p->N_k > (1 << 29) || p->n_select > (1 << 20) || p->near_tokens > (1 << 29)) return HA_ERR_UNSUPPORTED;
-  const int64_t T = (p->N_q + p->q_block - 1) / p->q_block, Tk = (p->N_k + p->k_block - 1) / p->k_block, BH = (int64_t)p->B * p->H;
-  // (a launch takes 2^31 - 1 workgroups, and an index into one head's lists 31 bits)
-  if (BH * T > (1 << 24) || BH * Tk > (1 << 25) || T * p->n_select > (1 << 30)) return HA_ERR_UNSUPPORTED;
+  const int64_t T = (p->N_q + p->q_block - 1) / p->q_block, Tk = (p->N_k + p->k_block - 1) / p->k_block, B = p->B;
+  // (a launch takes 2^32 - 1 threads, 256 to a tile, a key block or 16 rows, and an index into one head's lists 31 bits)
+  if (B * p->H * T > (1 << 20) || B * p->H_kv * Tk > (1 << 23) || T * p->n_select > (1 << 30)) return HA_ERR_UNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(p->q_start) & 3u || reinterpret_cast<uintptr_t>(p->key_len) & 3u) return HA_ERR_ALIGN;
   return HA_OK;
 }
@@ -148,6 +149,8 @@ __device__ __forceinline__ uint64_t rank_key(const ScoreArgs &a, int held, int s
 // (columns) at columns 16 i + 4 (l / 16) + u of every 16, the contraction's k of product (i, u); register v of the result is tile 4 v + l / 16,
 // block l % 16.  (As vector products the sums came from LDS for every block, and that bound it: 22 us for 15 at 256 tiles by 512 blocks of 12 heads.)
 constexpr int kTiles = 16;
+constexpr int kFusedBlocks = 1024;     // keys of kTiles tiles that fit LDS
+constexpr int kRowBlocks = 256;        // keys of a tile that one wave holds in four registers: one launch (4 x 256: 7.4 us for 11.5 in two, 256 x 256: 8.1 for 17.9)
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 template <int D>
 __device__ __forceinline__ void load_sums(const ScoreArgs &a, int bh, int t0, int lane, f64x4 (&q)[D / 16]) {
@@ -282,7 +285,8 @@ __device__ __forceinline__ void choose_wave(const uint64_t *keys, int sel, int32
   for (int i = at + lane; i < sel; i += 64) out[i] = -1;
 }
 
-// Many tiles: a workgroup scores kTiles of them against all blocks (at most 64 V), then every wave makes one tile's choice.
+// Many tiles: a workgroup scores kTiles of them against all blocks (at most 64 V), then every wave makes one tile's choice.  26 us at 256 tiles x 512 blocks
+// of 12 heads (480p), 15 of them the scores; 192 workgroups of 16 waves, whose chain of loads, products, barrier and search is what it takes.
 template <int D, int V>
 __global__ __launch_bounds__(1024) void score_and_choose_kernel(ScoreArgs a) {
   const Sparse &s = a.s;
@@ -373,11 +377,11 @@ __device__ __forceinline__ void keys_of_tile(const ScoreArgs &a, int row, int lo
 template <int D, bool F32>
 __global__ __launch_bounds__(512) void choose_row_kernel(ScoreArgs a) {
   __shared__ double part[8][D];
-  __shared__ uint64_t keys[256];
-  if (threadIdx.x < 256 && (int)threadIdx.x >= a.s.Tk) keys[threadIdx.x] = 0;
+  __shared__ uint64_t keys[kRowBlocks];
+  if (threadIdx.x < kRowBlocks && (int)threadIdx.x >= a.s.Tk) keys[threadIdx.x] = 0;
   keys_of_tile<D, F32, 8>(a, blockIdx.x, 0, a.s.Tk, part, keys);
   __syncthreads();
-  if (threadIdx.x < 64) choose_wave<4>(keys, a.s.sel, a.blocks + (int64_t)blockIdx.x * a.s.sel, threadIdx.x);
+  if (threadIdx.x < 64) choose_wave<kRowBlocks / 64>(keys, a.s.sel, a.blocks + (int64_t)blockIdx.x * a.s.sel, threadIdx.x);
 }
 
 // More: the means are many, so that a workgroup takes 128 of them, and a second launch makes the choice.
@@ -386,12 +390,13 @@ __global__ __launch_bounds__(1024) void keys_kernel(ScoreArgs a) {
   __shared__ double part[16][D];
   keys_of_tile<D, F32, 16>(a, blockIdx.y, blockIdx.x * 128, min(a.s.Tk, (int)(blockIdx.x + 1) * 128), part, a.keys + (int64_t)blockIdx.y * a.s.Tk);
 }
-__global__ __launch_bounds__(64) void choose_1k_kernel(const uint64_t *keys, int Tk, int sel, int32_t *blocks) {
-  __shared__ uint64_t k[1024];
+template <int V>
+__global__ __launch_bounds__(64) void choose_list_kernel(const uint64_t *keys, int Tk, int sel, int32_t *blocks) {
+  __shared__ uint64_t k[64 * V];
   const int64_t row = blockIdx.x;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) k[64 * i + threadIdx.x] = 64 * i + (int)threadIdx.x < Tk ? keys[row * Tk + 64 * i + threadIdx.x] : 0;
-  choose_wave<16>(k, sel, blocks + row * sel, threadIdx.x);      // (every lane reads what it wrote)
+  for (int i = 0; i < V; ++i) k[64 * i + threadIdx.x] = 64 * i + (int)threadIdx.x < Tk ? keys[row * Tk + 64 * i + threadIdx.x] : 0;
+  choose_wave<V>(k, sel, blocks + row * sel, threadIdx.x);       // (every lane reads what it wrote)
 }
 
 // Very many blocks: 256 threads to a list, keys read from memory for every bit.
@@ -459,32 +464,44 @@ __global__ __launch_bounds__(256) void choose_kernel(const uint64_t *all_keys, i
 }
 
 // ---- fp32 tensors as three bf16 images -----------------------------------------------------------------------------------
-// One pass at the rate of memory: 4 bytes of a value read, 6 written.
+// One pass at the rate of memory: 4 bytes of a value read, 6 written (30 M values 49 us, 6.3 TB/s).
 struct SplitJobs {
   SplitJob job[4];
-  unsigned end[4];                      // of the workgroups up to this job's
+  unsigned end[4];                      // how many groups of rows up to this job's
 };
 template <int D>
 __global__ __launch_bounds__(256) void split_kernel(Sparse s, SplitJobs jobs) {
   constexpr int TPR = D / 8, RPB = 256 / TPR;
   int at = 0;
-  while (blockIdx.x >= jobs.end[at]) ++at;
-  const SplitJob &j = jobs.job[at];
-  const int64_t row = (int64_t)(blockIdx.x - (at ? jobs.end[at - 1] : 0)) * RPB + threadIdx.x / TPR, rows = (int64_t)s.B * j.heads * j.n;
-  if (row >= rows) return;
-  const int c = 8 * (threadIdx.x % TPR), n = (int)(row % j.n), h = (int)(row / j.n % j.heads), b = (int)(row / j.n / j.heads);
-  const f32x4 *p = reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(j.in.p) + b * j.in.sb + h * j.in.sh + n * j.in.sn + c);
-  bf16x8 out[3];
-  split8_any(p[0], p[1], out);
+  for (unsigned i = blockIdx.x; i < jobs.end[3]; i += gridDim.x) {
+    while (i >= jobs.end[at]) ++at;
+    const SplitJob &j = jobs.job[at];
+    const int64_t row = (int64_t)(i - (at ? jobs.end[at - 1] : 0)) * RPB + threadIdx.x / TPR, rows = (int64_t)s.B * j.heads * j.n;
+    if (row >= rows) continue;
+    const int c = 8 * (threadIdx.x % TPR), n = (int)(row % j.n), h = (int)(row / j.n % j.heads), b = (int)(row / j.n / j.heads);
+    const f32x4 *p = reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(j.in.p) + b * j.in.sb + h * j.in.sh + n * j.in.sn + c);
+    bf16x8 out[3];
+    split8_any(p[0], p[1], out);
 #pragma unroll
-  for (int p3 = 0; p3 < 3; ++p3) *reinterpret_cast<bf16x8 *>(j.out + (p3 * rows + row) * D + c) = out[p3];
+    for (int p3 = 0; p3 < 3; ++p3) *reinterpret_cast<bf16x8 *>(j.out + (p3 * rows + row) * D + c) = out[p3];
+  }
 }
 
 size_t sums_bytes(const Sparse &s, int d) { return round256((size_t)s.B * s.Hkv * s.T * d * 8); }
 
-constexpr int kFusedBlocks = 1024;     // keys of kTiles tiles that fit LDS
-// Few tiles make their choice from the queries on, a workgroup or several each; many share passes over the means.
-bool few_tiles(const Sparse &s) { return (int64_t)s.B * s.Hkv * s.T <= 256; }
+// Few tiles make their choice from the queries on, a workgroup or several each; many share passes over the means.  Us at d = 128, sixteen of the blocks:
+//   tiles x blocks      4 x 16  512 x 16  256 x 256  1024 x 256  4096 x 240  |  4 x 500  128 x 500  256 x 500  512 x 500  256 x 940
+//   on their own           4.5       6.1        8.1        17.6        55.3  |     11.0       17.2       26.5       43.1       42.0
+//   sums and scores        7.2       9.0       21.4        25.2        38.9  |     19.1       27.8       27.6       28.1       38.8
+bool few_tiles(const Sparse &s) { return (int64_t)s.B * s.Hkv * s.T <= (s.Tk <= kRowBlocks ? 1024 : 128); }
+
+// The choice from keys in memory: a wave that holds them where they are up to 2048.
+void launch_choose(const Sparse &s, const uint64_t *keys, int32_t *blocks, hipStream_t st) {
+  const unsigned rows = (unsigned)s.B * s.Hkv * s.T;
+  if (s.Tk <= 1024) choose_list_kernel<16><<<rows, 64, 0, st>>>(keys, s.Tk, s.sel, blocks);
+  else if (s.Tk <= 2048) choose_list_kernel<32><<<rows, 64, 0, st>>>(keys, s.Tk, s.sel, blocks);
+  else choose_kernel<<<rows, 256, 0, st>>>(keys, s.Tk, s.sel, blocks);
+}
 
 // Blocks that are always kept, at most.
 int64_t forced_blocks(const ha_sparse_problem &p) {
@@ -510,6 +527,7 @@ hipError_t launch_split(const Sparse &s, int d, const SplitJob *jobs, int n_jobs
     all.end[i] = blocks;
   }
   if (blocks == 0) return hipSuccess;
+  if (blocks > 1 << 23) blocks = 1 << 23;
   if (d == 128) split_kernel<128><<<blocks, 256, 0, st>>>(s, all);
   else split_kernel<64><<<blocks, 256, 0, st>>>(s, all);
   return hipGetLastError();
@@ -545,7 +563,7 @@ extern "C" ha_status hybrid_attn_key_means(const ha_sparse_problem *p, const ha_
 extern "C" size_t hybrid_attn_select_workspace_bytes(const ha_sparse_problem *p) {
   if (check_sparse(p) != HA_OK) return 0;
   const Sparse s = sparse_of(*p);
-  if (few_tiles(s) && s.Tk <= 256) return 0;
+  if (few_tiles(s) && s.Tk <= kRowBlocks) return 0;
   return sums_bytes(s, p->d_head) + (!few_tiles(s) && s.Tk <= kFusedBlocks ? 0 : round256((size_t)s.B * s.Hkv * s.T * s.Tk * 8));
 }
 
@@ -573,13 +591,12 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
 #define HA_ROW(K, ...) do { \
     if (p->d_head == 128) { if (p->dtype == HA_F32) K<128, true>__VA_ARGS__(a); else K<128, false>__VA_ARGS__(a); } \
     else { if (p->dtype == HA_F32) K<64, true>__VA_ARGS__(a); else K<64, false>__VA_ARGS__(a); } } while (0)
-    if (s.Tk <= 256) {
+    if (s.Tk <= kRowBlocks) {
       HA_ROW(choose_row_kernel, <<<rows, 512, 0, stream>>>);
     } else {
       HA_ROW(keys_kernel, <<<dim3((s.Tk + 127) / 128, rows), 1024, 0, stream>>>);
       if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
-      if (s.Tk <= 1024) choose_1k_kernel<<<rows, 64, 0, stream>>>(keys, s.Tk, s.sel, blocks);
-      else choose_kernel<<<rows, 256, 0, stream>>>(keys, s.Tk, s.sel, blocks);
+      launch_choose(s, keys, blocks, stream);
     }
 #undef HA_ROW
     e = hipGetLastError();
@@ -594,6 +611,7 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
   if (s.Tk <= kFusedBlocks) {
 #define HA_FUSED(V) (p->d_head == 128 ? score_and_choose_kernel<128, V><<<dim3(groups, heads), 1024, 0, stream>>>(a) \
                                       : score_and_choose_kernel<64, V><<<dim3(groups, heads), 1024, 0, stream>>>(a))
+    // (a list's keys in as few registers as hold them; us at 4096 tiles with 4 / 8 / 10 registers and with 16: 240 blocks 38.9 / 47.7, 500 47.1 / 52.7, 590 48.8 / 52.2)
     if (s.Tk <= 256) HA_FUSED(4);
     else if (s.Tk <= 512) HA_FUSED(8);
     else if (s.Tk <= 640) HA_FUSED(10);
@@ -604,7 +622,7 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
     if (p->d_head == 128) scores_kernel<128><<<grid, 512, 0, stream>>>(a);
     else scores_kernel<64><<<grid, 512, 0, stream>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
-    choose_kernel<<<rows, 256, 0, stream>>>(keys, s.Tk, s.sel, blocks);
+    launch_choose(s, keys, blocks, stream);
   }
   e = hipGetLastError();
   return e == hipSuccess ? HA_OK : device_error(e);

@@ -154,6 +154,17 @@ def test_long_lists(dtype):
     check(problem(14, H=1, Hkv=1, Nq=70, Nk=9000, dtype=dtype, d=64, qb=64, kb=64, sel=140))
 
 
+def test_gradients_over_more_blocks_than_are_counted_at_once():
+    check(problem(51, H=1, Hkv=1, Nq=700, Nk=64 * 4100 + 5, d=64, qb=64, kb=64, sel=6))
+
+
+def test_lists_around_the_length_that_is_walked_twice():
+    """448, 512 and 576 keys to a row, in tiles of one launch (causal) and of one length."""
+    check(problem(52, H=2, Hkv=1, Nq=900, d=64, qb=64, kb=64, sel=16, causal=True))
+    for sel in (7, 8, 9):
+        check(problem(53 + sel, H=1, Hkv=1, Nq=130, Nk=1000, qb=128, kb=64, sel=sel))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,Nq", [(1, 1), (3, 1), (8, 4), (32, 1), (5, 6), (1, 32), (33, 1), (11, 3)])
@@ -309,7 +320,8 @@ def test_choice_of_many_blocks_for_one_query(Nk, sel):
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("N,Nk,H,sel,kb", [(64 * 300, 64 * 200, 1, 5, 64), (64 * 130, 64 * 600, 2, 16, 64), (64 * 100, 64 * 1000, 3, 9, 64), (64 * 260, 128 * 1100, 1, 64, 128)])
+@pytest.mark.parametrize("N,Nk,H,sel,kb", [(64 * 300, 64 * 200, 1, 5, 64), (64 * 130, 64 * 600, 2, 16, 64), (64 * 100, 64 * 1000, 3, 9, 64), (64 * 260, 128 * 1100, 1, 64, 128), (64 * 1030, 64 * 256, 1, 7, 64),
+                                           (64 * 1025, 64 * 257, 1, 20, 64), (64 * 140, 64 * 2100, 1, 40, 64)])
 def test_choice_of_many_tiles(N, Nk, H, sel, kb):
     gen = torch.Generator().manual_seed(36)
     q, k = tokens(gen, 1, H, N - 7, 64, BF16), tokens(gen, 1, H, Nk - 1, 64, BF16)
