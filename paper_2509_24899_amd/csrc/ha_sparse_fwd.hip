@@ -34,11 +34,19 @@ struct FwdArgs {
 // exponentials of its own, then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work
 // of one wave at the same time, and of two with two workgroups to a CU.  12 heads of 32760 tokens, 64 blocks of 64: 0.81 ms, 1.0 PFLOP/s, matrix cores busy
 // 54 % of the cycles at 1.73 GHz; what bounds it is power and, behind that, the L2 (lists that all name the same blocks take 0.77 ms).
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(FwdArgs a) {
+//
+// Tiles of 64 queries are two waves, and four steps in LDS would leave a CU with four of them at d = 128.  So they hold two steps' keys and three steps' values,
+// asked for two steps ahead: 32 heads of 8192 tokens, 16 blocks of 64, 183 us for 231 (d = 64: 101 for 116); with a workgroup or two to a CU there is nothing to
+// win at d = 128, and four steps it is (DEEP; four heads: 30 us for 35, at d = 64 28 for 27).
+template <int D, int NW, bool DEEP>
+__global__ __launch_bounds__(64 * NW, !DEEP && D == 64 ? 3 : DEEP && NW == 2 ? 1 : 2) void sparse_fwd_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, SLOTS = 4;
-  __shared__ __attribute__((aligned(1024))) char lds[SLOTS * SLOT];      // [step][k | v]
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32);
+  constexpr int AHEAD = DEEP ? 3 : 2, KSLOTS = DEEP ? 4 : 2, VSLOTS = DEEP ? 4 : 3;      // (a step's keys go ahead of its values)
+  // a step's place
+  constexpr auto k_at = [](int step) { return DEEP ? step % KSLOTS * 2 * TILE : step % KSLOTS * TILE; };
+  constexpr auto v_at = [](int step) { return DEEP ? step % VSLOTS * 2 * TILE + TILE : (KSLOTS + step % VSLOTS) * TILE; };
+  __shared__ __attribute__((aligned(1024))) char lds[(KSLOTS + VSLOTS) * TILE];      // keys of KSLOTS steps, values of VSLOTS
   const unsigned item = xcd_item(blockIdx.x, a.share);
   if (item >= a.items) return;
   const Sparse &s = a.s;
@@ -57,13 +65,13 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
   constexpr int REQUESTS = 2 * T::chunks(32) / NW;
   // (behind the list's last key zeros are requested: every step has as many requests, which is what the waits count)
-  auto request = [&](int key, int slot) {
-    char *to = lds + slot * SLOT;
+  auto request = [&](int key, int step) {
+    char *to = lds + k_at(step);
     const int rows = key < 0 ? 0 : min(limit - key, 32), at = max(key, 0);
     request_rows<D, 32, NW>(rows_rsrc<D>(kbase + (int64_t)at * ksn, rows, ksn), ksn, to, w, lane);
-    request_rows<D, 32, NW>(rows_rsrc<D>(vbase + (int64_t)at * vsn, rows, vsn), vsn, to + TILE, w, lane);
+    request_rows<D, 32, NW>(rows_rsrc<D>(vbase + (int64_t)at * vsn, rows, vsn), vsn, to + (v_at(step) - k_at(step)), w, lane);
   };
-  int key0 = walk.next(), key1 = walk.next(), key2 = walk.next();
+  int key0 = walk.next(), key1 = walk.next(), key2 = DEEP ? walk.next() : -1;
   const float c = a.scale_log2e;
   float m = -INFINITY, top = -INFINITY, l = 0.f;      // what the sums are expressed against, the largest logit and the sum of weights (this lane's keys)
   f32x16 o[RB];
@@ -74,7 +82,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
   if (key0 >= 0) {
     request(key0, 0);
     request(key1, 1);
-    request(key2, 2);
+    if constexpr (DEEP) request(key2, 2);
     bf16x8 qf[KS];
     const char *qp = a.q.p + (b * a.q.sb + h * a.q.sh + (int64_t)min(qi, s.Nq - 1) * a.q.sn + 8 * g) * 2;
 #pragma unroll
@@ -87,8 +95,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int i = 0; i < 2; ++i) cols[rb][i] = T::cols_base(lds, lane) ^ (rb << 6) ^ (i << 5);
-    auto read_k = [&](int slot, int ks) { return T::row_piece(rows[ks] + slot * SLOT); };
-    auto read_v = [&](int slot, int rb, int u) { return T::col_piece(cols[rb][0] + slot * SLOT + TILE + 16 * u * T::PITCH, cols[rb][1] + slot * SLOT + TILE + (16 * u + 8) * T::PITCH); };
+    auto read_k = [&](int step, int ks) { return T::row_piece(rows[ks] + k_at(step)); };
+    auto read_v = [&](int step, int rb, int u) {
+      const int at = v_at(step) + 16 * u * T::PITCH;
+      return T::col_piece(cols[rb][0] + at, cols[rb][1] + at + 8 * T::PITCH);
+    };
     const float gap = 8.f / c;
     float mc = 0.f;
     // logits of keys that this wave's queries do not all see (a key of -1: of none), then the running maximum.  What has been summed follows it when
@@ -116,27 +127,27 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
     };
     const f32x16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     f32x16 s_a, s_b;
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * REQUESTS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * REQUESTS) : "memory");
     __syncthreads();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s_a = mfma32(read_k(0, ks), qf[ks], ks == 0 ? none : s_a);
     mask(s_a, key0);
     follow(s_a);
-    auto step = [&](f32x16 &sc, f32x16 &sn, auto slot_c) {
-      constexpr int slot = decltype(slot_c)::value, next = (slot + 1) & (SLOTS - 1);
+    auto step = [&](f32x16 &sc, f32x16 &sn, auto now_c) {
+      constexpr int now = decltype(now_c)::value, next = now + 1;
       // the next keys have landed, and no wave reads those of the step before any more
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * REQUESTS) : "memory");
       __syncthreads();
       bf16x8 kf[KS], vf[2 * RB], pb[2];
       kf[0] = read_k(next, 0);
       kf[1] = read_k(next, 1);
-      const int key3 = walk.next();
-      request(key3, (slot + 3) & (SLOTS - 1));
+      const int further = walk.next();
+      request(further, now + AHEAD);
       constexpr int PER = 16 / KS;         // logits to a product: 2 at d = 128, 4 at d = 64
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (ks + 2 < KS) kf[ks + 2] = read_k(next, ks + 2);
-        else vf[ks + 2 - KS] = read_v(slot, ks + 2 - KS, 0);
+        else vf[ks + 2 - KS] = read_v(now, ks + 2 - KS, 0);
         HA_FENCE();
         sn = mfma32(kf[ks], qf[ks], ks == 0 ? none : sn);
 #pragma unroll
@@ -155,15 +166,15 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
       }
 #pragma unroll
       for (int n = 0; n < 2 * RB; ++n) {   // n = RB u + rb
-        if (n + 2 < 2 * RB) vf[n + 2] = read_v(slot, (n + 2) % RB, (n + 2) / RB);
+        if (n + 2 < 2 * RB) vf[n + 2] = read_v(now, (n + 2) % RB, (n + 2) / RB);
         HA_FENCE();
         o[n % RB] = mfma32(vf[n], pb[n / RB], o[n % RB]);
       }
       mask(sn, key1);
       follow(sn);
       key0 = key1;
-      key1 = key2;
-      key2 = key3;
+      key1 = DEEP ? key2 : further;
+      key2 = further;
     };
     while (true) {
       step(s_a, s_b, std::integral_constant<int, 0>{});
@@ -174,6 +185,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_fwd_kernel(Fw
       if (key0 < 0) break;
       step(s_b, s_a, std::integral_constant<int, 3>{});
       if (key0 < 0) break;
+      if constexpr (!DEEP) {
+        step(s_a, s_b, std::integral_constant<int, 4>{});
+        if (key0 < 0) break;
+        step(s_b, s_a, std::integral_constant<int, 5>{});
+        if (key0 < 0) break;
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
@@ -669,7 +686,8 @@ FwdPlan plan_forward(const ha_sparse_problem &p, const Sparse &s) {
 template <int D, bool F32, int NW>
 hipError_t launch_fwd(const FwdArgs &a, hipStream_t st) {
   if constexpr (F32) sparse_fwd_f32_kernel<D, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
-  else sparse_fwd_kernel<D, NW><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  else if (NW == 4 || (D == 128 && a.items <= 512)) sparse_fwd_kernel<D, NW, NW == 4 || D == 128><<<8 * a.share, 64 * NW, 0, st>>>(a);
+  else sparse_fwd_kernel<D, NW, NW == 4><<<8 * a.share, 64 * NW, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -215,6 +215,8 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 // The forward's walk with three products, S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  1.10 ms at 480p (1.1 PFLOP/s), matrix cores busy 64 % of the cycles.
+// Tiles of 64 queries are two waves, which go 32 keys at a time where a CU has more than two of them: all gradients of 32 heads of 8192 tokens, 16 blocks of 64,
+// 631 us for 657 with 64 keys at a time (d = 64: 332 for 343), of four heads 131 for 122 (90 for 87).
 //
 // dS is rounded to bf16 for the matrix cores, and delta stems from an output that was rounded, so a row's dS no longer add up to nothing, and what is left
 // over goes with the mean key: to be seen where few keys share a row (of rounding apart, dQ is 0.18 % off at 1024 keys, 0.19 at 512, 0.25 at 64 and 0.3 at 16;
@@ -222,11 +224,11 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 // put delta right for dK.
 constexpr int kFewKeys = 512;
 
-template <int D, bool F32, int NW>
-__global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW == 4 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
+template <int D, bool F32, int NW, int ROWS = Pieces<F32>::ROWS>
+__global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW == 4 || ROWS == 32 ? 2 : 1) void sparse_dq_kernel(GradArgs a) {
   typedef Tile<D> T;
   enum { ONLY, FIRST, SECOND };
-  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, ROWS = Pieces<F32>::ROWS, STAGE = T::bytes(ROWS);
+  constexpr int KS = D / 16, RB = D / 32, NS = Pieces<F32>::N, STAGE = T::bytes(ROWS);
   constexpr int STAGES = F32 && NW == 2 ? 1 : 2;      // (two waves: one stage, and more workgroups to a CU)
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * NS * STAGE];
   const unsigned item = xcd_item(blockIdx.x, a.share);
@@ -784,7 +786,8 @@ hipError_t launch_grad(const ha_sparse_problem &p, GradArgs &a, hipStream_t st) 
     a.items = (unsigned)((int64_t)s.B * s.H * s.T);
     a.share = xcd_share(a.items);
     if (s.qb == 128) sparse_dq_kernel<D, F32, 4><<<8 * a.share, 256, 0, st>>>(a);
-    else sparse_dq_kernel<D, F32, 2><<<8 * a.share, 128, 0, st>>>(a);
+    else if (F32 || a.items <= 512) sparse_dq_kernel<D, F32, 2><<<8 * a.share, 128, 0, st>>>(a);
+    else sparse_dq_kernel<D, F32, 2, 32><<<8 * a.share, 128, 0, st>>>(a);      // half the LDS, more workgroups to a CU
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (s.Nk > 0) {

@@ -158,6 +158,14 @@ def test_gradients_over_more_blocks_than_are_counted_at_once():
     check(problem(51, H=1, Hkv=1, Nq=700, Nk=64 * 4100 + 5, d=64, qb=64, kb=64, sel=6))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sel", [1, 2, 3, 4, 7])
+def test_more_short_tiles_than_two_to_a_cu(d, sel):
+    """Tiles of 64 queries with less of LDS each, lists that end at every place of the unrolled loop."""
+    check(problem(60 + sel, B=1, H=26, Hkv=2, Nq=1270, Nk=64 * 9 - 40, d=d, qb=64, kb=64, sel=sel))
+    check(problem(70 + sel, B=2, H=13, Hkv=1, Nq=1270, d=d, qb=64, kb=128, sel=sel, causal=True, ragged=[1270, 700], starts=[0, -300]))
+
+
 def test_lists_around_the_length_that_is_walked_twice():
     """448, 512 and 576 keys to a row, in tiles of one launch (causal) and of one length."""
     check(problem(52, H=2, Hkv=1, Nq=900, d=64, qb=64, kb=64, sel=16, causal=True))
