@@ -832,7 +832,7 @@ extern "C" ha_status hybrid_attn_sparse_grad(const ha_sparse_problem *p, const h
   if (reinterpret_cast<uintptr_t>(blocks) & 3u || reinterpret_cast<uintptr_t>(lse) & 3u) return HA_ERR_ALIGN;
   const Sparse s = a.s = sparse_of(*p);
   const GradPlanS f = plan_grad(*p, s);
-  if (p->N_q > 0 && f.total == 0) return HA_ERR_UNSUPPORTED;
+  if (f.total == 0) return HA_ERR_UNSUPPORTED;      // (any plan that is not refused has some bytes, without queries or keys too)
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < f.total) return HA_ERR_WORKSPACE;
   if (p->N_q == 0 && p->N_k == 0) return HA_OK;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
