@@ -1,5 +1,7 @@
 // Marshalling of the calls of block-sparse attention and of the many-tensor optimiser (part of ha_binding.cpp, by the same rule: what is not plain and
 // right gives None, and the Python code takes the call).  These calls allocate what the Python code would: outputs and workspaces that were not given.
+// A refusal of the library gives None too, for the Python code's message: it has enqueued nothing.  A device error may follow launches that are on their way,
+// so that the call must not be made twice, and is raised here.
 //
 // Host time per call in Python / here, us: key_means 13.1 / 5.6, select_blocks 17.0 / 7.0, sparse_forward 22.9 / 6.7, sparse_grad (eight launches) 56 / 41,
 // grad_norm (two launches) 15.9 / 12.6.
@@ -31,7 +33,16 @@ struct Calls {
   many_fn many;
 };
 Calls g_calls = {};
-PyObject *g_get_device = nullptr, *g_native = nullptr;      // the current device's index; "native"
+PyObject *g_get_device = nullptr, *g_native = nullptr, *g_error = nullptr;      // the current device's index; "native"; HybridAttnError(status, where)
+
+// What a call gives whose status is not HA_OK.
+PyObject *failed(ha_status st, const char *where) {
+  if (st != HA_ERR_DEVICE) Py_RETURN_NONE;
+  if (!g_error) return PyErr_Format(PyExc_RuntimeError, "%s: device error", where);
+  const Ref e(PyObject_CallFunction(g_error, "is", static_cast<int>(st), where));
+  if (e.p) PyErr_SetObject(g_error, e.p);
+  return nullptr;
+}
 
 // The tensor's device is the current one, and the call goes to its current stream.
 bool here(PyObject *stream, const at::Tensor &t, void **out) {
@@ -149,7 +160,7 @@ PyObject *key_means(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor means = out ? *out : fresh(sizes, at::kFloat, *k);
     ha_status st;
     HA_CALL(st, g_calls.means(&p, &kv, last, static_cast<float *>(means.data_ptr()), stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_key_means");
     return THPVariable_Wrap(means);
   } catch (...) {
     PyErr_Clear();
@@ -180,7 +191,7 @@ PyObject *select_blocks(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor blocks = out ? *out : fresh(sizes, at::kInt, *q);
     ha_status st;
     HA_CALL(st, g_calls.select(&p, &qv, static_cast<const float *>(means->data_ptr()), static_cast<int32_t *>(blocks.data_ptr()), ws, bytes, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_select_blocks");
     return THPVariable_Wrap(blocks);
   } catch (...) {
     PyErr_Clear();
@@ -227,7 +238,7 @@ PyObject *sparse_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     float *lse_at = new_lse.defined() ? static_cast<float *>(new_lse.data_ptr()) : nullptr;
     ha_status st;
     HA_CALL(st, g_calls.forward(&p, &qv, &kv, &vv, lists, &ov, lse_at, ws, bytes, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_sparse_forward");
     const Ref o_py(THPVariable_Wrap(o));
     if (!new_lse.defined()) return PyTuple_Pack(2, o_py.p, Py_None);
     const Ref l_py(THPVariable_Wrap(new_lse));
@@ -264,7 +275,7 @@ PyObject *sparse_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const float *lse_at = static_cast<const float *>(lse->data_ptr());
     ha_status st;
     HA_CALL(st, g_calls.grad(&p, &qv, &kv, &vv, lists, &ov, lse_at, &dv, &gv[0], &gv[1], &gv[2], ws, bytes, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_sparse_grad");
     const Ref a(THPVariable_Wrap(grads[0])), b(THPVariable_Wrap(grads[1])), c(THPVariable_Wrap(grads[2]));
     return PyTuple_Pack(3, a.p, b.p, c.p);
   } catch (...) {
@@ -319,7 +330,7 @@ PyObject *grad_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     float *to = static_cast<float *>(result.data_ptr());
     ha_status st;
     HA_CALL(st, g_calls.norm(list.n, static_cast<const ha_tensor *>(list.at), max_norm, to, ws, bytes, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_grad_norm");
     return THPVariable_Wrap(result);
   } catch (...) {
     PyErr_Clear();
@@ -340,7 +351,7 @@ PyObject *grad_clip(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const float *from = static_cast<const float *>(result->data_ptr());
     ha_status st;
     HA_CALL(st, g_calls.clip(list.n, static_cast<const ha_tensor *>(list.at), static_cast<const ha_tensor *>(out.at), from, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_grad_clip");
     return PyLong_FromLong(st);
   } catch (...) {
     PyErr_Clear();
@@ -363,7 +374,7 @@ PyObject *update_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const float *from = static_cast<const float *>(result->data_ptr());
     ha_status st;
     HA_CALL(st, g_calls.many(&o, list.n, static_cast<const ha_param *>(list.at), from, stream));
-    if (st != HA_OK) Py_RETURN_NONE;
+    if (st != HA_OK) return failed(st, "hybrid_attn_param_update_many");
     return PyLong_FromLong(st);
   } catch (...) {
     PyErr_Clear();
@@ -447,10 +458,10 @@ PyObject *describe_params(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
 }
 
-// bind_calls(addresses of the ten functions in the order of Calls, current-device function)
+// bind_calls(addresses of the ten functions in the order of Calls, current-device function, class of errors)
 PyObject *bind_calls(PyObject *, PyObject *args) {
-  PyObject *list, *get_device;
-  if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &list, &get_device)) return nullptr;
+  PyObject *list, *get_device, *error = nullptr;
+  if (!PyArg_ParseTuple(args, "O!O|O", &PyTuple_Type, &list, &get_device, &error)) return nullptr;
   void *at[sizeof(Calls) / sizeof(void *)];
   constexpr Py_ssize_t N = sizeof(at) / sizeof(at[0]);
   if (PyTuple_GET_SIZE(list) != N) {
@@ -461,6 +472,8 @@ PyObject *bind_calls(PyObject *, PyObject *args) {
   if (PyErr_Occurred()) return nullptr;
   Py_INCREF(get_device);
   Py_XSETREF(g_get_device, get_device);
+  Py_XINCREF(error);
+  Py_XSETREF(g_error, error);
   if (!g_native && !(g_native = PyUnicode_InternFromString("native"))) return nullptr;
   static_assert(sizeof(g_calls) == sizeof(at), "function pointers only");
   std::memcpy(&g_calls, at, sizeof(g_calls));

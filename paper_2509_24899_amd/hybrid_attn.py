@@ -196,7 +196,7 @@ def _calls():
                 native.bind_calls(tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
                     "hybrid_attn_key_means", "hybrid_attn_select_workspace_bytes", "hybrid_attn_select_blocks", "hybrid_attn_sparse_workspace_bytes",
                     "hybrid_attn_sparse_forward", "hybrid_attn_sparse_grad_workspace_bytes", "hybrid_attn_sparse_grad", "hybrid_attn_grad_norm",
-                    "hybrid_attn_grad_clip", "hybrid_attn_param_update_many")), current)
+                    "hybrid_attn_grad_clip", "hybrid_attn_param_update_many")), current, HybridAttnError)
         _CALLS = native
     return _CALLS
 
