@@ -1,6 +1,6 @@
 """Global gradient norm, clipping and the update of many parameters (include/hybrid_attn_optim.h).
 
-    grads, params = TensorList(grads), ParamList(masters, grads, m, v, copies)         # once: they hold the tensors and their addresses
+    grads, params = TensorList(grads), ParamList(masters, grads, m, v, copies)         # once, if the gradients are the same tensors in every step
     result = hybrid_attn_grad_norm(grads, max_norm)                                     # device (norm, factor)
     hybrid_attn_param_update_many(params, lr, kind=HA_OPT_ADAMW, step=step, clip=result)
 
@@ -51,21 +51,30 @@ def _native(c, n, workspace_bytes, device):
 
 
 class TensorList:
-    """Contiguous bf16 or fp32 tensors on one GPU, with their descriptors for the C ABI.  It holds the tensors; a program whose gradients keep their
-    memory over its steps builds it once, one whose gradients are new tensors every step builds it every step."""
+    """Contiguous bf16 or fp32 tensors on one GPU, with their descriptors for the C ABI.  It holds the tensors, and every call that takes it looks at the
+    memory they have then (data, set_ and resize_ may give them another).  It does not see gradients that take a tensor's place: a program whose
+    gradients are the same tensors in every step builds it once, one that sets them to None or makes new ones builds it every step."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
         self.c = (ha_tensor * len(self.tensors))()
+        self.device = self.sizes = None
+        self.refresh()
+
+    def refresh(self):
+        """Describes the tensors as they are now."""
         native = _ha._CALLS or _ha._calls()
         if native and self.tensors and (done := native.describe_tensors(self.tensors, ctypes.addressof(self.c))) is not None:
-            self.device, self.sizes = torch.device("cuda", done[0]), done[1]
+            index, sizes = done
+            device = self.device if self.device is not None and self.device.index == index else torch.device("cuda", index)
         else:
-            self.device = _one_device(self.tensors)
+            device = _one_device(self.tensors)
             self.c[:] = [ha_tensor(t.data_ptr(), t.numel(), _ha._dtype_code(t), 0) for t in self.tensors]
-            self.sizes = [t.numel() for t in self.tensors]
-        self.workspace_bytes = _ha._lib().hybrid_attn_grad_norm_workspace_bytes(len(self.tensors), self.c)
-        self.native = _native(self.c, len(self.tensors), self.workspace_bytes, self.device)
+            sizes = [t.numel() for t in self.tensors]
+        if sizes != self.sizes or device != self.device:
+            self.device, self.sizes = device, sizes
+            self.workspace_bytes = _ha._lib().hybrid_attn_grad_norm_workspace_bytes(len(self.tensors), self.c)
+            self.native = _native(self.c, len(self.tensors), self.workspace_bytes, self.device)
 
     def __len__(self):
         return len(self.tensors)
@@ -73,25 +82,33 @@ class TensorList:
 
 class ParamList:
     """Parameters for hybrid_attn_param_update_many: fp32 masters, their gradients (fp32 or bf16), AdamW's moments (None or lists of None: plain steps
-    only) and the copies the forward reads (list, or None; single ones may be None).  It holds the tensors."""
+    only) and the copies the forward reads (list, or None; single ones may be None).  It holds the tensors; what TensorList says of their memory, and of
+    gradients that are new tensors, holds here too."""
 
     def __init__(self, masters, grads, m=None, v=None, param_io=None):
+        masters, grads = list(masters), list(grads)
         n = len(masters)
         m, v, io = (list(x) if x is not None else [None] * n for x in (m, v, param_io))
-        masters, grads = list(masters), list(grads)
         if not len(grads) == len(m) == len(v) == len(io) == n:
             raise ValueError("masters, grads, m, v and param_io must be lists of one length")
         self.tensors = (masters, grads, m, v, io)
         self.c = (ha_param * n)()
+        self.device = self.native = None
+        self.refresh()
+
+    def refresh(self):
+        """Describes the tensors as they are now."""
         native = _ha._CALLS or _ha._calls()
-        if native and n and (device := native.describe_params(self.tensors, ctypes.addressof(self.c))) is not None:
-            self.device = torch.device("cuda", device)
+        if native and len(self) and (index := native.describe_params(self.tensors, ctypes.addressof(self.c))) is not None:
+            device = self.device if self.device is not None and self.device.index == index else torch.device("cuda", index)
         else:
-            self._describe()
-        self.native = _native(self.c, n, 0, self.device)
+            device = self._describe()
+        if device != self.device or self.native is None:
+            self.device = device
+            self.native = _native(self.c, len(self), 0, device)
 
     def _describe(self):
-        self.device = _one_device([t for x in self.tensors for t in x])
+        device = _one_device([t for x in self.tensors for t in x])
         for p, g, a, b, c in zip(*self.tensors):
             if any(t is not None and t.dtype != torch.float32 for t in (p, a, b)):
                 raise ValueError("masters, m and v must be fp32")
@@ -102,13 +119,17 @@ class ParamList:
             return None if t is None else t.data_ptr()
         self.c[:] = [ha_param(at(p), at(g), at(a), at(b), at(c), p.numel(), _ha._dtype_code(g), _ha.HA_BF16 if c is None else _ha._dtype_code(c))
                      for p, g, a, b, c in zip(*self.tensors)]
+        return device
 
     def __len__(self):
         return len(self.tensors[0])
 
 
 def _tensor_list(x) -> TensorList:
-    return x if isinstance(x, TensorList) else TensorList(x)
+    if not isinstance(x, TensorList):
+        return TensorList(x)
+    x.refresh()
+    return x
 
 
 def _result(t, device):
@@ -174,6 +195,7 @@ def hybrid_attn_param_update_many(params: ParamList, lr: float, kind: int = 0, s
                                   beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01, clip=None, stream=None):
     """One update of all parameters of a ParamList in place, as hybrid_attn_param_update makes it of one.  clip: hybrid_attn_grad_norm's result, whose factor
     multiplies the gradients besides grad_scale; where it is not finite, nothing changes.  Does not synchronise."""
+    params.refresh()
     native = _ha._CALLS or _ha._calls()
     if native and native.update_many(params, lr, kind, step, grad_scale, beta1, beta2, eps, weight_decay, clip, stream) is not None:
         return
