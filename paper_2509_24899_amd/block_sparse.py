@@ -143,10 +143,11 @@ def _key_means(k, k_block, key_len, only_last, out, stream):
     if only_last > 0 and out is None:
         raise ValueError("only_last needs out: the other blocks' means are left as they are")
     with _ha._on_device_of(k):
-        prob = make_sparse_problem(k.shape, k.shape, k.dtype, k.device, k_block=k_block, key_len=key_len)
+        B, H_kv, N_k, d = k.shape
+        prob = make_sparse_problem((B, H_kv, 0, d), k.shape, k.dtype, k.device, k_block=k_block, key_len=key_len)      # (no queries: their limits are not the means')
         lib = _ha._lib()
         _check(lib.hybrid_attn_sparse_validate(prob), "hybrid_attn_sparse_validate")
-        shape = (k.shape[0], k.shape[1], _cdiv(k.shape[2], k_block), k.shape[3])
+        shape = (B, H_kv, _cdiv(N_k, k_block), d)
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=k.device)
         _float32("out", out, shape, k.device)

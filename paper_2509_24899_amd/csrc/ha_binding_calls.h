@@ -152,7 +152,7 @@ PyObject *key_means(PyObject *, PyObject *const *args, Py_ssize_t n) {
     ha_view kv;
     int32_t last;
     void *stream;
-    if (!k || !view_of(k, *k, &kv) || !sizes_of(&p, *k, k->size(1), k->size(2), k->size(1), k->size(2)) || !block_sizes(nullptr, args[1], &p) ||
+    if (!k || !view_of(k, *k, &kv) || !sizes_of(&p, *k, k->size(1), 0, k->size(1), k->size(2)) || !block_sizes(nullptr, args[1], &p) ||
         !per_entry(args[2], k->size(0), *k, &p.key_len) || !small_int(args[3], &last) || (last != 0 && !out) || !here(args[5], *k, &stream))
       Py_RETURN_NONE;
     const int64_t sizes[] = {k->size(0), k->size(1), blocks_of(k->size(2), p.k_block), k->size(3)};
