@@ -66,7 +66,8 @@ ha_status hybrid_attn_key_means(const ha_sparse_problem *p, const ha_view *k, in
 /* Enqueues the choice: blocks, device int32 [B, H_kv, ceil(N_q / q_block), n_select], every list in rising order with -1 behind its last block.
  * Blocks without a key below key_len are in no list, and with causal neither are those behind the last position of the tile.  Blocks that are
  * always kept (keep_first, near_tokens) come first, then those of highest score, of equal ones the lower index.  Scores are formed in double.
- * HA_ERR_SHAPE where n_select does not hold the blocks that are always kept, and not all blocks.  (A score that is NaN ranks above all others.)
+ * HA_ERR_SHAPE where n_select does not hold the blocks that are always kept, and not all blocks (with q_start, which the host does not read: where there
+ * are places at which it would not, blocks that are kept for both reasons counted twice).  (A score that is NaN ranks above all others.)
  * workspace: device, 256-byte aligned, hybrid_attn_select_workspace_bytes() bytes. */
 size_t hybrid_attn_select_workspace_bytes(const ha_sparse_problem *p);
 ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const ha_view *q, const float *means, int32_t *blocks, void *workspace,

@@ -503,14 +503,28 @@ void launch_choose(const Sparse &s, const uint64_t *keys, int32_t *blocks, hipSt
   else choose_kernel<<<rows, 256, 0, st>>>(keys, s.Tk, s.sel, blocks);
 }
 
-// Blocks that are always kept, at most.
-int64_t forced_blocks(const ha_sparse_problem &p) {
-  int64_t n = p.keep_first;
-  if (p.near_tokens >= 0) {
-    const int64_t span = (p.N_q < p.q_block ? p.N_q : p.q_block) + (int64_t)p.near_tokens * (p.causal ? 1 : 2);
-    n += (span - 1 + p.k_block - 1) / p.k_block + 1;
+// Whether a list holds the blocks that are always kept.  A count that no place of the tiles exceeds decides first; where it does not fit and the places are
+// known (q_start lies on the device), the blocks of every tile are counted.
+bool holds_kept_blocks(const ha_sparse_problem &p) {
+  const int64_t kb = p.k_block, Tk = (p.N_k + kb - 1) / kb, before = p.near_tokens, behind = p.causal ? 0 : p.near_tokens;
+  if (p.n_select >= Tk) return true;
+  int64_t most = p.keep_first;
+  if (p.near_tokens >= 0) most += ((p.N_q < p.q_block ? p.N_q : p.q_block) + before + behind - 1 + kb - 1) / kb + 1;
+  if (most <= p.n_select) return true;
+  if (p.q_start) return false;
+  auto block = [&](int64_t key) { return key >= 0 ? key / kb : -((-key + kb - 1) / kb); };
+  for (int64_t i = 0; i < p.N_q; i += p.q_block) {
+    const int64_t lo = (int64_t)p.N_k - p.N_q + i, hi = lo + (p.N_q - i < p.q_block ? p.N_q - i : p.q_block) - 1;      // the tile's positions
+    const int64_t last = p.causal && block(hi) < Tk - 1 ? block(hi) : Tk - 1;                                      // the last block that it may see
+    const int64_t first_kept = p.keep_first < last + 1 ? p.keep_first : last + 1;
+    int64_t n = first_kept > 0 ? first_kept : 0;
+    if (p.near_tokens >= 0) {
+      const int64_t from = block(lo - before) > n ? block(lo - before) : n, to = block(hi + behind) < last ? block(hi + behind) : last;
+      if (to >= from) n += to - from + 1;
+    }
+    if (n > p.n_select) return false;
   }
-  return n;
+  return true;
 }
 
 }  // namespace
@@ -575,7 +589,7 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
   if ((st = check_view(*p, q, p->H, p->N_q, p->q_block, false, qv)) != HA_OK) return st;
   const Sparse s = sparse_of(*p);
   if (p->causal && p->near_tokens < 0) return HA_ERR_SHAPE;
-  if (p->n_select < s.Tk && forced_blocks(*p) > p->n_select) return HA_ERR_SHAPE;
+  if (!holds_kept_blocks(*p)) return HA_ERR_SHAPE;
   if (p->N_q == 0) return HA_OK;
   if (!blocks || (p->N_k > 0 && !means)) return HA_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(means) & 15u || reinterpret_cast<uintptr_t>(blocks) & 3u) return HA_ERR_ALIGN;
