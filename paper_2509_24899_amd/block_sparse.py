@@ -68,6 +68,7 @@ def make_sparse_problem(q_shape, k_shape, dtype, device, q_block=128, k_block=64
         raise ValueError(f"unsupported dtype {dtype}: q, k, v must be bfloat16 or float32")
     if softmax_scale is None:
         softmax_scale = float(d) ** -0.5
+    _ha._fit_int32(B=B, H=H, H_kv=k_shape[1], N_q=Nq, N_k=k_shape[2], d=d, q_block=q_block, k_block=k_block, n_select=n_select, keep_first=keep_first, near=near)
     return ha_sparse_problem(B, H, k_shape[1], Nq, k_shape[2], d, _ha.HA_BF16 if dtype == torch.bfloat16 else _ha.HA_F32, q_block, k_block, n_select,
                              int(bool(causal)), keep_first, near, softmax_scale, _per_entry(q_start, "q_start", B, device), _per_entry(key_len, "key_len", B, device))
 
@@ -142,6 +143,7 @@ def _key_means(k, k_block, key_len, only_last, out, stream):
         raise ValueError("k must be a [B, H_kv, N_k, d] view")
     if only_last > 0 and out is None:
         raise ValueError("only_last needs out: the other blocks' means are left as they are")
+    _ha._fit_int32(only_last=only_last)
     with _ha._on_device_of(k):
         B, H_kv, N_k, d = k.shape
         prob = make_sparse_problem((B, H_kv, 0, d), k.shape, k.dtype, k.device, k_block=k_block, key_len=key_len)      # (no queries: their limits are not the means')

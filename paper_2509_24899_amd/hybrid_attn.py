@@ -325,6 +325,13 @@ def _alloc_on(stream):
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
+def _fit_int32(**numbers):
+    """Refuses what ctypes would cut off to the C ABI's 32 bits."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name} must fit 32 bits, got {x}")
+
+
 def _on_device(device):
     """Context in which `device` is the current GPU: the C ABI launches on the current one."""
     return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)

@@ -204,6 +204,7 @@ def hybrid_attn_param_update_many(params: ParamList, lr: float, kind: int = 0, s
         _result(clip, params.device)
     if params.device is None:
         return
+    _ha._fit_int32(kind=kind, step=step)
     opt = _ha.ha_optimizer(kind, step, lr, grad_scale, beta1, beta2, eps, weight_decay)
     with _ha._on_device(params.device):
         stream_handle = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(params.device.index)
