@@ -625,10 +625,12 @@ extern "C" ha_status hybrid_attn_select_blocks(const ha_sparse_problem *p, const
   if (s.Tk <= kFusedBlocks) {
 #define HA_FUSED(V) (p->d_head == 128 ? score_and_choose_kernel<128, V><<<dim3(groups, heads), 1024, 0, stream>>>(a) \
                                       : score_and_choose_kernel<64, V><<<dim3(groups, heads), 1024, 0, stream>>>(a))
-    // (a list's keys in as few registers as hold them; us at 4096 tiles with 4 / 8 / 10 registers and with 16: 240 blocks 38.9 / 47.7, 500 47.1 / 52.7, 590 48.8 / 52.2)
+    // A list's keys in four registers, eight, twelve or sixteen: every one that holds nothing costs its part of the search, and its LDS.  Us with as many as hold
+    // the blocks / with 16, d = 128: 4096 tiles 240 blocks 38.9 / 47.7, 500 47.1 / 52.7, 513 49.9 / 52.5, 768 53.0 / 55.2; 768 tiles 513 blocks 34.5 / 37.0, 768 37.0 / 38.9;
+    // 14 thousand tiles 513 blocks 185 / 195, 768 198 / 206.  (Ten are 2 - 4 % sooner than twelve where they hold them.)
     if (s.Tk <= 256) HA_FUSED(4);
     else if (s.Tk <= 512) HA_FUSED(8);
-    else if (s.Tk <= 640) HA_FUSED(10);
+    else if (s.Tk <= 768) HA_FUSED(12);
     else HA_FUSED(16);
 #undef HA_FUSED
   } else {
