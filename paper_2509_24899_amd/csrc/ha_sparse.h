@@ -108,13 +108,23 @@ static __device__ __forceinline__ void split8(f32x8 x, bf16x8 (&out)[NS]) {
       for (int i = 0; i < 8; ++i) x[i] -= static_cast<float>(out[n][i]);
   }
 }
-// Values that may be infinite: those have one piece (infinity less infinity is none).
+// Any values: infinities and NaN have one piece (infinity less infinity is none), and the first piece of a finite value above bf16's largest, which would
+// round to infinity, is cut off instead of rounded.
 static __device__ __forceinline__ void split8_any(f32x4 lo, f32x4 hi, bf16x8 (&out)[3]) {
   const f32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   split8<3>(x, out);
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) any |= !__builtin_isfinite(static_cast<float>(out[0][i]));
+  if (!any) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (!__builtin_isfinite(x[i])) out[1][i] = out[2][i] = static_cast<__bf16>(0.f);
+    if (!__builtin_isfinite(static_cast<float>(out[0][i]))) {
+      const float first = __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u), rest = __builtin_isfinite(x[i]) ? x[i] - first : 0.f;
+      if (__builtin_isfinite(x[i])) out[0][i] = static_cast<__bf16>(first);
+      out[1][i] = static_cast<__bf16>(rest);
+      out[2][i] = static_cast<__bf16>(rest - static_cast<float>(out[1][i]));
+    }
 }
 // a b with both in pieces, small terms first; of three pieces the products that stay below the last bit are left out (six of nine are formed).
 template <int NS>
