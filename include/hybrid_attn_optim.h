@@ -24,7 +24,8 @@ typedef struct ha_tensor {
 
 /* Enqueues result[0] = sqrt(sum of the squares of all elements of all tensors) and result[1] = min(1, max_norm / result[0]), 1 where the
  * norm is 0.  result: device float[2].  Squares are summed in double, in a fixed order (bitwise reproducible).  A NaN among the gradients makes
- * both NaN; an infinity makes the norm infinite and the factor NaN: the calls that take the result then leave what they would write as it was.
+ * both NaN; an infinity makes the norm infinite and the factor NaN: the calls that take the result then leave what they would write as it was.  (Finite gradients
+ * whose norm is beyond fp32 have result[0] infinite, and the factor that brings them down to max_norm.)
  * max_norm: positive, or infinity (the norm alone is wanted: the factor is 1 while the norm is finite).  workspace: device, 8-byte aligned,
  * hybrid_attn_grad_norm_workspace_bytes() bytes, contents undefined before and after.  Errors (nothing is enqueued): HA_ERR_NULL,
  * HA_ERR_SHAPE, HA_ERR_UNSUPPORTED (unknown dtype), HA_ERR_ALIGN, HA_ERR_WORKSPACE, HA_ERR_DEVICE. */
@@ -50,7 +51,7 @@ typedef struct ha_param {
 /* hybrid_attn_param_update of all the parameters in as few launches as they fit.  result: device float[2] as hybrid_attn_grad_norm leaves it
  * or NULL: gradients are scaled by opt->grad_scale * result[1] (where the gradients' scale matters to the norm, it is taken of the gradients as
  * they stand, without grad_scale).  Where result[1] is not finite, nothing is written: a step whose gradients overflowed is skipped on
- * the device.  No two of the tensors that are written (masters, moments, copies) overlap.  Errors as for hybrid_attn_param_update. */
+ * the device.  The rates are opt's floats, 1 - beta too.  No two of the tensors that are written (masters, moments, copies) overlap.  Errors as for hybrid_attn_param_update. */
 ha_status hybrid_attn_param_update_many(const ha_optimizer *opt, int32_t n_params, const ha_param *params, const float *result, void *hip_stream);
 
 #ifdef __cplusplus

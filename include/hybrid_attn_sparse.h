@@ -33,7 +33,8 @@ typedef struct ha_sparse_problem {
   int32_t N_q, N_k;       /* 0 is allowed: no queries, or no keys */
   int32_t d_head;         /* 64 or 128 */
   int32_t dtype;          /* ha_dtype of q, k, v, out and their gradients.  HA_F32 tensors are not rounded to bf16: every value is
-                             split into three bf16 ones and multiplied in six products with fp32 accumulation, about fp32's own precision. */
+                             split into three bf16 ones and multiplied in six products with fp32 accumulation, about fp32's own precision
+                             (values below some 2^-110 keep fewer bits: a piece is a multiple of 2^-133). */
   int32_t q_block, k_block;   /* 64 or 128 each */
   int32_t n_select;       /* length of a list, 1 .. 2^20 */
   int32_t causal;         /* 0 or 1 */
@@ -65,7 +66,8 @@ ha_status hybrid_attn_key_means(const ha_sparse_problem *p, const ha_view *k, in
 
 /* Enqueues the choice: blocks, device int32 [B, H_kv, ceil(N_q / q_block), n_select], every list in rising order with -1 behind its last block.
  * Blocks without a key below key_len are in no list, and with causal neither are those behind the last position of the tile.  Blocks that are
- * always kept (keep_first, near_tokens) come first, then those of highest score, of equal ones the lower index.  Scores are formed in double.
+ * always kept (keep_first, near_tokens) come first, then those of highest score, of equal ones the lower index.  Scores are sums rounded in double, the same bit
+ * for bit every time; ones that differ by no more than such roundings may stand in either order.
  * HA_ERR_SHAPE where n_select does not hold the blocks that are always kept, and not all blocks (with q_start, which the host does not read: where there
  * are places at which it would not, blocks that are kept for both reasons counted twice).  (A score that is NaN ranks above all others.)
  * workspace: device, 256-byte aligned, hybrid_attn_select_workspace_bytes() bytes. */

@@ -135,7 +135,8 @@ static __device__ __forceinline__ f32x16 mfma_split(const bf16x8 (&a)[NS], const
     for (int n = 0; n <= order; ++n) c = mfma32(a[order - n], b[n], c);
   return c;
 }
-// Pieces of a tensor, and rows that lie in LDS at a time (two stages of keys and values, or of queries and gradients, have to fit).
+// Pieces of a tensor, and rows of a step of the kernels that take both types (fp32 forward, dQ, fp32 dK and dV): one or two steps' keys and values, or queries and
+// gradients, in all their pieces lie in LDS.
 template <bool F32>
 struct Pieces {
   static constexpr int N = F32 ? 3 : 1, ROWS = F32 ? 32 : 64;

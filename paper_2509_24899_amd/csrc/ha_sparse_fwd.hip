@@ -3,11 +3,14 @@
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i),   j over the keys of the blocks in the tile's list
 //
 // in one pass over the list: m_i follows the largest logit seen, and what has been summed is rescaled when it has moved far.  A workgroup takes
-// one tile of queries of one head, 32 queries to a wave, and walks the list 64 keys at a time (fp32: 32); keys and values lie in LDS (two stages, the next on its way
-// while the current one is worked on) and every wave reads all of them.  Per wave and 32 keys: S^T = K Q^T on the matrix cores, exponentials,
-// O^T += V^T P^T with P straight from the registers that hold S.  The logits and the weights' sums are fp32; the weights are rounded to bf16 for
-// the second product only (fp32 tensors: all operands are three bf16 pieces, six products each).
-// Few tiles: the list is cut into ranges, a workgroup each, whose sums a second kernel joins.
+// one tile of queries of one head, 32 queries to a wave, and walks the list 32 keys at a time; keys and values lie in LDS (how many steps of them, and how far ahead
+// they are asked for, stands at each kernel) and every wave reads all of them.  Per wave and 32 keys: S^T = K Q^T on the matrix cores, exponentials,
+// O^T += V^T P^T with P straight from the registers that hold S.  Few tiles: the list is cut into ranges, a workgroup each, whose sums a second kernel joins.
+//
+// The logits, the weights' sums and O are fp32.  Of bf16 tensors the weights are rounded to bf16 for the second product, since a matrix instruction takes both
+// its operands in one type and V is bf16; the sum that divides is that of the unrounded ones.  A weight is off by half a step at most, 2^-8, and the output by 0.23 %
+// on the average where its own rounding alone makes 0.17; the weights in two pieces would be half as many products again of the second kind, a quarter of all.
+// Of fp32 tensors all operands are three bf16 pieces, six products each.
 #include <cmath>
 #include <type_traits>
 

@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256) void inverse_fill_kernel(GradArgs a) {
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
-// The forward's walk with three products, S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  1.10 ms at 480p (1.1 PFLOP/s), matrix cores busy 64 % of the cycles.
+// The forward's walk with three products, S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  1.10 ms at 480p (1.1 PFLOP/s), matrix cores busy 63 % of the cycles.
 // Tiles of 64 queries are two waves, which go 32 keys at a time where a CU has more than two of them: all gradients of 32 heads of 8192 tokens, 16 blocks of 64,
 // 631 us for 657 with 64 keys at a time (d = 64: 332 for 343), of four heads 131 for 122 (90 for 87).
 //
@@ -314,9 +314,9 @@ __global__ __launch_bounds__(64 * NW, F32 ? (NW == 2 && D == 64 ? 2 : 1) : NW ==
           if constexpr (PASS == FIRST) {
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-            total += static_cast<float>(db[0][x]);
-            unrounded += ds[x];
-          }
+              total += static_cast<float>(db[0][x]);
+              unrounded += ds[x];
+            }
           }
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
@@ -366,7 +366,8 @@ __device__ __forceinline__ void request_stat(const float *src, char *to, int lan
 
 // Four waves: the halves of the keys by two chunks at a time.  Two workgroups to a CU, so that one's loads, waits and exponentials run under the other's
 // products; that leaves 256 registers to a wave: 128 for dK and dV, 32 for S and dP, K and half of V; the other half of V lies in LDS.  S starts from
-// -lse / scale and dP from -delta, so that exp2(c S) is P and P dP is dS.  1.65 ms at 480p for four products (1.0 PFLOP/s), matrix cores busy 57 %.  It is
+// -lse / scale and dP from -delta, so that exp2(c S) is P and P dP is dS; the d / 16 sums then round at the size of lse / scale, which puts a weight off by up to d / 16 lse 2^-24
+// (1e-5 of it at lse = 20, where its rounding to bf16 is 4e-3).  1.65 ms at 480p for four products (1.0 PFLOP/s), matrix cores busy 56 %.  It is
 // bound by how little of one workgroup's loads and vector work the other one covers, and by the L2 (items in another order miss it almost twice as often).
 template <int D>
 __global__ __launch_bounds__(256, 2) void sparse_dkv_kernel(GradArgs a) {

@@ -2,8 +2,10 @@
 //
 //   mean_j = sum of the keys of block j / their number        score_tj = (sum of the queries of tile t over its heads) . mean_j
 //
-// Everything that decides is formed in double: the sums of 64 or 128 bf16 values are exact there, and two scores that differ at all are in the
-// right order, whatever the order of summation (in fp32 about one list in ten thousand changed with it).  The sums over q and k are bound by
+// Everything that decides is formed in double (in fp32 about one list in ten thousand changed with the order of summation).  The sums of 64 or 128 bf16 values
+// are exact there, sums of fp32 values are not, and a score is a sum of d products rounded in double: scores that are closer than some 1e-15 of their terms
+// may stand in either order, and rank by index only where the doubles are equal.  A list is the same bit for bit for one problem; the two ways of forming the
+// scores (few_tiles) sum in different orders, so that such near ties may fall otherwise where the number of tiles is another.  The sums over q and k are bound by
 // memory (12 heads of 32760 x 128 bf16, 100 MB: 20 us for keys and 20 for queries, 5 TB/s); the scores of 128 queries against a block of 64 keys take one
 // product of d values.
 #include <climits>
@@ -286,7 +288,9 @@ __device__ __forceinline__ void choose_wave(const uint64_t *keys, int sel, int32
 }
 
 // Many tiles: a workgroup scores kTiles of them against all blocks (at most 64 V), then every wave makes one tile's choice.  26 us at 256 tiles x 512 blocks
-// of 12 heads (480p), 15 of them the scores; 192 workgroups of 16 waves, whose chain of loads, products, barrier and search is what it takes.
+// of 12 heads (480p), 15 of them the scores: 192 workgroups, one to a CU, each a chain of loads, products, barrier and search, matrix cores busy 28 % of the cycles.
+// Sixteen waves take all registers of a CU, so that no second workgroup runs beside one: 591 tiles x 591 blocks of 24 heads (720p with guidance), 888 workgroups,
+// are four rounds of such chains, 111 us, matrix cores busy 31 %.
 template <int D, int V>
 __global__ __launch_bounds__(1024) void score_and_choose_kernel(ScoreArgs a) {
   const Sparse &s = a.s;

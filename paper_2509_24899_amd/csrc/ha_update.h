@@ -37,7 +37,7 @@ static inline ha_status check_optimizer(const ha_optimizer *opt) {
   return HA_OK;
 }
 
-// (the bias corrections of AdamW in double precision)
+// (the bias corrections of AdamW in double precision, of the betas that ha_optimizer holds: floats, as 1 - beta is in update_element)
 static inline UpdateRates update_rates(const ha_optimizer &opt) {
   UpdateRates a{opt.lr, opt.grad_scale, opt.beta1, opt.beta2, opt.eps, 1.f, 0.f, 1.f};
   if (opt.kind == HA_OPT_ADAMW) {

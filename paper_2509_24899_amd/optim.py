@@ -144,7 +144,7 @@ def hybrid_attn_grad_norm_workspace_bytes(grads) -> int:
 
 def hybrid_attn_grad_norm(grads, max_norm: float = float("inf"), result=None, workspace=None, stream=None):
     """Enqueue the global 2-norm of a TensorList (or a list of tensors) and the factor min(1, max_norm / norm) that brings it down to max_norm: returns
-    a device fp32 tensor (norm, factor).  The factor is NaN where the norm is not finite.  Does not synchronise."""
+    a device fp32 tensor (norm, factor).  The factor is NaN where a gradient is not finite.  Does not synchronise."""
     grads = _tensor_list(grads)
     native = _ha._CALLS or _ha._calls()
     if native and (done := native.grad_norm(grads, max_norm, result, workspace, stream)) is not None:
@@ -173,7 +173,7 @@ def _grad_norm(grads, max_norm, result, workspace, stream):
 
 def hybrid_attn_grad_clip(grads, result, out=None, stream=None):
     """Enqueue out = factor * grads for all tensors, with the factor of hybrid_attn_grad_norm's result; out None: in place.  A factor that is not finite
-    leaves out as it was.  Does not synchronise."""
+    leaves out as it was.  No tensor may stand in a list that is written twice.  Does not synchronise."""
     grads = _tensor_list(grads)
     out = grads if out is None else _tensor_list(out)
     if out.sizes != grads.sizes:
@@ -194,7 +194,8 @@ def hybrid_attn_grad_clip(grads, result, out=None, stream=None):
 def hybrid_attn_param_update_many(params: ParamList, lr: float, kind: int = 0, step: int = 1, grad_scale: float = 1.0, beta1: float = 0.9,
                                   beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01, clip=None, stream=None):
     """One update of all parameters of a ParamList in place, as hybrid_attn_param_update makes it of one.  clip: hybrid_attn_grad_norm's result, whose factor
-    multiplies the gradients besides grad_scale; where it is not finite, nothing changes.  Does not synchronise."""
+    multiplies the gradients besides grad_scale; where it is not finite, nothing changes.  No master, moment or copy may stand in the list twice.  Does not
+    synchronise."""
     params.refresh()
     native = _ha._CALLS or _ha._calls()
     if native and native.update_many(params, lr, kind, step, grad_scale, beta1, beta2, eps, weight_decay, clip, stream) is not None:
