@@ -27,7 +27,8 @@ extern "C" {
  * Query i stands at position q_start[b] + i.  It sees key j of a listed block if j < key_len[b] and, with causal, j <= its position.  A query that
  * sees no key has out = 0 and lse = -infinity, and its gradients are zero.  What the memory of keys and values holds at and behind key_len is
  * never used, and with causal neither is what stands behind the last position of a tile; a NaN or infinity at a key that some query of a tile sees may
- * reach all queries of that tile. */
+ * reach all queries of that tile.  The gradients form the weights anew from lse, an fp32 number, which puts them off by some |lse| 2^-22 of their value; logits
+ * (scale q . k) beyond 2^28 in magnitude may give infinities or NaN, in the forward too. */
 typedef struct ha_sparse_problem {
   int32_t B, H, H_kv;     /* H a multiple of H_kv */
   int32_t N_q, N_k;       /* 0 is allowed: no queries, or no keys */
