@@ -33,7 +33,7 @@ struct Calls {
   many_fn many;
 };
 Calls g_calls = {};
-PyObject *g_get_device = nullptr, *g_native = nullptr, *g_error = nullptr;      // the current device's index; "native"; HybridAttnError(status, where)
+PyObject *g_get_device = nullptr, *g_native = nullptr, *g_tensors = nullptr, *g_error = nullptr;      // the current device's index; "native", "tensors"; HybridAttnError(status, where)
 
 // What a call gives whose status is not HA_OK.
 PyObject *failed(ha_status st, const char *where) {
@@ -284,13 +284,74 @@ PyObject *sparse_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
 }
 
-// The `native` tuple of a TensorList or a ParamList: address of the descriptors, how many, workspace bytes of the norm, device index.
+// One tensor of a list: contiguous, on the GPU that *device names (-1: none yet), of a type that the library has.
+bool listed(PyObject *o, int64_t *device, const at::Tensor **t, int32_t *type) {
+  *t = tensor(o);
+  if (!*t || !(*t)->is_cuda() || !(*t)->is_contiguous() || (*device >= 0 && (*t)->get_device() != *device)) return false;
+  if ((*t)->scalar_type() != at::kFloat && (*t)->scalar_type() != at::kBFloat16) return false;
+  *device = (*t)->get_device();
+  *type = (*t)->scalar_type() == at::kFloat ? HA_F32 : HA_BF16;
+  return true;
+}
+
+// One entry of a ParamList's five lists: master, gradient, moments, copy (the last three may be None).
+bool described(PyObject *const *list, Py_ssize_t i, int64_t *device, ha_param *out) {
+  void *at[5];
+  int32_t type[5] = {HA_F32, HA_F32, HA_F32, HA_F32, HA_BF16};
+  int64_t size = 0;
+  for (int f = 0; f < 5; ++f) {
+    PyObject *o = PyList_GET_ITEM(list[f], i);
+    at[f] = nullptr;
+    if (f >= 2 && o == Py_None) continue;
+    const at::Tensor *t;
+    if (!listed(o, device, &t, &type[f]) || (f != 1 && f != 4 && type[f] != HA_F32) || (f > 0 && t->numel() != size)) return false;
+    size = t->numel();
+    at[f] = t->data_ptr();
+  }
+  *out = ha_param{static_cast<float *>(at[0]), at[1], static_cast<float *>(at[2]), static_cast<float *>(at[3]), at[4], static_cast<uint64_t>(size), type[1], type[4]};
+  return true;
+}
+// The five lists of a ParamList, of one length.
+bool five_lists(PyObject *o, PyObject **list) {
+  if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 5) return false;
+  for (int f = 0; f < 5; ++f) {
+    list[f] = PyTuple_GET_ITEM(o, f);
+    if (!PyList_CheckExact(list[f]) || PyList_GET_SIZE(list[f]) != PyList_GET_SIZE(list[0])) return false;
+  }
+  return true;
+}
+
+// Whether the descriptors are those of the tensors as they are now.
+bool still(PyObject *tensors, const ha_tensor *d, Py_ssize_t n, int64_t device) {
+  if (!PyList_CheckExact(tensors) || PyList_GET_SIZE(tensors) != n) return false;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const at::Tensor *t;
+    int32_t type;
+    if (!listed(PyList_GET_ITEM(tensors, i), &device, &t, &type) || d[i].data != t->data_ptr() || d[i].n != static_cast<uint64_t>(t->numel()) || d[i].dtype != type) return false;
+  }
+  return true;
+}
+bool still(PyObject *tensors, const ha_param *d, Py_ssize_t n, int64_t device) {
+  PyObject *list[5];
+  if (!five_lists(tensors, list) || PyList_GET_SIZE(list[0]) != n) return false;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    ha_param p;
+    if (!described(list, i, &device, &p) || p.master != d[i].master || p.grad != d[i].grad || p.m != d[i].m || p.v != d[i].v || p.param_io != d[i].param_io || p.n != d[i].n ||
+        p.grad_dtype != d[i].grad_dtype || p.io_dtype != d[i].io_dtype)
+      return false;
+  }
+  return true;
+}
+
+// The `native` tuple of a TensorList or a ParamList: address of the descriptors, how many, workspace bytes of the norm, device index.  A list whose tensors have other
+// memory than is described is left to the Python code, which describes it anew.
 struct List {
   void *at;
   int32_t n;
   size_t bytes;
   int64_t device;
 };
+template <typename Descriptor>
 bool list_of(PyObject *o, List *out) {
   const Ref t(PyObject_GetAttr(o, g_native));
   if (!t.p || !PyTuple_CheckExact(t.p) || PyTuple_GET_SIZE(t.p) != 4) {
@@ -301,11 +362,12 @@ bool list_of(PyObject *o, List *out) {
   out->n = static_cast<int32_t>(PyLong_AsLong(PyTuple_GET_ITEM(t.p, 1)));
   out->bytes = PyLong_AsSize_t(PyTuple_GET_ITEM(t.p, 2));
   out->device = PyLong_AsLong(PyTuple_GET_ITEM(t.p, 3));
-  if (PyErr_Occurred()) {
+  const Ref tensors(PyErr_Occurred() ? nullptr : PyObject_GetAttr(o, g_tensors));
+  if (!tensors.p) {
     PyErr_Clear();
     return false;
   }
-  return out->device >= 0;
+  return out->device >= 0 && still(tensors.p, static_cast<const Descriptor *>(out->at), out->n, out->device);
 }
 bool result_of(PyObject *o, int64_t device, const at::Tensor **out) {
   const at::Tensor *t = tensor(o);
@@ -321,7 +383,7 @@ PyObject *grad_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     List list;
     float max_norm;
     const at::Tensor *given = nullptr;
-    if (!list_of(args[0], &list) || !number(args[1], &max_norm) || (args[2] != Py_None && !result_of(args[2], list.device, &given))) Py_RETURN_NONE;
+    if (!list_of<ha_tensor>(args[0], &list) || !number(args[1], &max_norm) || (args[2] != Py_None && !result_of(args[2], list.device, &given))) Py_RETURN_NONE;
     const at::Tensor result = given ? *given : at::empty({2}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, static_cast<c10::DeviceIndex>(list.device)));
     at::Tensor keep;
     void *stream, *ws;
@@ -345,7 +407,7 @@ PyObject *grad_clip(PyObject *, PyObject *const *args, Py_ssize_t n) {
     List list, out;
     const at::Tensor *result;
     void *stream;
-    if (!list_of(args[0], &list) || !list_of(args[2], &out) || list.n != out.n || list.device != out.device || !result_of(args[1], list.device, &result) ||
+    if (!list_of<ha_tensor>(args[0], &list) || !list_of<ha_tensor>(args[2], &out) || list.n != out.n || list.device != out.device || !result_of(args[1], list.device, &result) ||
         !here(args[3], *result, &stream))
       Py_RETURN_NONE;
     const float *from = static_cast<const float *>(result->data_ptr());
@@ -367,7 +429,7 @@ PyObject *update_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
     ha_optimizer o = {};
     const at::Tensor *result = nullptr;
     void *stream;
-    if (!list_of(args[0], &list) || !number(args[1], &o.lr) || !small_int(args[2], &o.kind) || !small_int(args[3], &o.step) || !number(args[4], &o.grad_scale) ||
+    if (!list_of<ha_param>(args[0], &list) || !number(args[1], &o.lr) || !small_int(args[2], &o.kind) || !small_int(args[3], &o.step) || !number(args[4], &o.grad_scale) ||
         !number(args[5], &o.beta1) || !number(args[6], &o.beta2) || !number(args[7], &o.eps) || !number(args[8], &o.weight_decay) ||
         !result_of(args[9], list.device, &result) || !here(args[10], *result, &stream))
       Py_RETURN_NONE;
@@ -382,16 +444,6 @@ PyObject *update_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
 }
 #undef HA_CALL
-
-// One tensor of a list: contiguous, on the GPU that *device names (-1: none yet), of a type that the library has.
-bool listed(PyObject *o, int64_t *device, const at::Tensor **t, int32_t *type) {
-  *t = tensor(o);
-  if (!*t || !(*t)->is_cuda() || !(*t)->is_contiguous() || (*device >= 0 && (*t)->get_device() != *device)) return false;
-  if ((*t)->scalar_type() != at::kFloat && (*t)->scalar_type() != at::kBFloat16) return false;
-  *device = (*t)->get_device();
-  *type = (*t)->scalar_type() == at::kFloat ? HA_F32 : HA_BF16;
-  return true;
-}
 
 // describe_tensors(list, address of as many ha_tensor) -> (device index, sizes), or None
 PyObject *describe_tensors(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -423,34 +475,17 @@ PyObject *describe_tensors(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 // describe_params((masters, grads, m, v, copies), address of as many ha_param) -> device index, or None
 PyObject *describe_params(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  if (n != 2 || !PyTuple_CheckExact(args[0]) || PyTuple_GET_SIZE(args[0]) != 5) Py_RETURN_NONE;
+  if (n != 2) Py_RETURN_NONE;
   try {
     ha_param *to = static_cast<ha_param *>(PyLong_AsVoidPtr(args[1]));
     PyObject *list[5];
-    for (int f = 0; f < 5; ++f) {
-      list[f] = PyTuple_GET_ITEM(args[0], f);
-      if (!PyList_CheckExact(list[f]) || PyList_GET_SIZE(list[f]) != PyList_GET_SIZE(list[0])) Py_RETURN_NONE;
-    }
-    if (!to) {
+    if (!to || !five_lists(args[0], list)) {
       PyErr_Clear();
       Py_RETURN_NONE;
     }
     int64_t device = -1;
-    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list[0]); ++i) {
-      void *at[5];
-      int32_t type[5] = {HA_F32, HA_F32, HA_F32, HA_F32, HA_BF16};
-      int64_t size = 0;
-      for (int f = 0; f < 5; ++f) {
-        PyObject *o = PyList_GET_ITEM(list[f], i);
-        at[f] = nullptr;
-        if (f >= 2 && o == Py_None) continue;
-        const at::Tensor *t;
-        if (!listed(o, &device, &t, &type[f]) || (f != 1 && f != 4 && type[f] != HA_F32) || (f > 0 && t->numel() != size)) Py_RETURN_NONE;
-        size = t->numel();
-        at[f] = t->data_ptr();
-      }
-      to[i] = ha_param{static_cast<float *>(at[0]), at[1], static_cast<float *>(at[2]), static_cast<float *>(at[3]), at[4], static_cast<uint64_t>(size), type[1], type[4]};
-    }
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list[0]); ++i)
+      if (!described(list, i, &device, &to[i])) Py_RETURN_NONE;
     return PyLong_FromLongLong(device);
   } catch (...) {
     PyErr_Clear();
@@ -475,6 +510,7 @@ PyObject *bind_calls(PyObject *, PyObject *args) {
   Py_XINCREF(error);
   Py_XSETREF(g_error, error);
   if (!g_native && !(g_native = PyUnicode_InternFromString("native"))) return nullptr;
+  if (!g_tensors && !(g_tensors = PyUnicode_InternFromString("tensors"))) return nullptr;
   static_assert(sizeof(g_calls) == sizeof(at), "function pointers only");
   std::memcpy(&g_calls, at, sizeof(g_calls));
   Py_RETURN_NONE;

@@ -126,10 +126,7 @@ class ParamList:
 
 
 def _tensor_list(x) -> TensorList:
-    if not isinstance(x, TensorList):
-        return TensorList(x)
-    x.refresh()
-    return x
+    return x if isinstance(x, TensorList) else TensorList(x)
 
 
 def _result(t, device):
@@ -139,7 +136,9 @@ def _result(t, device):
 
 
 def hybrid_attn_grad_norm_workspace_bytes(grads) -> int:
-    return _tensor_list(grads).workspace_bytes
+    grads = _tensor_list(grads)
+    grads.refresh()
+    return grads.workspace_bytes
 
 
 def hybrid_attn_grad_norm(grads, max_norm: float = float("inf"), result=None, workspace=None, stream=None):
@@ -154,6 +153,7 @@ def hybrid_attn_grad_norm(grads, max_norm: float = float("inf"), result=None, wo
 
 @_ha._allocations_follow_stream
 def _grad_norm(grads, max_norm, result, workspace, stream):
+    grads.refresh()
     device = grads.device if grads.device is not None else result.device if result is not None else torch.device("cuda", torch.cuda.current_device())
     with _ha._on_device(device):
         if result is None:
@@ -176,11 +176,13 @@ def hybrid_attn_grad_clip(grads, result, out=None, stream=None):
     leaves out as it was.  No tensor may stand in a list that is written twice.  Does not synchronise."""
     grads = _tensor_list(grads)
     out = grads if out is None else _tensor_list(out)
+    native = _ha._CALLS or _ha._calls()
+    if native and out.sizes == grads.sizes and native.grad_clip(grads, result, out, stream) is not None:
+        return
+    grads.refresh()
+    out.refresh()
     if out.sizes != grads.sizes:
         raise ValueError("out must be a list of tensors of the gradients' sizes")
-    native = _ha._CALLS or _ha._calls()
-    if native and native.grad_clip(grads, result, out, stream) is not None:
-        return
     _ha._require_gpu(result)
     if grads.device is not None and out.device != grads.device:
         raise ValueError(f"out must be on {grads.device}")
@@ -196,10 +198,10 @@ def hybrid_attn_param_update_many(params: ParamList, lr: float, kind: int = 0, s
     """One update of all parameters of a ParamList in place, as hybrid_attn_param_update makes it of one.  clip: hybrid_attn_grad_norm's result, whose factor
     multiplies the gradients besides grad_scale; where it is not finite, nothing changes.  No master, moment or copy may stand in the list twice.  Does not
     synchronise."""
-    params.refresh()
     native = _ha._CALLS or _ha._calls()
     if native and native.update_many(params, lr, kind, step, grad_scale, beta1, beta2, eps, weight_decay, clip, stream) is not None:
         return
+    params.refresh()
     if clip is not None:
         _ha._require_gpu(clip)
         _result(clip, params.device)
