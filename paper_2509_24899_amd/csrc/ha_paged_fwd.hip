@@ -1,0 +1,713 @@
+// Attention of new tokens over a paged cache, gfx950.
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i),   j over the slots that new token i sees
+//
+// All query heads of a key head are rows of one product (row R of a sequence is token R / G, head R % G of the group), so that keys and values are read once for a
+// group.  Logits, sums and the output's sums are fp32; of bf16 tensors the weights are rounded to bf16 for the second product (half a step, 2^-8 of each, the sum
+// that divides is that of the unrounded ones), of fp32 tensors every operand is three bf16 pieces, six products each.
+//   few   32 rows at most (single tokens): bound by memory.  A workgroup takes a range of a sequence's slots for a key head, every wave slots of its own.
+//   tile  128 rows, 32 to a wave: bound by the matrix cores.  All waves read the same slots out of LDS.
+// Where either leaves compute units idle the slots are cut into ranges, whose sums a second kernel joins.
+#include <cmath>
+
+#include "ha_paged.h"
+
+#include <algorithm>
+
+namespace ha {
+
+ha_status check_paged(const ha_paged_problem *p) {
+  if (!p) return HA_ERR_NULL;
+  if (p->B <= 0 || p->H <= 0 || p->H_kv <= 0 || p->H % p->H_kv || p->T < 0 || p->d_head <= 0) return HA_ERR_SHAPE;
+  if (p->n_pages < 0 || p->max_pages < 0 || p->max_new < 0 || p->max_new > p->T) return HA_ERR_SHAPE;
+  if (p->causal != 0 && p->causal != 1) return HA_ERR_SHAPE;
+  if (!(p->softmax_scale >= 1e-30f && p->softmax_scale <= 1e30f)) return HA_ERR_SHAPE;
+  if (!p->q_offset && (int64_t)p->B * p->max_new != p->T) return HA_ERR_SHAPE;
+  if (p->dtype != HA_BF16 && p->dtype != HA_F32) return HA_ERR_UNSUPPORTED;
+  if (p->d_head != 64 && p->d_head != 128) return HA_ERR_UNSUPPORTED;
+  if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128 && p->page != 256) return HA_ERR_UNSUPPORTED;
+  if ((int64_t)p->max_pages * p->page > (1 << 30) || (int64_t)p->n_pages * p->page > ((int64_t)1 << 40)) return HA_ERR_UNSUPPORTED;
+  if (p->B > 65535 || p->H > 65535 || (int64_t)p->B * p->H_kv > 65535 || (int64_t)p->T * (p->H / p->H_kv) > (1 << 20) || (int64_t)p->T * p->H > (1 << 24)) return HA_ERR_UNSUPPORTED;
+  if (!p->key_len || (!p->page_table && p->max_pages > 0)) return HA_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(p->page_table) & 3u || reinterpret_cast<uintptr_t>(p->key_len) & 3u || reinterpret_cast<uintptr_t>(p->q_offset) & 3u) return HA_ERR_ALIGN;
+  return HA_OK;
+}
+
+Paged paged_of(const ha_paged_problem &p) {
+  return Paged{p.B, p.H, p.H_kv, p.H / p.H_kv, p.T, p.n_pages, p.page, __builtin_ctz(p.page), p.max_pages, p.max_new, p.causal, p.page_table, p.key_len, p.q_offset};
+}
+
+ha_status check_pool(const ha_paged_problem &p, const ha_view *v, bool written, View &out) {
+  const ha_status st = check_rows(p.n_pages, p.H_kv, p.n_pages ? p.page : 0, p.d_head, p.dtype, v, written, out);
+  if (st != HA_OK) return st;
+  if (p.n_pages && out.sn > ((int64_t)1 << 31) / (p.dtype == HA_BF16 ? 2 : 4) / (p.page + 1)) return HA_ERR_SHAPE;
+  return HA_OK;
+}
+
+namespace {
+
+struct FwdArgs {
+  Paged p;
+  View q, k, v, out;
+  float *lse;
+  int n_split, tiles;         // ranges of the slots; tile: tiles of a key head
+  int leave_few;              // tile: sequences of 32 rows or fewer are another launch's
+  float *po, *pm, *pl;        // n_split > 1: [group][range][rows][D], [group][range][rows]
+  float scale, scale_log2e;
+  unsigned items, share;
+};
+
+// What 32 rows of a wave are: row R of a sequence.
+struct RowsOf {
+  int h, token, see, n_rows;  // this lane's query head, row of T, slots that it sees
+  __device__ __forceinline__ RowsOf(const Paged &p, const NewRows &n, int held, int hk, int R) {
+    n_rows = n.n * p.G;
+    R = min(R, n_rows - 1);
+    const int i = R / p.G;
+    h = hk * p.G + R - i * p.G;
+    token = n.first + i;
+    see = p.causal ? min(held, held - n.all + i + 1) : held;
+  }
+};
+
+// The numbers of the two pages that hold slots key .. key + 15 and key + 16 .. key + 31 (key a multiple of 32).
+struct Step {
+  int key, id0, id1;
+};
+static __device__ __forceinline__ Step step_at(const Paged &p, PageWalk &walk, int key) {
+  const int index = key >> p.page_log2;
+  Step s{key, walk.at(index), -1};
+  s.id1 = p.page > 16 ? s.id0 : index + 1 < p.max_pages ? walk.at(index + 1) : -1;
+  return s;
+}
+// Bytes of a slot's row from the pool's first (the head's part is in `base`).
+static __device__ __forceinline__ int64_t slot_offset(const Paged &p, const View &v, int id, int slot, int esz) {
+  return ((int64_t)id * v.sb + (int64_t)(slot & (p.page - 1)) * v.sn) * esz;
+}
+// Logits of slots that this lane's row does not see.
+static __device__ __forceinline__ void mask_step(f32x16 &sc, const Step &s, int see, int all_see, int g) {
+  if (s.key + 32 > all_see || s.id0 < 0 || s.id1 < 0) {
+    const int see0 = s.id0 < 0 ? 0 : see, see1 = s.id1 < 0 ? 0 : see;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sc[x] = s.key + crow(x, g) < (x < 8 ? see0 : see1) ? sc[x] : -INFINITY;
+  }
+}
+
+static __device__ __forceinline__ float log_sum(float m, float l, float scale) { return l > 0.f ? m * scale + logf(l) : l == 0.f ? -INFINITY : l; }
+
+// ---- few rows --------------------------------------------------------------------------------------------------------
+template <int D>
+static constexpr int image_bytes() { return 4 * 32 * D * 4; }
+// The sums of four waves that walked slots of one range: joined through LDS (`image`: 4 x 32 D values) and stored.
+template <int D, bool F32>
+__device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D / 32], float m, float l, char *lds, float (&stats)[2][4][32], int item, const RowsOf &row, int w, int lane) {
+  constexpr int RB = D / 32, IMAGE = RB * 4 * 64;
+  const int r = lane & 31, g = lane >> 5;
+  const float c = a.scale_log2e;
+  l = xhalf_sum(l);
+  __syncthreads();
+  f32x4 *image = reinterpret_cast<f32x4 *>(lds);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4)
+      image[w * IMAGE + (rb * 4 + x4) * 64 + lane] = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+  if (g == 0) {
+    stats[0][w][r] = m;
+    stats[1][w][r] = l;
+  }
+  __syncthreads();
+  if (w >= RB || r >= row.n_rows) return;
+  float top = stats[0][0][r], total = 0.f;      // wave w: columns 32 w .. of the joined rows
+#pragma unroll
+  for (int i = 1; i < 4; ++i) top = fmaxf(top, stats[0][i][r]);
+  f32x4 y[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float mi = stats[0][i][r], f = mi == top ? 1.f : fast_exp2((mi - top) * c);
+    total += stats[1][i][r] * f;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) y[x4] += image[i * IMAGE + (w * 4 + x4) * 64 + lane] * f;
+  }
+  if (a.n_split > 1) {
+    const int64_t at = (int64_t)item * 32 + r;
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) *reinterpret_cast<f32x4 *>(a.po + at * D + 32 * w + 8 * x4 + 4 * g) = y[x4];
+    if (w == 0 && g == 0) {
+      a.pm[at] = top;
+      a.pl[at] = total;
+    }
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int x4 = 0; x4 < 4; ++x4) {
+    char *to = a.out.p + (row.h * a.out.sh + row.token * a.out.sn + 32 * w + 8 * x4 + 4 * g) * (F32 ? 4 : 2);
+    if constexpr (F32) *reinterpret_cast<f32x4 *>(to) = y[x4] * inv;
+    else *reinterpret_cast<bf16x4 *>(to) = __builtin_convertvector(y[x4] * inv, bf16x4);
+  }
+  if (a.lse && w == 0 && g == 0) a.lse[(int64_t)row.token * a.p.H + row.h] = log_sum(top, total, a.scale);
+}
+
+// Sums of one step: logits sc of 32 slots and the running maximum, sum and output.
+template <int RB>
+static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &m, float &mc, float &l, f32x16 (&o)[RB]) {
+  float top = m;
+#pragma unroll
+  for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+  top = xhalf_max(top);
+  const float f = top == m ? 1.f : fast_exp2((m - top) * c);      // (neither may have seen a slot)
+  mc = top == -INFINITY ? 0.f : top * c;
+  m = top;
+  l *= f;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_few_kernel(FwdArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, REQUESTS = 2 * T::chunks(32);
+  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * SLOT];      // [wave][stage][k | v]; then [wave][register image]
+  static_assert(image_bytes<D>() <= 4 * 2 * SLOT, "the images fit the stages");
+  __shared__ float stats[2][4][32];
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / p.Hkv, hk = bh % p.Hkv;
+  const NewRows n(p, b);
+  if (n.n <= 0 || n.n * p.G > 32) return;
+  const int held = p.held(b);
+  const RowsOf row(p, n, held, hk, r);
+  const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
+  const int steps = (limit + 31) / 32;
+  int at = (int)((int64_t)range * steps / a.n_split) + w;
+  const int end = (int)((int64_t)(range + 1) * steps / a.n_split);
+  PageWalk walk(p, b, lane);
+  const char *kbase = a.k.p + hk * a.k.sh * 2, *vbase = a.v.p + hk * a.v.sh * 2;
+  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  char *mine = lds + w * (2 * SLOT);
+  auto request = [&](const Step &s, int stage) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int id = i ? s.id1 : s.id0, key = s.key + 16 * i, rows = id < 0 ? 0 : min(limit - key, 16), page = max(id, 0);
+      char *to = mine + stage * SLOT + i * T::bytes(16);
+      request_rows<D, 16, 1>(rows_rsrc<D>(kbase + slot_offset(p, a.k, page, key, 2), rows, ksn), ksn, to, 0, lane);
+      request_rows<D, 16, 1>(rows_rsrc<D>(vbase + slot_offset(p, a.v, page, key, 2), rows, vsn), vsn, to + TILE, 0, lane);
+    }
+  };
+  Step now{};
+  if (at < end) {
+    now = step_at(p, walk, 32 * at);
+    request(now, 0);
+  }
+  bf16x8 qf[KS];
+  const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+  const unsigned rows0 = T::rows_base(mine, lane), cols0 = T::cols_base(mine, lane);
+  const float c = a.scale_log2e;
+  float m = -INFINITY, mc = 0.f, l = 0.f;
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  for (int stage = 0; at < end; stage ^= 1) {
+    Step next{};
+    at += 4;
+    if (at < end) {
+      next = step_at(p, walk, 32 * at);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the last step's reads of that stage are done)
+      request(next, stage ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    const unsigned kt = rows0 + stage * SLOT, vt = cols0 + stage * SLOT;
+    f32x16 sc;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sc = mfma32(T::rows_at(kt, 0, ks), qf[ks], sc);
+    mask_step(sc, now, row.see, all_see, g);
+    follow(sc, c, m, mc, l, o);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 pr;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
+        l += pr[x];
+      }
+      const bf16x8 pb = __builtin_convertvector(pr, bf16x8);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb] = mfma32(T::cols_at(vt, rb, 16 * u, TILE), pb, o[rb]);
+    }
+    now = next;
+  }
+  join_waves<D, false>(a, o, m, l, lds, stats, blockIdx.x, row, w, lane);
+}
+
+// The same of fp32 tensors, which are split into pieces in registers: a slot's row of keys to a lane, eight rows of a column of the values.  Keys are asked for a
+// step ahead.
+template <int D>
+__global__ __launch_bounds__(256, 1) void paged_few_f32_kernel(FwdArgs a) {
+  constexpr int KS = D / 16, RB = D / 32;
+  __shared__ __attribute__((aligned(1024))) char lds[image_bytes<D>()];
+  __shared__ float stats[2][4][32];
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / p.Hkv, hk = bh % p.Hkv;
+  const NewRows n(p, b);
+  if (n.n <= 0 || n.n * p.G > 32) return;
+  const int held = p.held(b);
+  const RowsOf row(p, n, held, hk, r);
+  const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
+  const int steps = (limit + 31) / 32;
+  int at = (int)((int64_t)range * steps / a.n_split) + w;
+  const int end = (int)((int64_t)(range + 1) * steps / a.n_split);
+  PageWalk walk(p, b, lane);
+  const char *kbase = a.k.p + (hk * a.k.sh + 8 * g) * 4, *vbase = a.v.p + (hk * a.v.sh + r) * 4;
+  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+  f32x4 kr[KS][2];
+  auto request = [&](const Step &s) {      // (zeros for slots that nobody sees)
+    const int id = r < 16 ? s.id0 : s.id1;
+    const bool there = id >= 0 && s.key + r < limit;
+    const float *x = reinterpret_cast<const float *>(kbase + (there ? slot_offset(p, a.k, id, s.key + r, 4) : 0));
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) kr[ks][i] = there ? *reinterpret_cast<const f32x4 *>(x + 16 * ks + 4 * i) : none;
+  };
+  Step now{};
+  if (at < end) {
+    now = step_at(p, walk, 32 * at);
+    request(now);
+  }
+  bf16x8 qf[KS][3];
+  const float *qp = reinterpret_cast<const float *>(a.q.p) + row.h * a.q.sh + row.token * a.q.sn + 8 * g;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(qp + 16 * ks), *reinterpret_cast<const f32x4 *>(qp + 16 * ks + 4), qf[ks]);
+  const float c = a.scale_log2e;
+  float m = -INFINITY, mc = 0.f, l = 0.f;
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  while (at < end) {
+    float vr[2][RB][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int id = u ? now.id1 : now.id0;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int slot = now.key + crow(8 * u + x, g);
+        const bool there = id >= 0 && slot < limit;
+        const float *y = reinterpret_cast<const float *>(vbase + (there ? slot_offset(p, a.v, id, slot, 4) : 0));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) vr[u][rb][x] = there ? y[32 * rb] : 0.f;
+      }
+    }
+    f32x16 sc;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 kf[3];
+      split8_any(kr[ks][0], kr[ks][1], kf);
+      sc = mfma_split<3>(kf, qf[ks], sc);
+    }
+    Step next{};
+    at += 4;
+    if (at < end) {
+      next = step_at(p, walk, 32 * at);
+      request(next);
+    }
+    mask_step(sc, now, row.see, all_see, g);
+    follow(sc, c, m, mc, l, o);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 pr;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
+        l += pr[x];
+      }
+      bf16x8 pb[3];
+      split8<3>(pr, pb);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float(&v)[8] = vr[u][rb];
+        bf16x8 vf[3];
+        split8_any(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]}, vf);
+        o[rb] = mfma_split<3>(vf, pb, o[rb]);
+      }
+    }
+    now = next;
+  }
+  join_waves<D, true>(a, o, m, l, lds, stats, blockIdx.x, row, w, lane);
+}
+
+// ---- tiles of rows ---------------------------------------------------------------------------------------------------
+// Rows of T before a sequence, in tiles of 128 rows: the tiles of sequence b are those from here on, as many as it needs.
+static __device__ __forceinline__ int first_tile(const Paged &p, int b) { return p.offset(b) * p.G / 128 + b; }
+
+// Writes a 32-row tile held as C^T (the row is the lane's) times `f` through `stage` (this wave's own LDS) to the rows at to(r), those below `rows`.
+template <int D, bool F32, typename To>
+static __device__ __forceinline__ void store_tile(const f32x16 (&o)[D / 32], float f, char *stage, int rows, int lane, To to) {
+  constexpr int PASSES = F32 ? 2 : 1, DP = D / PASSES, ESZ = F32 ? 4 : 2, PITCH = DP * ESZ + 16, CPR = DP * ESZ / 16;
+  const int r = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+#pragma unroll
+    for (int b = 0; b < D / 32 / PASSES; ++b)
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const int col = 32 * b + 8 * x4 + 4 * g;
+        const f32x16 &t = o[pass * (D / 32 / PASSES) + b];
+        const f32x4 y = {t[4 * x4] * f, t[4 * x4 + 1] * f, t[4 * x4 + 2] * f, t[4 * x4 + 3] * f};
+        if constexpr (F32) *reinterpret_cast<f32x4 *>(stage + r * PITCH + col * 4) = y;
+        else *reinterpret_cast<bf16x4 *>(stage + r * PITCH + col * 2) = __builtin_convertvector(y, bf16x4);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (a wave's LDS instructions execute in order)
+#pragma unroll
+    for (int i = lane; i < 32 * CPR; i += 64) {
+      const int row = i / CPR, ch = i % CPR;
+      if (row < rows) *reinterpret_cast<f32x4 *>(to(row) + pass * DP * ESZ + ch * 16) = *reinterpret_cast<const f32x4 *>(stage + row * PITCH + ch * 16);
+    }
+    if (PASSES > 1) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// What a workgroup of tiles works on; n_rows = 0: nothing.
+struct TileOf {
+  int hk, range, b, row0, n_rows;      // row0: the tile's first row of the sequence
+  __device__ __forceinline__ TileOf(const Paged &p, const FwdArgs &a, unsigned item, int lane) {
+    range = item % a.n_split;
+    const int tile = item / a.n_split % a.tiles;
+    hk = item / a.n_split / a.tiles;
+    b = last_not_above(p.B, tile, lane, [&](int s) { return first_tile(p, s); });
+    const NewRows n(p, b);
+    row0 = (tile - first_tile(p, b)) * 128;
+    n_rows = n.n * p.G;
+    if (row0 < 0 || row0 >= n_rows || (a.leave_few && n_rows <= 32)) n_rows = 0;
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void store_partial(const FwdArgs &a, const f32x16 (&o)[D / 32], float m, float l, unsigned item, int w, int lane) {
+  const int r = lane & 31, g = lane >> 5;
+  const int64_t row = (int64_t)item * 128 + 32 * w + r;
+#pragma unroll
+  for (int rb = 0; rb < D / 32; ++rb)
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4)
+      *reinterpret_cast<f32x4 *>(a.po + row * D + 32 * rb + 8 * x4 + 4 * g) = f32x4{o[rb][4 * x4], o[rb][4 * x4 + 1], o[rb][4 * x4 + 2], o[rb][4 * x4 + 3]};
+  if (g == 0) {
+    a.pm[row] = m;
+    a.pl[row] = l;
+  }
+}
+
+// 32 slots to a step, in registers a step ahead and in one stage of LDS, where fp32 rows stand in three pieces.
+template <int D, bool F32>
+__global__ __launch_bounds__(256, 1) void paged_tile_kernel(FwdArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1, STAGE = T::bytes(32), ESZ = F32 ? 4 : 2, PER = 32 * T::PIECES / 256;
+  constexpr int LDS = 2 * NS * STAGE > 4 * store_bytes<D, F32>() ? 2 * NS * STAGE : 4 * store_bytes<D, F32>();
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];      // [k | v][piece][32 rows]
+  const unsigned item = xcd_item(blockIdx.x, a.share);
+  if (item >= a.items) return;
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const TileOf tile(p, a, item, lane);
+  if (tile.n_rows <= 0) return;
+  const int b = tile.b, hk = tile.hk;
+  const NewRows n(p, b);
+  const int held = p.held(b), R0 = tile.row0 + 32 * w;
+  const RowsOf row(p, n, held, hk, R0 + r);
+  const int last = min(tile.row0 + 127, tile.n_rows - 1) / p.G;      // the tile's last token, this wave's first
+  const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
+  const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
+  const int steps = (limit + 31) / 32;
+  int at = (int)((int64_t)tile.range * steps / a.n_split);
+  const int end = (int)((int64_t)(tile.range + 1) * steps / a.n_split);
+  PageWalk walk(p, b, lane);
+  const char *kbase = a.k.p + hk * a.k.sh * ESZ, *vbase = a.v.p + hk * a.v.sh * ESZ;
+  Row8 kr[PER], vr[PER];
+  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+  auto request = [&](const Step &s) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at_ = threadIdx.x + 256 * i, line = at_ / T::PIECES, piece = at_ % T::PIECES, id = line < 16 ? s.id0 : s.id1, slot = s.key + line;
+      kr[i] = vr[i] = Row8{none, none};
+      if (id >= 0 && slot < limit) {
+        kr[i] = load_row8<F32, true>(kbase + slot_offset(p, a.k, id, slot, ESZ), 0, 8 * piece, 8 * piece + 4);
+        vr[i] = load_row8<F32, true>(vbase + slot_offset(p, a.v, id, slot, ESZ), 0, 8 * piece, 8 * piece + 4);
+      }
+    }
+  };
+  auto deposit = [&]() {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at_ = threadIdx.x + 256 * i, line = at_ / T::PIECES, piece = at_ % T::PIECES;
+      char *to = lds + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
+      if constexpr (F32) {
+        bf16x8 x[3];
+        split8_any(kr[i].a, kr[i].b, x);
+#pragma unroll
+        for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = x[s];
+        split8_any(vr[i].a, vr[i].b, x);
+#pragma unroll
+        for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + (3 + s) * STAGE) = x[s];
+      } else {
+        *reinterpret_cast<bf16x8 *>(to) = __builtin_convertvector(__builtin_shufflevector(kr[i].a, kr[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+        *reinterpret_cast<bf16x8 *>(to + STAGE) = __builtin_convertvector(__builtin_shufflevector(vr[i].a, vr[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+      }
+    }
+  };
+  Step now{};
+  if (at < end) {
+    now = step_at(p, walk, 32 * at);
+    request(now);
+  }
+  bf16x8 qf[KS][NS];
+  const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * ESZ;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    if constexpr (F32) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
+    else qf[ks][0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+  }
+  const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
+  const float c = a.scale_log2e;
+  float m = -INFINITY, mc = 0.f, l = 0.f;
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  while (at < end) {
+    deposit();
+    __syncthreads();
+    Step next{};
+    ++at;
+    if (at < end) {
+      next = step_at(p, walk, 32 * at);
+      request(next);
+    }
+    f32x16 sc;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 kf[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kf[s] = T::rows_at(rows0, 0, ks, s * STAGE);
+      sc = mfma_split<NS>(kf, qf[ks], sc);
+    }
+    mask_step(sc, now, row.see, all_see, g);
+    follow(sc, c, m, mc, l, o);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x8 pr;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
+        l += pr[x];
+      }
+      bf16x8 pb[NS];
+      split8<NS>(pr, pb);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        bf16x8 vf[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) vf[s] = T::cols_at(cols0, rb, 16 * u, (NS + s) * STAGE);
+        o[rb] = mfma_split<NS>(vf, pb, o[rb]);
+      }
+    }
+    __syncthreads();                                  // every wave is done with the stage
+    now = next;
+  }
+  l = xhalf_sum(l);
+  if (a.n_split > 1) {
+    store_partial<D>(a, o, m, l, item, w, lane);
+    return;
+  }
+  if (a.lse && g == 0 && R0 + r < tile.n_rows) a.lse[(int64_t)row.token * p.H + row.h] = log_sum(m, l, a.scale);
+  store_tile<D, F32>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, F32>(), tile.n_rows - R0, lane, [&](int line) {
+    const int R = R0 + line, i = R / p.G;
+    return a.out.p + ((hk * p.G + R - i * p.G) * a.out.sh + (int64_t)(n.first + i) * a.out.sn) * ESZ;
+  });
+}
+
+// Joins the ranges of a row, at most 64: a wave to a row.  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
+template <int D, bool F32, int ROWS>
+__global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
+  constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, c4 = 4 * (lane % LPR);
+  const int line = __builtin_amdgcn_readfirstlane(blockIdx.x % (ROWS / 4) * 4 + (threadIdx.x >> 6)), group = blockIdx.x / (ROWS / 4);
+  int b, hk, R, n_rows;
+  if constexpr (ROWS == 32) {
+    b = group / p.Hkv;
+    hk = group % p.Hkv;
+    R = line;
+    n_rows = NewRows(p, b).n * p.G;
+    if (n_rows > 32) return;
+  } else {
+    const TileOf tile(p, a, (unsigned)group * a.n_split, lane);
+    b = tile.b;
+    hk = tile.hk;
+    R = tile.row0 + line;
+    n_rows = tile.n_rows;
+  }
+  if (R >= n_rows) return;
+  const bool has = lane < a.n_split;
+  const int64_t at0 = (int64_t)group * a.n_split * ROWS + line;      // range i: at0 + i ROWS
+  const float mi = has ? a.pm[at0 + (int64_t)lane * ROWS] : -INFINITY;
+  float m = mi;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  const float f = mi == m ? 1.f : fast_exp2((mi - m) * a.scale_log2e);
+  float l = has ? a.pl[at0 + (int64_t)lane * ROWS] * f : 0.f;      // (a range that saw nothing has 0, or the NaN that has to show)
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < a.n_split; i0 += 4 * AT_ONCE) {
+    f32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(i0 + u * AT_ONCE + lane / LPR, a.n_split - 1);
+      x[u] = *reinterpret_cast<const f32x4 *>(a.po + (at0 + (int64_t)i * ROWS) * D + c4);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * AT_ONCE + lane / LPR;
+      const float fi = __shfl(f, min(i, 63));
+      if (i < a.n_split) o += x[u] * fi;
+    }
+  }
+#pragma unroll
+  for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] += __shfl_xor(o[u], d);
+  if (lane >= LPR) return;
+  const int i = R / p.G, h = hk * p.G + R - i * p.G;
+  const int64_t token = p.offset(b) + i;
+  if (a.lse && lane == 0) a.lse[token * p.H + h] = log_sum(m, l, a.scale);
+  o *= l == 0.f ? 0.f : 1.f / l;
+  const int64_t to = h * a.out.sh + token * a.out.sn + c4;
+  if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out.p) + to) = o;
+  else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(a.out.p) + to) = __builtin_convertvector(o, bf16x4);
+}
+
+struct Part {
+  bool runs;
+  int n_split, groups;
+  size_t off_po, off_pm, off_pl;
+};
+struct FwdPlan {
+  Part few, tile;
+  size_t total;
+};
+
+FwdPlan plan_forward(const ha_paged_problem &p) {
+  FwdPlan f{};
+  const int64_t G = p.H / p.H_kv, steps = ((int64_t)p.max_pages * p.page + 31) / 32;
+  f.few.runs = p.T > 0 && p.max_new > 0 && (p.max_new * G <= 32 || p.q_offset);
+  f.tile.runs = p.max_new * G > 32;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round256(bytes);
+    return here;
+  };
+  auto split = [&](Part &part, int64_t groups, int64_t least, int rows) {
+    part.groups = (int)groups;
+    part.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({64, groups > 0 ? 256 / groups : 1, steps / least}));
+    if (part.runs && part.n_split > 1) {
+      const size_t n = (size_t)groups * part.n_split * rows;
+      part.off_po = take(n * p.d_head * 4);
+      part.off_pm = take(n * 4);
+      part.off_pl = take(n * 4);
+    }
+  };
+  split(f.few, (int64_t)p.B * p.H_kv, 4, 32);
+  split(f.tile, (p.T * G / 128 + p.B) * p.H_kv, 8, 128);
+  f.total = at;
+  return f;
+}
+
+template <int D, bool F32, int ROWS>
+hipError_t launch_join(const FwdArgs &a, int groups, hipStream_t st) {
+  paged_join_kernel<D, F32, ROWS><<<(unsigned)groups * (ROWS / 4), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <int D, bool F32>
+hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  auto part = [&](const Part &x) {
+    a.n_split = x.n_split;
+    a.po = reinterpret_cast<float *>(ws + x.off_po);
+    a.pm = reinterpret_cast<float *>(ws + x.off_pm);
+    a.pl = reinterpret_cast<float *>(ws + x.off_pl);
+  };
+  if (f.tile.runs) {
+    part(f.tile);
+    a.leave_few = f.few.runs;
+    a.tiles = f.tile.groups / a.p.Hkv;
+    a.items = (unsigned)f.tile.groups * f.tile.n_split;
+    a.share = xcd_share(a.items);
+    paged_tile_kernel<D, F32><<<8 * a.share, 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.n_split > 1 && (e = launch_join<D, F32, 128>(a, f.tile.groups, st)) != hipSuccess) return e;
+  }
+  if (f.few.runs) {
+    part(f.few);
+    const unsigned n = (unsigned)f.few.groups * f.few.n_split;
+    if constexpr (F32) paged_few_f32_kernel<D><<<n, 256, 0, st>>>(a);
+    else paged_few_kernel<D><<<n, 256, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.n_split > 1) e = launch_join<D, F32, 32>(a, f.few.groups, st);
+  }
+  return e;
+}
+
+}  // namespace
+}  // namespace ha
+
+using namespace ha;
+
+extern "C" ha_status hybrid_attn_paged_validate(const ha_paged_problem *p) { return check_paged(p); }
+
+extern "C" size_t hybrid_attn_paged_workspace_bytes(const ha_paged_problem *p) {
+  if (check_paged(p) != HA_OK) return 0;
+  return plan_forward(*p).total;
+}
+
+extern "C" ha_status hybrid_attn_paged_forward(const ha_paged_problem *p, const ha_view *q, const ha_view *k_pages, const ha_view *v_pages, const ha_view *out, float *lse,
+                                               void *workspace, size_t workspace_bytes, void *hip_stream) {
+  ha_status st = check_paged(p);
+  if (st != HA_OK) return st;
+  FwdArgs a{};
+  if ((st = check_packed(*p, q, p->H, false, a.q)) != HA_OK || (st = check_pool(*p, k_pages, false, a.k)) != HA_OK || (st = check_pool(*p, v_pages, false, a.v)) != HA_OK ||
+      (st = check_packed(*p, out, p->H, true, a.out)) != HA_OK)
+    return st;
+  if (reinterpret_cast<uintptr_t>(lse) & 3u) return HA_ERR_ALIGN;
+  if (p->T == 0) return HA_OK;
+  const FwdPlan f = plan_forward(*p);
+  if ((st = check_workspace(workspace, workspace_bytes, f.total)) != HA_OK) return st;
+  a.p = paged_of(*p);
+  a.lse = lse;
+  a.scale = p->softmax_scale;
+  a.scale_log2e = p->softmax_scale * kLog2e;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  char *ws = static_cast<char *>(workspace);
+  const bool f32 = p->dtype == HA_F32;
+  const hipError_t e = p->d_head == 128 ? (f32 ? launch_forward<128, true>(a, f, ws, stream) : launch_forward<128, false>(a, f, ws, stream))
+                                        : (f32 ? launch_forward<64, true>(a, f, ws, stream) : launch_forward<64, false>(a, f, ws, stream));
+  return e == hipSuccess ? HA_OK : device_error(e);
+}

@@ -125,8 +125,8 @@ def _lib():
         lib.hybrid_attn_param_update.argtypes = [ctypes.POINTER(ha_optimizer), ctypes.c_size_t, vp, vp, vp, vp, vp,
                                                  ctypes.c_int32, vp]
         lib.hybrid_attn_param_update.restype = ctypes.c_int
-        from . import block_sparse, optim
-        for name, arguments, result in (*block_sparse.SIGNATURES, *optim.SIGNATURES):
+        from . import block_sparse, optim, paged, rotary
+        for name, arguments, result in (*block_sparse.SIGNATURES, *optim.SIGNATURES, *rotary.SIGNATURES, *paged.SIGNATURES):
             function = getattr(lib, name)
             function.argtypes, function.restype = arguments, result
         lib.hybrid_attn_abi_version.argtypes = []
@@ -690,13 +690,20 @@ def device_inputs(w, device="cuda"):
     return q, k, v, fm(mq), fm(mk)
 
 
-# The calls of include/hybrid_attn_sparse.h and include/hybrid_attn_optim.h, under the names that their modules (which import this one) give them.
+# The calls of include/hybrid_attn_sparse.h, hybrid_attn_optim.h, hybrid_attn_rotary.h and hybrid_attn_paged.h, under the names that their modules (which import this one)
+# give them.
 _ELSEWHERE = {
     "block_sparse": ("ha_sparse_problem", "ha_view", "make_sparse_problem", "hybrid_attn_sparse_validate", "hybrid_attn_key_means",
                      "hybrid_attn_select_workspace_bytes", "hybrid_attn_select_blocks", "hybrid_attn_sparse_workspace_bytes", "hybrid_attn_sparse_forward",
                      "hybrid_attn_sparse_grad_workspace_bytes", "hybrid_attn_sparse_grad"),
     "optim": ("ha_tensor", "ha_param", "TensorList", "ParamList", "hybrid_attn_grad_norm_workspace_bytes", "hybrid_attn_grad_norm", "hybrid_attn_grad_clip",
               "hybrid_attn_param_update_many"),
+    "rotary": ("ha_rotary", "ha_rows_problem", "Rotary", "hybrid_attn_rotary_frequencies", "hybrid_attn_rotary_grid", "hybrid_attn_grid_positions",
+               "hybrid_attn_rotary_validate", "hybrid_attn_rotate", "hybrid_attn_rotate_grad", "hybrid_attn_norm_rotate",
+               "hybrid_attn_norm_rotate_grad_workspace_bytes", "hybrid_attn_norm_rotate_grad"),
+    "paged": ("ha_paged_problem", "make_paged_problem", "hybrid_attn_paged_validate", "hybrid_attn_paged_append", "hybrid_attn_paged_workspace_bytes",
+              "hybrid_attn_paged_forward", "hybrid_attn_paged_weights_workspace_bytes", "hybrid_attn_paged_weights", "hybrid_attn_paged_evict_workspace_bytes",
+              "hybrid_attn_paged_evict"),
 }
 
 
