@@ -13,6 +13,7 @@
 #include "ha_paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ha {
 
@@ -412,11 +413,197 @@ __device__ __forceinline__ void store_partial(const FwdArgs &a, const f32x16 (&o
   }
 }
 
-// 32 slots to a step, in registers a step ahead and in one stage of LDS, where fp32 rows stand in three pieces.
-template <int D, bool F32>
-__global__ __launch_bounds__(256, 1) void paged_tile_kernel(FwdArgs a) {
+// bf16: 32 slots to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next slots under the exponentials of its own,
+// then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work of one wave at the same time, and of two
+// with two workgroups to a CU.
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1, STAGE = T::bytes(32), ESZ = F32 ? 4 : 2, PER = 32 * T::PIECES / 256;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOTS = 4, AHEAD = 3, CHUNKS = T::chunks(32) / 4, REQUESTS = 2 * CHUNKS;
+  constexpr auto k_at = [](int step) { return step % SLOTS * 2 * TILE; };
+  constexpr auto v_at = [](int step) { return step % SLOTS * 2 * TILE + TILE; };
+  __shared__ __attribute__((aligned(1024))) char lds[SLOTS * 2 * TILE];
+  static_assert(4 * store_bytes<D, false>() <= SLOTS * 2 * TILE, "the stores' staging areas fit");
+  const unsigned item = xcd_item(blockIdx.x, a.share);
+  if (item >= a.items) return;
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const TileOf tile(p, a, item, lane);
+  if (tile.n_rows <= 0) return;
+  const int b = tile.b, hk = tile.hk;
+  const NewRows n(p, b);
+  const int held = p.held(b), R0 = tile.row0 + 32 * w;
+  const RowsOf row(p, n, held, hk, R0 + r);
+  const int last = min(tile.row0 + 127, tile.n_rows - 1) / p.G;      // the tile's last token
+  const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
+  const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
+  const int steps = (limit + 31) / 32, end = (int)((int64_t)(tile.range + 1) * steps / a.n_split);
+  int at = (int)((int64_t)tile.range * steps / a.n_split);
+  PageWalk walk(p, b, lane);
+  const char *kbase = a.k.p + hk * a.k.sh * 2, *vbase = a.v.p + hk * a.v.sh * 2;
+  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  auto next_step = [&]() {
+    Step s{-1, -1, -1};
+    if (at < end) s = step_at(p, walk, 32 * at);
+    ++at;
+    return s;
+  };
+  // (behind the last step zeros are requested: every step has as many requests, which is what the waits count)
+  int line[CHUNKS], off_k[CHUNKS], off_v[CHUNKS];      // a chunk's place: its half's 16 slots, this lane's row and piece
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int first = (4 * i + w) * T::ROWS_PER_CHUNK, row_ = first + lane / T::PIECES;
+    line[i] = first / 16;
+    off_k[i] = (row_ % 16) * ksn + (((lane % T::PIECES) ^ T::swz(row_)) << 4);
+    off_v[i] = (row_ % 16) * vsn + (((lane % T::PIECES) ^ T::swz(row_)) << 4);
+  }
+  auto request = [&](const Step &s, int step) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int id = line[i] ? s.id1 : s.id0, key = max(s.key, 0) + 16 * line[i], rows = id < 0 ? 0 : min(limit - key, 16), page = max(id, 0);
+      const unsigned to = __builtin_amdgcn_readfirstlane(lds_offset(lds) + k_at(step) + (4 * i + w) * 1024);
+      const i32x4 kr = rows_rsrc<D>(kbase + slot_offset(p, a.k, page, key, 2), rows, ksn), vr = rows_rsrc<D>(vbase + slot_offset(p, a.v, page, key, 2), rows, vsn);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off_k[i]), "s"(kr) : "memory");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + TILE), "v"(off_v[i]), "s"(vr) : "memory");
+    }
+  };
+  Step s0 = next_step(), s1 = next_step(), s2 = next_step();
+  const float c = a.scale_log2e;
+  float m = -INFINITY, top = -INFINITY, l = 0.f;      // what the sums are expressed against, the largest logit and the sum of weights (this lane's slots)
+  f32x16 o[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  if (s0.key >= 0) {
+    request(s0, 0);
+    request(s1, 1);
+    request(s2, 2);
+    bf16x8 qf[KS];
+    const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+    // addresses of all operands of a step; the slot goes into the instruction
+    unsigned rows[KS], cols[RB][2];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) rows[ks] = T::rows_base(lds, lane) ^ (ks << 5);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) cols[rb][i] = T::cols_base(lds, lane) ^ (rb << 6) ^ (i << 5);
+    auto read_k = [&](int step, int ks) { return T::row_piece(rows[ks] + k_at(step)); };
+    auto read_v = [&](int step, int rb, int u) {
+      const int at_ = v_at(step) + 16 * u * T::PITCH;
+      return T::col_piece(cols[rb][0] + at_, cols[rb][1] + at_ + 8 * T::PITCH);
+    };
+    const float gap = 8.f / c;
+    float mc = 0.f;
+    // What has been summed follows the maximum when some row's has moved by 8 in the exponent (weights stay below 2^8).
+    auto mask = [&](f32x16 &sc, const Step &s) {
+      if (s.key < 0) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = -INFINITY;
+      } else {
+        mask_step(sc, s, row.see, all_see, g);
+      }
+    };
+    auto follow_far = [&](const f32x16 &sc) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+      if (__any(top - m > gap)) {
+        top = xhalf_max(top);
+        const float f = top == m ? 1.f : fast_exp2((m - top) * c);      // (neither may have seen a slot)
+        l *= f;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[rb][x] *= f;
+        m = top;
+        mc = m == -INFINITY ? 0.f : m * c;
+      }
+    };
+    const f32x16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    f32x16 s_a, s_b;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * REQUESTS) : "memory");
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s_a = mfma32(read_k(0, ks), qf[ks], ks == 0 ? none : s_a);
+    mask(s_a, s0);
+    follow_far(s_a);
+    auto step = [&](f32x16 &sc, f32x16 &sn, auto now_c) {
+      constexpr int now = decltype(now_c)::value, next = now + 1;
+      // the next slots have landed, and no wave reads those of the step before any more
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * REQUESTS) : "memory");
+      __syncthreads();
+      bf16x8 kf[KS], vf[2 * RB], pb[2];
+      kf[0] = read_k(next, 0);
+      kf[1] = read_k(next, 1);
+      const Step further = next_step();
+      request(further, now + AHEAD);
+      constexpr int PER = 16 / KS;         // logits to a product: 2 at d = 128, 4 at d = 64
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 2 < KS) kf[ks + 2] = read_k(next, ks + 2);
+        else vf[ks + 2 - KS] = read_v(now, ks + 2 - KS, 0);
+        HA_FENCE();
+        sn = mfma32(kf[ks], qf[ks], ks == 0 ? none : sn);
+#pragma unroll
+        for (int y = 0; y < PER; ++y) {
+          const int x = ks * PER + y;
+          sc[x] = fast_exp2(__builtin_fmaf(sc[x], c, -mc));
+          l += sc[x];
+          if (x % 8 == 7) {
+            f32x8 pr;
+#pragma unroll
+            for (int z = 0; z < 8; ++z) pr[z] = sc[x - 7 + z];
+            pb[x / 8] = __builtin_convertvector(pr, bf16x8);
+          }
+        }
+        HA_FENCE();
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * RB; ++i) {   // i = RB u + rb
+        if (i + 2 < 2 * RB) vf[i + 2] = read_v(now, (i + 2) % RB, (i + 2) / RB);
+        HA_FENCE();
+        o[i % RB] = mfma32(vf[i], pb[i / RB], o[i % RB]);
+      }
+      mask(sn, s1);
+      follow_far(sn);
+      s0 = s1;
+      s1 = s2;
+      s2 = further;
+    };
+    while (true) {
+      step(s_a, s_b, std::integral_constant<int, 0>{});
+      if (s0.key < 0) break;
+      step(s_b, s_a, std::integral_constant<int, 1>{});
+      if (s0.key < 0) break;
+      step(s_a, s_b, std::integral_constant<int, 2>{});
+      if (s0.key < 0) break;
+      step(s_b, s_a, std::integral_constant<int, 3>{});
+      if (s0.key < 0) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  l = xhalf_sum(l);
+  if (a.n_split > 1) {
+    store_partial<D>(a, o, m, l, item, w, lane);
+    return;
+  }
+  if (a.lse && g == 0 && R0 + r < tile.n_rows) a.lse[(int64_t)row.token * p.H + row.h] = log_sum(m, l, a.scale);
+  __syncthreads();                                    // the slots become the staging area of the stores
+  store_tile<D, false>(o, l == 0.f ? 0.f : 1.f / l, lds + w * store_bytes<D, false>(), tile.n_rows - R0, lane, [&](int line_) {
+    const int R = R0 + line_, i = R / p.G;
+    return a.out.p + ((hk * p.G + R - i * p.G) * a.out.sh + (int64_t)(n.first + i) * a.out.sn) * 2;
+  });
+}
+
+// fp32: 32 slots to a step, in registers a step ahead and in one stage of LDS in three pieces.
+template <int D>
+__global__ __launch_bounds__(256, 1) void paged_tile_f32_kernel(FwdArgs a) {
+  constexpr bool F32 = true;
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, RB = D / 32, NS = 3, STAGE = T::bytes(32), ESZ = 4, PER = 32 * T::PIECES / 256;
   constexpr int LDS = 2 * NS * STAGE > 4 * store_bytes<D, F32>() ? 2 * NS * STAGE : 4 * store_bytes<D, F32>();
   __shared__ __attribute__((aligned(1024))) char lds[LDS];      // [k | v][piece][32 rows]
   const unsigned item = xcd_item(blockIdx.x, a.share);
@@ -455,18 +642,13 @@ __global__ __launch_bounds__(256, 1) void paged_tile_kernel(FwdArgs a) {
     for (int i = 0; i < PER; ++i) {
       const int at_ = threadIdx.x + 256 * i, line = at_ / T::PIECES, piece = at_ % T::PIECES;
       char *to = lds + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
-      if constexpr (F32) {
-        bf16x8 x[3];
-        split8_any(kr[i].a, kr[i].b, x);
+      bf16x8 x[3];
+      split8_any(kr[i].a, kr[i].b, x);
 #pragma unroll
-        for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = x[s];
-        split8_any(vr[i].a, vr[i].b, x);
+      for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = x[s];
+      split8_any(vr[i].a, vr[i].b, x);
 #pragma unroll
-        for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + (3 + s) * STAGE) = x[s];
-      } else {
-        *reinterpret_cast<bf16x8 *>(to) = __builtin_convertvector(__builtin_shufflevector(kr[i].a, kr[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
-        *reinterpret_cast<bf16x8 *>(to + STAGE) = __builtin_convertvector(__builtin_shufflevector(vr[i].a, vr[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
-      }
+      for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + (3 + s) * STAGE) = x[s];
     }
   };
   Step now{};
@@ -477,10 +659,7 @@ __global__ __launch_bounds__(256, 1) void paged_tile_kernel(FwdArgs a) {
   bf16x8 qf[KS][NS];
   const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * ESZ;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    if constexpr (F32) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
-    else qf[ks][0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
-  }
+  for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
   const float c = a.scale_log2e;
   float m = -INFINITY, mc = 0.f, l = 0.f;
@@ -625,9 +804,12 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     at += round256(bytes);
     return here;
   };
+  // Parts until every CU has a workgroup that keeps `least` steps of 32 slots; tiles: two workgroups where each keeps 64.
   auto split = [&](Part &part, int64_t groups, int64_t least, int rows) {
     part.groups = (int)groups;
-    part.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({64, groups > 0 ? 256 / groups : 1, steps / least}));
+    int64_t parts = groups > 0 ? std::min(256 / groups, steps / least) : 1;
+    if (rows == 128 && groups > 0) parts = std::max(parts, std::min(512 / groups, steps / 64));
+    part.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
     if (part.runs && part.n_split > 1) {
       const size_t n = (size_t)groups * part.n_split * rows;
       part.off_po = take(n * p.d_head * 4);
@@ -661,7 +843,8 @@ hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st)
     a.tiles = f.tile.groups / a.p.Hkv;
     a.items = (unsigned)f.tile.groups * f.tile.n_split;
     a.share = xcd_share(a.items);
-    paged_tile_kernel<D, F32><<<8 * a.share, 256, 0, st>>>(a);
+    if constexpr (F32) paged_tile_f32_kernel<D><<<8 * a.share, 256, 0, st>>>(a);
+    else paged_tile_kernel<D><<<8 * a.share, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.n_split > 1 && (e = launch_join<D, F32, 128>(a, f.tile.groups, st)) != hipSuccess) return e;
   }
