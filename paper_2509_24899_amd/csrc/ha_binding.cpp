@@ -16,6 +16,7 @@
 #include <limits>
 
 #include "../../include/hybrid_attn_optim.h"
+#include "../../include/hybrid_attn_paged.h"
 #include "../../include/hybrid_attn_sparse.h"
 
 namespace {
@@ -243,12 +244,15 @@ PyObject *bind(PyObject *, PyObject *args) {
 }  // namespace
 
 #include "ha_binding_calls.h"
+#include "ha_binding_rows.h"
 
 namespace {
 
 #define HA_FAST(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HA_FAST(key_means), HA_FAST(select_blocks), HA_FAST(sparse_forward), HA_FAST(sparse_grad), HA_FAST(grad_norm), HA_FAST(grad_clip),
                          HA_FAST(update_many), HA_FAST(describe_tensors), HA_FAST(describe_params), {"bind_calls", bind_calls, METH_VARARGS, nullptr},
+                         HA_FAST(rotate), HA_FAST(norm_rotate), HA_FAST(norm_rotate_grad), HA_FAST(paged_append), HA_FAST(paged_forward), HA_FAST(paged_weights),
+                         HA_FAST(paged_evict), {"bind_rows", bind_rows, METH_VARARGS, nullptr},
                          {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL, nullptr},
                          {"param_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(param_update)), METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
@@ -276,6 +280,13 @@ PyMODINIT_FUNC PyInit_hybridattn_binding() {
                                       static_cast<Py_ssize_t>(sizeof(ha_tensor)), static_cast<Py_ssize_t>(sizeof(ha_param)));
   if (!calls_abi || PyModule_AddObject(m, "calls_abi", calls_abi) < 0) {
     Py_XDECREF(calls_abi);
+    Py_DECREF(m);
+    return nullptr;
+  }
+  PyObject *rows_abi = Py_BuildValue("(nnn)", static_cast<Py_ssize_t>(sizeof(ha_rotary)), static_cast<Py_ssize_t>(sizeof(ha_rows_problem)),
+                                     static_cast<Py_ssize_t>(sizeof(ha_paged_problem)));
+  if (!rows_abi || PyModule_AddObject(m, "rows_abi", rows_abi) < 0) {
+    Py_XDECREF(rows_abi);
     Py_DECREF(m);
     return nullptr;
   }

@@ -443,7 +443,6 @@ PyObject *update_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
     Py_RETURN_NONE;
   }
 }
-#undef HA_CALL
 
 // describe_tensors(list, address of as many ha_tensor) -> (device index, sizes), or None
 PyObject *describe_tensors(PyObject *, PyObject *const *args, Py_ssize_t n) {

@@ -1,7 +1,7 @@
 // Paged caches, gfx950: storing new tokens (normed and rotated on the way), and eviction of the slots that have had the least weight.
 //
 // Storing is one pass over the new rows, bound by memory, or by a few dependent loads where they are few.  Eviction finds, for each sequence and key head, the
-// weight of the last slot that stays, eight bits at a time; then the slots that stay, in order; then copies their rows, which is what takes long.
+// weight of the last slot that stays, and lists the slots that stay in order; then a second kernel copies their rows, which is what takes long.
 #include <cmath>
 
 #include "ha_paged.h"
@@ -102,148 +102,187 @@ static __device__ __forceinline__ unsigned ordered(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// One sequence and key head to a workgroup of 1024.
+// The slots that stay, of one sequence and key head to a workgroup of 1024.  The weights of 65536 slots are held in registers (more are read anew in every pass), slot
+// j0 + 1024 i + t in register i of thread t.  Three passes over 11, 11 and 10 bits of their order count how many have each digit, from the top, until the last weight that
+// stays is known; its ties stay from the lowest slot on.
 __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
-  constexpr int PER = 8;      // consecutive slots of a thread
-  __shared__ unsigned hist[256];
+  constexpr int PER = 64, BINS = 2048, CHUNK = PER * 1024;
+  __shared__ unsigned hist[BINS];
+  __shared__ unsigned wave_sums[16];
   __shared__ unsigned found[2];               // the digit, what is still to be taken of it
-  __shared__ int wave_sums[2][16];
+  __shared__ unsigned stays[PER][16], ties[PER][16];      // [register][wave]: how many; then how many ahead of them
   const Paged &p = a.p;
   const int bh = blockIdx.x, b = bh / p.Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int held = p.held(b), capacity = p.capacity();
-  const float *x = a.weights + (int64_t)bh * capacity;
-  float *out = a.weights_out + (int64_t)bh * capacity;
+  const int held = p.held(b);
+  const float *x = a.weights + (int64_t)bh * p.capacity();
   int32_t *kept = a.kept + (int64_t)bh * a.keep;
-  const bool all = held <= a.keep;
+  if (bh % p.Hkv == 0 && threadIdx.x == 0) a.len_out[b] = min(held, a.keep);
+  for (int j = held + threadIdx.x; j < a.keep; j += 1024) kept[j] = -1;
+  if (held <= a.keep) {
+    for (int j = threadIdx.x; j < held; j += 1024) kept[j] = j;
+    return;
+  }
   const int lo = a.first, hi = held - a.last, wanted = a.keep - a.first - a.last;      // candidates lo .. hi - 1, how many of them stay
+  unsigned u[PER];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (j0 + 1024 * i >= held) break;
+      const int j = j0 + 1024 * i + threadIdx.x;
+      u[i] = j < held ? ordered(x[j]) : 0;
+    }
+  };
+  const bool once = held <= CHUNK;
+  if (once) load(0);
+  // the sum over the threads ahead of this one, and over all
+  auto prefix_sum = [&](unsigned n, unsigned &total) {
+    unsigned upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned y = __shfl_up(upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 63) wave_sums[w] = upto;
+    __syncthreads();
+    unsigned before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      before += i < w ? wave_sums[i] : 0;
+      total += wave_sums[i];
+    }
+    __syncthreads();
+    return before + upto - n;
+  };
   unsigned prefix = 0, need = wanted;         // the leading digits of the last weight that stays, and how many stay of those that share them
-  if (!all && wanted > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+  if (wanted > 0) {
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      const unsigned above = pass == 0 ? 0 : ~0u << (shift + bits);      // digits that are known
+      hist[2 * threadIdx.x] = hist[2 * threadIdx.x + 1] = 0;
       __syncthreads();
-      for (int j = lo + threadIdx.x; j < hi; j += 1024) {
-        const unsigned u = ordered(x[j]);
-        if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(u >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (w == 0) {           // from the largest digit down: lane l has digits 255 - 4 l ..
-        unsigned mine[4], sum = 0;
+      for (int j0 = 0; j0 < held; j0 += CHUNK) {
+        if (!once) load(j0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += mine[i] = hist[255 - 4 * lane - i];
-        unsigned upto = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const unsigned y = __shfl_up(upto, d);
-          if (lane >= d) upto += y;
-        }
-        unsigned above = upto - sum;
-        if (above < need && need <= upto) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (above < need && need <= above + mine[i]) {
-              found[0] = 255 - 4 * lane - i;
-              found[1] = need - above;
-            }
-            above += mine[i];
+        for (int i = 0; i < PER; ++i) {
+          if (j0 + 1024 * i >= held) break;
+          const int j = j0 + 1024 * i + threadIdx.x;
+          const bool counts = j >= lo && j < hi && (u[i] & above) == prefix;
+          const unsigned digit = (u[i] >> shift) & ((1u << bits) - 1);
+          const uint64_t who = __ballot(counts);
+          if (who == 0) continue;
+          // (equal weights, of slots that nothing has looked at yet for instance, would queue up at one place)
+          const int first = __ffsll((long long)who) - 1;
+          if (__ballot(counts && digit == __builtin_amdgcn_readlane(digit, first)) == who) {
+            if (lane == first) atomicAdd(&hist[digit], (unsigned)__popcll(who));
+          } else if (counts) {
+            atomicAdd(&hist[digit], 1u);
           }
         }
       }
       __syncthreads();
+      // from the largest digit down: thread t has digits 2047 - 2 t and 2046 - 2 t
+      const unsigned n0 = hist[BINS - 1 - 2 * threadIdx.x], n1 = hist[BINS - 2 - 2 * threadIdx.x];
+      unsigned total;
+      const unsigned before = prefix_sum(n0 + n1, total);
+      if (before < need && need <= before + n0 + n1) {
+        const bool second = need > before + n0;
+        found[0] = BINS - 1 - 2 * threadIdx.x - second;
+        found[1] = need - before - (second ? n0 : 0);
+      }
+      __syncthreads();
       prefix |= found[0] << shift;
       need = found[1];
-      __syncthreads();
     }
   }
-  // slots that stay, in order: all above the last weight, and the first `need` of those that equal it
-  int base = 0, equal_base = 0;
-  for (int j0 = 0; j0 < held; j0 += 1024 * PER) {
-    const int j = j0 + threadIdx.x * PER;
-    unsigned stays = 0, ties = 0;
-    float v[PER];
+  // slots that stay, in order: outside of the candidates, above the last weight, and the first `need` of those that equal it
+  unsigned base = 0, tie_base = 0;
+  for (int j0 = 0; j0 < held; j0 += CHUNK) {
+    if (!once) load(j0);
+    // 0: goes, 1: stays, 2: a tie
+    auto kind = [&](int i) {
+      const int j = j0 + 1024 * i + threadIdx.x;
+      if (j >= held) return 0;
+      if (j < lo || j >= hi) return 1;
+      return wanted == 0 || u[i] < prefix ? 0 : u[i] > prefix ? 1 : 2;
+    };
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      v[i] = 0.f;
-      if (j + i < held) {
-        v[i] = x[j + i];
-        const unsigned u = ordered(v[i]);
-        const bool middle = !all && j + i >= lo && j + i < hi;
-        if (!middle || (wanted > 0 && u > prefix)) stays |= 1u << i;
-        else if (wanted > 0 && u == prefix) ties |= 1u << i;
+      unsigned s = 0, t = 0;
+      if (j0 + 1024 * i < held) {
+        const int k = kind(i);
+        s = __popcll(__ballot(k == 1));
+        t = __popcll(__ballot(k == 2));
+      }
+      if (lane == 0) {
+        stays[i][w] = s;
+        ties[i][w] = t;
       }
     }
-    auto prefix_sum = [&](int n, int which, int &total) {      // of the threads ahead of this one
-      int upto = n;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(upto, d);
-        if (lane >= d) upto += y;
-      }
-      if (lane == 63) wave_sums[which][w] = upto;
-      __syncthreads();
-      int before = 0;
-      total = 0;
-      for (int i = 0; i < 16; ++i) {
-        if (i < w) before += wave_sums[which][i];
-        total += wave_sums[which][i];
-      }
-      return before + upto - n;
-    };
-    int n_ties, n_stay;
-    int tie = equal_base + prefix_sum(__popc(ties), 0, n_ties);
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (ties >> i & 1) {
-        if (tie < (int)need) stays |= 1u << i;
-        ++tie;
-      }
-    int at = base + prefix_sum(__popc(stays), 1, n_stay);
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (stays >> i & 1) {
-        kept[at] = j + i;
-        out[at] = v[i];
-        ++at;
-      }
-    base += n_stay;
-    equal_base += n_ties;
     __syncthreads();
+    // entry t of the register-major list: ties ahead of it say how many of its own stay
+    unsigned *all_stay = &stays[0][0], *all_ties = &ties[0][0], total_ties, total;
+    const unsigned my_ties = all_ties[threadIdx.x], ties_before = tie_base + prefix_sum(my_ties, total_ties);
+    const unsigned mine = all_stay[threadIdx.x] + min(ties_before < need ? need - ties_before : 0u, my_ties);
+    const unsigned before = base + prefix_sum(mine, total);
+    all_ties[threadIdx.x] = ties_before;
+    all_stay[threadIdx.x] = before;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (j0 + 1024 * i >= held) break;
+      const int k = kind(i);
+      const uint64_t below = ((uint64_t)1 << lane) - 1, tied = __ballot(k == 2);
+      const bool stay = k == 1 || (k == 2 && ties[i][w] + __popcll(tied & below) < need);
+      const uint64_t all = __ballot(stay);
+      if (stay) kept[stays[i][w] + __popcll(all & below)] = j0 + 1024 * i + threadIdx.x;
+    }
+    base += total;
+    tie_base += total_ties;
   }
-  for (int j = base + threadIdx.x; j < a.keep; j += 1024) kept[j] = -1;
-  for (int j = base + threadIdx.x; j < capacity; j += 1024) out[j] = 0.f;
-  if (bh % p.Hkv == 0 && threadIdx.x == 0) a.len_out[b] = base;
 }
 
-// Copies the rows of the slots that stay: 64 of them to a workgroup, 16 bytes to a thread.
+// Copies the rows and weights of the slots that stay, 64 of them to a workgroup, 16 bytes of a row to a thread.  The workgroups behind them clear the weights behind.
 template <int ROW>            // bytes of a row
 __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int esz) {
-  constexpr int TPR = ROW / 16, RPP = 256 / TPR, U = 64 / RPP;
+  constexpr int TPR = ROW / 16, RPP = 256 / TPR, U = RPP >= 16 ? 64 / RPP : 4;
   const Paged &p = a.p;
-  const int bh = blockIdx.x / a.row_blocks, b = bh / p.Hkv, hk = bh % p.Hkv, i0 = (blockIdx.x % a.row_blocks) * 64;
+  const int bh = blockIdx.x / a.row_blocks, b = bh / p.Hkv, hk = bh % p.Hkv, i0 = (blockIdx.x % a.row_blocks) * 64, capacity = p.capacity();
+  const int stay = min(p.held(b), a.keep);
+  if (threadIdx.x < 64) {
+    const int i = i0 + threadIdx.x;
+    if (i < capacity) a.weights_out[(int64_t)bh * capacity + i] = i < stay ? a.weights[(int64_t)bh * capacity + a.kept[(int64_t)bh * a.keep + i]] : 0.f;
+  }
+  if (i0 >= stay) return;
   const int c = threadIdx.x % TPR * 16;
-  f32x4 k[U], v[U];
-  int to[U];                  // page that the row goes to, or -1
+#pragma unroll 1
+  for (int i1 = i0 + threadIdx.x / TPR; i1 < min(i0 + 64, stay); i1 += U * RPP) {
+    f32x4 k[U], v[U];
+    int to[U];                // page that the row goes to, or -1
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int i = i0 + u * RPP + threadIdx.x / TPR;
-    const int slot = i < a.keep ? a.kept[(int64_t)bh * a.keep + i] : -1;
-    to[u] = -1;
-    k[u] = v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0) {
-      const int id = p.page_of(b, slot), out = a.out_table[(int64_t)b * a.out_pages + (i >> p.page_log2)];
-      if ((unsigned)out < (unsigned)p.n_pages) to[u] = out;
-      if (id >= 0) {
-        const int64_t row = slot & (p.page - 1);
-        k[u] = *reinterpret_cast<const f32x4 *>(a.k.p + (id * a.k.sb + hk * a.k.sh + row * a.k.sn) * esz + c);
-        v[u] = *reinterpret_cast<const f32x4 *>(a.v.p + (id * a.v.sb + hk * a.v.sh + row * a.v.sn) * esz + c);
+    for (int u = 0; u < U; ++u) {
+      const int i = i1 + u * RPP;
+      to[u] = -1;
+      k[u] = v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i < stay) {
+        const int slot = a.kept[(int64_t)bh * a.keep + i];
+        const int id = p.page_of(b, slot), out = a.out_table[(int64_t)b * a.out_pages + (i >> p.page_log2)];
+        if ((unsigned)out < (unsigned)p.n_pages) to[u] = out;
+        if (id >= 0) {
+          const int64_t row = slot & (p.page - 1);
+          k[u] = *reinterpret_cast<const f32x4 *>(a.k.p + (id * a.k.sb + hk * a.k.sh + row * a.k.sn) * esz + c);
+          v[u] = *reinterpret_cast<const f32x4 *>(a.v.p + (id * a.v.sb + hk * a.v.sh + row * a.v.sn) * esz + c);
+        }
       }
     }
-  }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t row = (i0 + u * RPP + threadIdx.x / TPR) & (p.page - 1);
-    if (to[u] >= 0) {
-      *reinterpret_cast<f32x4 *>(a.k.p + (to[u] * a.k.sb + hk * a.k.sh + row * a.k.sn) * esz + c) = k[u];
-      *reinterpret_cast<f32x4 *>(a.v.p + (to[u] * a.v.sb + hk * a.v.sh + row * a.v.sn) * esz + c) = v[u];
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = (i1 + u * RPP) & (p.page - 1);
+      if (to[u] >= 0) {
+        *reinterpret_cast<f32x4 *>(a.k.p + (to[u] * a.k.sb + hk * a.k.sh + row * a.k.sn) * esz + c) = k[u];
+        *reinterpret_cast<f32x4 *>(a.v.p + (to[u] * a.v.sb + hk * a.v.sh + row * a.v.sn) * esz + c) = v[u];
+      }
     }
   }
 }
@@ -302,7 +341,7 @@ extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t 
   if (st != HA_OK) return st;
   EvictArgs a{};
   if (keep < 1 || keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > keep || out_pages < 0) return HA_ERR_SHAPE;
-  const int64_t slots = (int64_t)p->max_pages * p->page, row_blocks = ((int64_t)keep + 63) / 64;
+  const int64_t slots = (int64_t)p->max_pages * p->page, row_blocks = (slots + 63) / 64;      // (of all slots: the weights behind those that stay are cleared)
   if ((int64_t)out_pages * p->page < keep) return HA_ERR_SHAPE;
   if (keep > (1 << 30) || (int64_t)p->B * p->H_kv * row_blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
   if ((st = check_pool(*p, k_pages, true, a.k)) != HA_OK || (st = check_pool(*p, v_pages, true, a.v)) != HA_OK) return st;
@@ -327,6 +366,7 @@ extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t 
   evict_choose_kernel<<<p->B * p->H_kv, 1024, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return device_error(e);
+  if (slots == 0) return HA_OK;
   const unsigned grid = (unsigned)(p->B * p->H_kv * row_blocks);
   const int esz = p->dtype == HA_F32 ? 4 : 2, row = p->d_head * esz;
   if (row == 128) evict_copy_kernel<128><<<grid, 256, 0, stream>>>(a, esz);

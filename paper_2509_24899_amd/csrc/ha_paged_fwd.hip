@@ -600,7 +600,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
 
 // fp32: 32 slots to a step, in registers a step ahead and in one stage of LDS in three pieces.
 template <int D>
-__global__ __launch_bounds__(256, 1) void paged_tile_f32_kernel(FwdArgs a) {
+__global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
   constexpr bool F32 = true;
   typedef Tile<D> T;
   constexpr int KS = D / 16, RB = D / 32, NS = 3, STAGE = T::bytes(32), ESZ = 4, PER = 32 * T::PIECES / 256;
@@ -808,7 +808,7 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
   auto split = [&](Part &part, int64_t groups, int64_t least, int rows) {
     part.groups = (int)groups;
     int64_t parts = groups > 0 ? std::min(256 / groups, steps / least) : 1;
-    if (rows == 128 && groups > 0) parts = std::max(parts, std::min(512 / groups, steps / 64));
+    if (rows == 128 && groups > 0) parts = std::max(parts, std::min(512 / groups, steps / (p.dtype == HA_F32 ? 4 : 64)));
     part.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
     if (part.runs && part.n_split > 1) {
       const size_t n = (size_t)groups * part.n_split * rows;

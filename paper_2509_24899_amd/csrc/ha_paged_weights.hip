@@ -2,9 +2,10 @@
 //
 //   w_j += sum over rows R that see slot j of exp(scale q_R . k_j - lse_R)
 //
-// A wave owns 32 slots, whose keys stay in its registers, and walks the rows 32 at a time: S = Q K^T with the slot as the lane's column, so that a slot's sum is a
-// lane's own.  Single tokens: bound by reading the keys.  Chunks: an exponential for every row and slot next to 2 d operations of the matrix cores, which
-// take about as long.
+// A wave owns 32 slots at a time, S = Q K^T with the slot as the lane's column, so that a slot's sum over the rows is a lane's own (and its other half's).
+//   few   32 rows at most: bound by reading the keys.  The rows stay in registers, the wave walks slots.
+//   tile  more rows: an exponential for every row and slot next to 2 d operations of the matrix cores, which take about as long.  The keys stay in registers, the
+//         four waves of a workgroup walk the rows, which they share in LDS.
 #include "ha_paged.h"
 
 #include <algorithm>
@@ -18,25 +19,176 @@ struct WeightArgs {
   const float *lse, *weights;
   float *out;
   float scale_log2e;
-  int blocks;                 // of 128 slots, in a sequence
+  int parts;                  // workgroups of a sequence and key head
+  int few;                    // tile: sequences of 32 rows or fewer are another launch's
 };
 
+// Row R of a sequence: its query, - lse log2 e (- infinity where it sees nothing or is none), and how many slots it sees.
+struct WeightRow {
+  int64_t query;              // in elements
+  float shift;
+  int see;
+  __device__ __forceinline__ WeightRow(const WeightArgs &a, const NewRows &n, int held, int hk, int R) {
+    const Paged &p = a.p;
+    const int n_rows = n.n * p.G, Rc = min(R, n_rows - 1), i = Rc / p.G, h = hk * p.G + Rc - i * p.G;
+    const int64_t token = n.first + i;
+    const float x = a.lse[token * p.H + h];
+    query = h * a.q.sh + token * a.q.sn;
+    shift = R < n_rows && x != -INFINITY ? -x * kLog2e : -INFINITY;
+    see = p.causal ? min(held, held - n.all + i + 1) : held;
+  }
+};
+
+static __device__ __forceinline__ void add_weight(const WeightArgs &a, int64_t at, float sum) { a.out[at] = (a.weights ? a.weights[at] : 0.f) + sum; }
+
+// Sum over 32 rows of the weights of this lane's slot; shift and see of the rows in LDS.  ALL: every row sees the slot.
+template <bool ALL>
+static __device__ __forceinline__ float sum_rows(const f32x16 &sc, const float *shift, const int *see, int slot, float c, int g) {
+  float sum = 0.f;
+#pragma unroll
+  for (int y4 = 0; y4 < 4; ++y4) {
+    const f32x4 t = *reinterpret_cast<const f32x4 *>(shift + 8 * y4 + 4 * g);
+    const i32x4 s = ALL ? i32x4{} : *reinterpret_cast<const i32x4 *>(see + 8 * y4 + 4 * g);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float e = fast_exp2(__builtin_fmaf(sc[4 * y4 + y], c, t[y]));
+      sum += ALL || (slot < s[y] && t[y] != -INFINITY) ? e : 0.f;
+    }
+  }
+  return sum;
+}
+
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void paged_weights_kernel(WeightArgs a) {
+__global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
+  typedef Tile<D> T;
   constexpr int KS = D / 16, NS = F32 ? 3 : 1, ESZ = F32 ? 4 : 2;
-  __shared__ float shift[4][32];      // [wave][row]: - lse log2 e
-  __shared__ int sees[4][32];         // slots that the row sees
+  __shared__ __attribute__((aligned(1024))) char lds[F32 ? 16 : 4 * T::bytes(32)];
+  __shared__ float shift[32];
+  __shared__ int see[32];
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int bh = blockIdx.x / a.blocks, b = bh / p.Hkv, hk = bh % p.Hkv, slot0 = (blockIdx.x % a.blocks) * 128 + 32 * w, slot = slot0 + r;
+  const int bh = blockIdx.x / a.parts, part = blockIdx.x % a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, capacity = p.capacity();
+  const NewRows n(p, b);
+  const int held = p.held(b), n_rows = n.n * p.G;
+  if (n_rows > 32) return;
+  bf16x8 qf[KS][NS];
+  if (n_rows > 0) {
+    const WeightRow row(a, n, held, hk, r);
+    const char *qp = a.q.p + (row.query + 8 * g) * ESZ;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if constexpr (F32) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
+      else qf[ks][0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+    }
+    if (threadIdx.x < 32) {
+      shift[r] = row.shift;
+      see[r] = row.see;
+    }
+  }
+  __syncthreads();
+  const int first_sees = p.causal ? min(held, held - n.all + 1) : held;
+  char *mine = lds + w * T::bytes(32);
+  const unsigned rows0 = F32 ? 0 : T::rows_base(mine, lane);
+  const char *kbase = a.k.p + hk * a.k.sh * ESZ;
+  for (int slot0 = (part * 4 + w) * 32; slot0 < capacity; slot0 += a.parts * 128) {
+    const int slot = slot0 + r;
+    float sum = 0.f;
+    if (slot0 < held && n_rows > 0) {
+      const int id0 = __builtin_amdgcn_readfirstlane(p.page_of(b, slot0)), id1 = p.page > 16 || slot0 + 16 >= capacity ? id0 : __builtin_amdgcn_readfirstlane(p.page_of(b, slot0 + 16));
+      f32x16 sc;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+      if constexpr (F32) {
+        const int id = r < 16 ? id0 : id1;
+        const bool there = id >= 0 && slot < held;
+        const char *kp = kbase + ((there ? id * a.k.sb + (int64_t)(slot & (p.page - 1)) * a.k.sn : 0) + 8 * g) * 4;
+        f32x4 x[KS][2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) x[ks][i] = there ? *reinterpret_cast<const f32x4 *>(kp + 64 * ks + 16 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          bf16x8 kf[3];
+          split8_any(x[ks][0], x[ks][1], kf);
+          sc = mfma_split<3>(qf[ks], kf, sc);
+        }
+      } else {
+        const int ksn = (int)a.k.sn * 2;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int id = i ? id1 : id0, at = slot0 + 16 * i, rows = id < 0 ? 0 : min(held - at, 16);
+          request_rows<D, 16, 1>(rows_rsrc<D>(kbase + (max(id, 0) * a.k.sb + (int64_t)(at & (p.page - 1)) * a.k.sn) * 2, rows, ksn), ksn, mine + i * T::bytes(16), 0, lane);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc = mfma32(qf[ks][0], T::rows_at(rows0, 0, ks), sc);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (the next slots may be asked for)
+      }
+      sum = slot0 + 32 <= first_sees ? sum_rows<true>(sc, shift, see, slot, a.scale_log2e, g) : sum_rows<false>(sc, shift, see, slot, a.scale_log2e, g);
+      if ((r < 16 ? id0 : id1) < 0) sum = 0.f;
+    }
+    sum = xhalf_sum(sum);
+    if (g == 0 && slot < capacity) add_weight(a, (int64_t)bh * capacity + slot, sum);
+  }
+}
+
+template <int D, bool F32>
+__global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a) {
+  typedef Tile<D> T;
+  constexpr int KS = D / 16, NS = F32 ? 3 : 1, ESZ = F32 ? 4 : 2, STAGE = T::bytes(32), PER = 32 * T::PIECES / 256;
+  __shared__ __attribute__((aligned(1024))) char lds[2][NS * STAGE];
+  __shared__ float shift[2][32];
+  __shared__ int see[2][32];
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+  const int bh = blockIdx.x / a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, first = (blockIdx.x % a.parts) * 128, slot0 = first + 32 * w, slot = slot0 + r, capacity = p.capacity();
   const NewRows n(p, b);
   const int held = p.held(b), n_rows = n.n * p.G, before = held - n.all;      // before: slots ahead of the first new token's
-  if (slot0 >= p.capacity()) return;
+  if (a.few && n_rows <= 32) return;
+  const int64_t out = (int64_t)bh * capacity + slot;
+  const int id = slot < held ? p.page_of(b, slot) : -1;
   float sum = 0.f;
-  if (slot0 < held && n_rows > 0) {
-    const int R_first = p.causal ? max(slot0 - before, 0) * p.G / 32 * 32 : 0;      // (of the 32 rows with the first that sees the wave's first slot)
-    const int id = slot < held ? p.page_of(b, slot) : -1;
-    const char *kp = a.k.p + (hk * a.k.sh + (id < 0 ? 0 : (int64_t)id * a.k.sb + (int64_t)(slot & (p.page - 1)) * a.k.sn) + 8 * g) * ESZ;
+  // rows that see the workgroup's first slot, from a multiple of 32 on
+  int R0 = first >= held ? n_rows : p.causal ? max(first - before, 0) * p.G / 32 * 32 : 0;
+  if (R0 < n_rows) {
+    Row8 x[PER];
+    float next_shift = 0.f;
+    int next_see = 0;
+    auto request = [&](int R) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = threadIdx.x + 256 * i, piece = at % T::PIECES;
+        const WeightRow row(a, n, held, hk, R + at / T::PIECES);
+        x[i] = load_row8<F32, true>(a.q.p, row.query, 8 * piece, 8 * piece + 4);
+      }
+      if (threadIdx.x < 32) {
+        const WeightRow row(a, n, held, hk, R + r);
+        next_shift = row.shift;
+        next_see = row.see;
+      }
+    };
+    auto deposit = [&](int stage) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = threadIdx.x + 256 * i, line = at / T::PIECES, piece = at % T::PIECES;
+        char *to = lds[stage] + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
+        if constexpr (F32) {
+          bf16x8 y[3];
+          split8_any(x[i].a, x[i].b, y);
+#pragma unroll
+          for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = y[s];
+        } else {
+          *reinterpret_cast<bf16x8 *>(to) = __builtin_convertvector(__builtin_shufflevector(x[i].a, x[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+        }
+      }
+      if (threadIdx.x < 32) {
+        shift[stage][r] = next_shift;
+        see[stage][r] = next_see;
+      }
+    };
+    request(R0);
+    const char *kp = a.k.p + (hk * a.k.sh + (id < 0 ? 0 : id * a.k.sb + (int64_t)(slot & (p.page - 1)) * a.k.sn) + 8 * g) * ESZ;
     bf16x8 kf[KS][NS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -48,51 +200,36 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(WeightArgs a) {
         }
         split8_any(lo, hi, kf[ks]);
       } else {
-        bf16x8 x = {};
-        if (id >= 0) x = *reinterpret_cast<const bf16x8 *>(kp + 32 * ks);
-        kf[ks][0] = x;
+        kf[ks][0] = bf16x8{};
+        if (id >= 0) kf[ks][0] = *reinterpret_cast<const bf16x8 *>(kp + 32 * ks);
       }
     }
-    for (int R0 = R_first; R0 < n_rows; R0 += 32) {
-      const int R = R0 + r, Rc = min(R, n_rows - 1), i = Rc / p.G, h = hk * p.G + Rc - i * p.G;
-      const int64_t token = n.first + i;
-      const char *qp = a.q.p + (h * a.q.sh + token * a.q.sn + 8 * g) * ESZ;
-      const float x = a.lse[token * p.H + h];
-      const int see = p.causal ? min(held, before + i + 1) : held;
-      if (g == 0) {
-        shift[w][r] = R < n_rows && x != -INFINITY ? -x * kLog2e : -INFINITY;
-        sees[w][r] = see;
-      }
+    deposit(0);
+    __syncthreads();
+    for (int stage = 0; R0 < n_rows; R0 += 32, stage ^= 1) {
+      if (R0 + 32 < n_rows) request(R0 + 32);
+      const unsigned rows0 = T::rows_base(lds[stage], lane);
       f32x16 sc;
 #pragma unroll
       for (int y = 0; y < 16; ++y) sc[y] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 qf[NS];
-        if constexpr (F32) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf);
-        else qf[0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) qf[s] = T::rows_at(rows0, 0, ks, s * STAGE);
         sc = mfma_split<NS>(qf, kf[ks], sc);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (a wave's LDS instructions execute in order)
-#pragma unroll
-      for (int y4 = 0; y4 < 4; ++y4) {
-        const f32x4 t = *reinterpret_cast<const f32x4 *>(&shift[w][8 * y4 + 4 * g]);
-        const int *s = &sees[w][8 * y4 + 4 * g];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const float e = fast_exp2(__builtin_fmaf(sc[4 * y4 + y], a.scale_log2e, t[y]));
-          sum += slot < s[y] && t[y] != -INFINITY ? e : 0.f;
-        }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      // (a row that sees all of the wave's slots: so do those behind it)
+      const int first_sees = p.causal ? min(held, before + R0 / p.G + 1) : held;
+      sum += slot0 + 32 <= first_sees && R0 + 32 <= n_rows ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
+                                                           : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g);
+      if (R0 + 32 < n_rows) deposit(stage ^ 1);
+      __syncthreads();
     }
     if (id < 0) sum = 0.f;
   }
   sum = xhalf_sum(sum);
-  if (g == 0 && slot < p.capacity()) {
-    const int64_t at = (int64_t)bh * p.capacity() + slot;
-    a.out[at] = (a.weights ? a.weights[at] : 0.f) + sum;
-  }
+  if (g == 0 && slot < capacity) add_weight(a, out, sum);
 }
 
 }  // namespace
@@ -111,8 +248,8 @@ extern "C" ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const 
   if (st != HA_OK) return st;
   WeightArgs a{};
   if ((st = check_packed(*p, q, p->H, false, a.q)) != HA_OK || (st = check_pool(*p, k_pages, false, a.k)) != HA_OK) return st;
-  const int64_t slots = (int64_t)p->max_pages * p->page, blocks = (slots + 127) / 128;
-  if ((int64_t)p->B * p->H_kv * blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
+  const int64_t slots = (int64_t)p->max_pages * p->page, blocks = (slots + 127) / 128, groups = (int64_t)p->B * p->H_kv, rows = (int64_t)p->max_new * (p->H / p->H_kv);
+  if (groups * blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
   if ((p->T > 0 && !lse) || (slots > 0 && !weights_out)) return HA_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out)) & 3u) return HA_ERR_ALIGN;
   if ((st = check_workspace(workspace, workspace_bytes, hybrid_attn_paged_weights_workspace_bytes(p))) != HA_OK) return st;
@@ -122,12 +259,23 @@ extern "C" ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const 
   a.weights = weights;
   a.out = weights_out;
   a.scale_log2e = p->softmax_scale * kLog2e;
-  a.blocks = (int)blocks;
-  const unsigned grid = (unsigned)(p->B * p->H_kv * blocks);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const bool f32 = p->dtype == HA_F32;
-  if (p->d_head == 128) { if (f32) paged_weights_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
-  else { if (f32) paged_weights_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? HA_OK : device_error(e);
+  const bool f32 = p->dtype == HA_F32, few = rows <= 32 || p->q_offset;
+  hipError_t e;
+  if (rows > 32) {
+    a.parts = (int)blocks;
+    a.few = few;
+    const unsigned grid = (unsigned)(groups * blocks);
+    if (p->d_head == 128) { if (f32) paged_weights_tile_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
+    else { if (f32) paged_weights_tile_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
+    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+  }
+  if (few) {
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 2048 / groups));
+    const unsigned grid = (unsigned)(groups * a.parts);
+    if (p->d_head == 128) { if (f32) paged_weights_few_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
+    else { if (f32) paged_weights_few_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
+    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+  }
+  return HA_OK;
 }

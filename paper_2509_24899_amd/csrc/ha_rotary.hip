@@ -179,17 +179,26 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all
 }
 
 // Sum of the workgroups' sums, 16 columns to a workgroup, in double.
-__global__ __launch_bounds__(256) void weight_sums_kernel(const float *partial, int n, int width, int D, float *dw_q, float *dw_k) {
-  __shared__ double lds[16][17];
+__global__ __launch_bounds__(1024) void weight_sums_kernel(const float *partial, int n, int width, int D, float *dw_q, float *dw_k) {
+  constexpr int U = 8;        // loads in flight
+  __shared__ double lds[64][17];
   const int c = threadIdx.x % 16, r = threadIdx.x / 16, col = blockIdx.x * 16 + c;
   double sum = 0.;
-  for (int i = r; i < n; i += 16) sum += (double)partial[(int64_t)i * width + col];
+  for (int i = r; i < n; i += 64 * U) {
+    float x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = i + 64 * u < n ? partial[(int64_t)(i + 64 * u) * width + col] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) sum += (double)x[u];
+  }
   lds[r][c] = sum;
   __syncthreads();
-  if (r) return;
-  for (int i = 1; i < 16; ++i) sum += lds[i][c];
+  for (int half = 32; half > 0; half /= 2) {
+    if (r < half) lds[r][c] += lds[r + half][c];
+    __syncthreads();
+  }
   float *out = col < D ? dw_q : dw_k;
-  if (out) out[col % D] = (float)sum;
+  if (r == 0 && out) out[col % D] = (float)lds[0][c];
 }
 
 ha_status check_problem(const ha_rows_problem *p) {
@@ -326,7 +335,7 @@ extern "C" ha_status hybrid_attn_norm_rotate_grad(const ha_rows_problem *p, cons
   else e = p->dtype == HA_F32 ? launch_grad<64, true>(a, grid, groups, r->interleaved, stream) : launch_grad<64, false>(a, grid, groups, r->interleaved, stream);
   if (e != hipSuccess) return device_error(e);
   if (a.partial) {
-    weight_sums_kernel<<<2 * d / 16, 256, 0, stream>>>(a.partial, (int)(grid.x * grid.y), 2 * d, d, grad_w_q, grad_w_k);
+    weight_sums_kernel<<<2 * d / 16, 1024, 0, stream>>>(a.partial, (int)(grid.x * grid.y), 2 * d, d, grad_w_q, grad_w_k);
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
   }
   return HA_OK;

@@ -201,6 +201,30 @@ def _calls():
     return _CALLS
 
 
+_ROWS = None
+
+
+def _rows():
+    """The same module, bound to the calls of rotary and paged as well, or False.  Looked for once, like _binding's result."""
+    global _ROWS
+    if _ROWS is None:
+        native = _calls()
+        if native is False and _CALLS is None:
+            return False                                  # (no library yet, which the call will report)
+        if native:
+            from . import paged, rotary
+            if getattr(native, "rows_abi", None) != tuple(ctypes.sizeof(s) for s in (rotary.ha_rotary, rotary.ha_rows_problem, paged.ha_paged_problem)):
+                native = False
+            else:
+                lib = _lib()
+                native.bind_rows(tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+                    "hybrid_attn_rotate", "hybrid_attn_norm_rotate", "hybrid_attn_norm_rotate_grad_workspace_bytes", "hybrid_attn_norm_rotate_grad", "hybrid_attn_paged_append",
+                    "hybrid_attn_paged_workspace_bytes", "hybrid_attn_paged_forward", "hybrid_attn_paged_weights_workspace_bytes", "hybrid_attn_paged_weights",
+                    "hybrid_attn_paged_evict_workspace_bytes", "hybrid_attn_paged_evict")))
+        _ROWS = native
+    return _ROWS
+
+
 def _mismatch(what):
     raise ValueError(f"feature map does not match the problem: {what}")
 

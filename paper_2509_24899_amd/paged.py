@@ -9,7 +9,8 @@ token gets in it, and eviction by that weight.
 
 q is a [T, H, d] view of the new tokens of all sequences, one behind the other (those of sequence b from q_offset[b] on; q_offset None: the same number each), k and v are
 [T, H_kv, d], and the pools k_pages and v_pages are [n_pages, H_kv, page, d] views, each with strides of its own and a contiguous last dimension.  page_table int32
-[B, max_pages], key_len int32 [B], q_offset int32 [B + 1].  Argument marshalling only, as in hybrid_attn; everything is public there.
+[B, max_pages], key_len int32 [B], q_offset int32 [B + 1].  Argument marshalling only, as in hybrid_attn; everything is public there.  Plain calls are marshalled by compiled code
+(csrc/ha_binding_rows.h), all others, and every error, here.
 """
 from __future__ import annotations
 
@@ -115,12 +116,19 @@ def _checked(*args, **kwargs):
     return lib, prob
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_paged_append(q, k, v, k_pages, v_pages, page_table, key_len, q_offset=None, max_new: Optional[int] = None, w_q=None, w_k=None,
                              rotary: Optional[_rot.Rotary] = None, positions=None, eps: Optional[float] = None, q_out=None, stream=None):
     """Store the new tokens' k and v [T, H_kv, d] in their slots (key_len counts them already) and return the queries that go with them; q may be None.  eps: queries and keys
     are normed for each head first, with the weights w_q and w_k (fp32 [d], or None); None: not.  rotary: they are rotated by positions, int32 [T, axes]; None: not.
     q_out may be q itself.  max_new: the most new tokens that a sequence has.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.paged_append(q, k, v, k_pages, v_pages, page_table, key_len, q_offset, max_new, w_q, w_k, rotary, positions, eps, q_out, stream)) is not None:
+        return done[0]
+    return _append(q, k, v, k_pages, v_pages, page_table, key_len, q_offset, max_new, w_q, w_k, rotary, positions, eps, q_out, stream)
+
+
+@_ha._allocations_follow_stream
+def _append(q, k, v, k_pages, v_pages, page_table, key_len, q_offset, max_new, w_q, w_k, rotary, positions, eps, q_out, stream):
     _ha._require_gpu(q, k, v, k_pages, v_pages, page_table, key_len, q_offset, w_q, w_k, positions, q_out)
     if eps is None and (w_q is not None or w_k is not None):
         raise ValueError("w_q and w_k are the norm's, which eps=None leaves out")
@@ -145,12 +153,19 @@ def hybrid_attn_paged_append(q, k, v, k_pages, v_pages, page_table, key_len, q_o
     return q_out
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_paged_forward(q, k_pages, v_pages, page_table, key_len, q_offset=None, max_new: Optional[int] = None, causal: bool = True,
                               softmax_scale: Optional[float] = None, with_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """Softmax attention of the new tokens q [T, H, d] over the slots of their sequences; returns (out, lse): out like q, lse fp32 [T, H] (the logarithm of every row's
     sum of weights) or None without with_lse.  causal: a new token sees the slots up to its own, otherwise all.  Rows of no sequence are left as they were.
     Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.paged_forward(q, k_pages, v_pages, page_table, key_len, q_offset, max_new, causal, softmax_scale, with_lse, out, lse, workspace, stream)) is not None:
+        return done
+    return _forward(q, k_pages, v_pages, page_table, key_len, q_offset, max_new, causal, softmax_scale, with_lse, out, lse, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _forward(q, k_pages, v_pages, page_table, key_len, q_offset, max_new, causal, softmax_scale, with_lse, out, lse, workspace, stream):
     _ha._require_gpu(q, k_pages, v_pages, page_table, key_len, q_offset, out, lse, workspace)
     with _ha._on_device_of(q):
         _pools(q, k_pages, v_pages)
@@ -170,11 +185,18 @@ def hybrid_attn_paged_forward(q, k_pages, v_pages, page_table, key_len, q_offset
     return out, lse
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_paged_weights(q, k_pages, lse, weights, page_table, key_len, q_offset=None, max_new: Optional[int] = None, causal: bool = True,
                               softmax_scale: Optional[float] = None, out=None, workspace=None, stream=None):
     """Add the weight that every slot got in hybrid_attn_paged_forward, from its queries and lse and the same arguments, to what it has had: weights fp32
     [B, H_kv, max_pages page], or None: nothing so far.  The sums go to out, or to weights itself; returned.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.paged_weights(q, k_pages, lse, weights, page_table, key_len, q_offset, max_new, causal, softmax_scale, out, workspace, stream)) is not None:
+        return done
+    return _weights(q, k_pages, lse, weights, page_table, key_len, q_offset, max_new, causal, softmax_scale, out, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _weights(q, k_pages, lse, weights, page_table, key_len, q_offset, max_new, causal, softmax_scale, out, workspace, stream):
     _ha._require_gpu(q, k_pages, lse, weights, page_table, key_len, q_offset, out, workspace)
     with _ha._on_device_of(q):
         _pools(q, k_pages)
@@ -192,12 +214,19 @@ def hybrid_attn_paged_weights(q, k_pages, lse, weights, page_table, key_len, q_o
     return out
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_paged_evict(k_pages, v_pages, weights, page_table, key_len, keep: int, out_table, keep_first: int = 0, keep_last: int = 0, len_out=None, weights_out=None,
                             kept=None, workspace=None, stream=None):
     """Copy the `keep` slots of every sequence and key head that matter most to slots 0, 1, .. of the pages of out_table (int32 [B, out_pages]), in their order: the first
     keep_first, the last keep_last, and the others of the largest weights (fp32 [B, H_kv, max_pages page]), of equal ones the lower slot.  Returns (int32 [B] slots that
     stay, their weights with zeros behind them, int32 [B, H_kv, keep] which slots stayed with -1 behind them).  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.paged_evict(k_pages, v_pages, weights, page_table, key_len, keep, out_table, keep_first, keep_last, len_out, weights_out, kept, workspace, stream)) is not None:
+        return done
+    return _evict(k_pages, v_pages, weights, page_table, key_len, keep, out_table, keep_first, keep_last, len_out, weights_out, kept, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _evict(k_pages, v_pages, weights, page_table, key_len, keep, out_table, keep_first, keep_last, len_out, weights_out, kept, workspace, stream):
     _ha._require_gpu(k_pages, v_pages, weights, page_table, key_len, out_table, len_out, weights_out, kept, workspace)
     with _ha._on_device_of(k_pages):
         _pools(k_pages, k_pages, v_pages)

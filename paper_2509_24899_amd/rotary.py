@@ -7,7 +7,7 @@
     x = hybrid_attn_rotate(x, rotary, places)                  # the rotation alone; hybrid_attn_rotate_grad: its gradient
 
 q is a [B, H, N, d] view, k a [B, H_kv, N, d] view, each with strides of its own and a contiguous last dimension.  Argument marshalling only, as in
-hybrid_attn; everything is public there.
+hybrid_attn; everything is public there.  Plain calls are marshalled by compiled code (csrc/ha_binding_rows.h), all others, and every error, here.
 """
 from __future__ import annotations
 
@@ -150,11 +150,17 @@ def hybrid_attn_norm_rotate_grad_workspace_bytes(problem: ha_rows_problem) -> in
 
 def hybrid_attn_rotate(x, rotary: Rotary, positions, out=None, stream=None):
     """Rotation of x [B, H, N, d] by positions, int32 [N, axes] or [B, N, axes]; out may be x itself.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.rotate(x, rotary, positions, False, out, stream)) is not None:
+        return done
     return _rotate(x, rotary, positions, False, out, stream)
 
 
 def hybrid_attn_rotate_grad(grad_out, rotary: Rotary, positions, out=None, stream=None):
     """Gradient of hybrid_attn_rotate's x from that of its result: the transposed rotation.  out may be grad_out itself.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.rotate(grad_out, rotary, positions, True, out, stream)) is not None:
+        return done
     return _rotate(grad_out, rotary, positions, True, out, stream)
 
 
@@ -171,10 +177,17 @@ def _rotate(x, rotary, positions, transposed, out, stream):
     return out
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_norm_rotate(q, k, w_q=None, w_k=None, rotary: Optional[Rotary] = None, positions=None, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
     """Queries and keys (k may be None) divided by the root of every row's mean square, times the weights (fp32 [d], or None), and rotated (rotary None: not): returns
     (q_out, k_out), which may be q and k themselves.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.norm_rotate(q, k, w_q, w_k, rotary, positions, eps, q_out, k_out, stream)) is not None:
+        return done
+    return _norm_rotate(q, k, w_q, w_k, rotary, positions, eps, q_out, k_out, stream)
+
+
+@_ha._allocations_follow_stream
+def _norm_rotate(q, k, w_q, w_k, rotary, positions, eps, q_out, k_out, stream):
     _ha._require_gpu(q, k, w_q, w_k, q_out, k_out)
     with _ha._on_device_of(q):
         prob = _rows_problem(q, k, eps)
@@ -189,11 +202,18 @@ def hybrid_attn_norm_rotate(q, k, w_q=None, w_k=None, rotary: Optional[Rotary] =
     return q_out, k_out
 
 
-@_ha._allocations_follow_stream
 def hybrid_attn_norm_rotate_grad(grad_q, grad_k, q, k, w_q=None, w_k=None, rotary: Optional[Rotary] = None, positions=None, eps: float = 1e-6, grad_in_q=None,
                                  grad_in_k=None, grad_w_q=None, grad_w_k=None, workspace=None, stream=None):
     """Gradients of q, k, w_q and w_k from those of hybrid_attn_norm_rotate's results; q, k and the rest as that took them.  Returns (grad_in_q, grad_in_k, grad_w_q,
     grad_w_k), the last two fp32 [d], each None where its tensor is.  Does not synchronise."""
+    native = _ha._ROWS or _ha._rows()
+    if native and (done := native.norm_rotate_grad(grad_q, grad_k, q, k, w_q, w_k, rotary, positions, eps, grad_in_q, grad_in_k, grad_w_q, grad_w_k, workspace, stream)) is not None:
+        return done
+    return _norm_rotate_grad(grad_q, grad_k, q, k, w_q, w_k, rotary, positions, eps, grad_in_q, grad_in_k, grad_w_q, grad_w_k, workspace, stream)
+
+
+@_ha._allocations_follow_stream
+def _norm_rotate_grad(grad_q, grad_k, q, k, w_q, w_k, rotary, positions, eps, grad_in_q, grad_in_k, grad_w_q, grad_w_k, workspace, stream):
     _ha._require_gpu(grad_q, grad_k, q, k, w_q, w_k, grad_in_q, grad_in_k, grad_w_q, grad_w_k, workspace)
     if (grad_k is None) != (k is None):
         raise ValueError("grad_k and k must both be given, or neither")
