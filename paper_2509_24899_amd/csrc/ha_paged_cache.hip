@@ -92,7 +92,8 @@ struct EvictArgs {
   int out_pages, keep, first, last;
   int32_t *len_out, *kept;
   float *weights_out;
-  int row_blocks;             // copying: workgroups of a sequence and head
+  int row_blocks, chunks;     // workgroups of a sequence and head: copying, choosing
+  unsigned *hist, *counts, *last_weight;      // [B H_kv][3][kBins], [B H_kv][chunks][2], [B H_kv][2]
 };
 
 // Order of weights as that of unsigned integers: a NaN above all.
@@ -102,18 +103,73 @@ static __device__ __forceinline__ unsigned ordered(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// The slots that stay, of one sequence and key head to a workgroup of 1024.  The weights of 65536 slots are held in registers (more are read anew in every pass), slot
-// j0 + 1024 i + t in register i of thread t.  Three passes over 11, 11 and 10 bits of their order count how many have each digit, from the top, until the last weight that
-// stays is known; its ties stay from the lowest slot on.
+// The order of the last weight that stays is found eleven, eleven and ten bits at a time: how many of the candidates have each digit, counted from the top.
+constexpr int kBins = 2048;
+static __device__ __forceinline__ int shift_of(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+static __device__ __forceinline__ unsigned digit_of(unsigned u, int pass) { return (u >> shift_of(pass)) & (pass == 2 ? 1023 : 2047); }
+static __device__ __forceinline__ unsigned known_bits(int pass) { return pass == 0 ? 0 : ~0u << (pass == 1 ? 21 : 10); }      // ahead of a pass
+
+// The sum over the threads ahead of this one of a workgroup, and over all; `sums` holds one number for each wave.
+template <int THREADS>
+static __device__ __forceinline__ unsigned prefix_sum(unsigned n, unsigned *sums, unsigned &total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  unsigned upto = n;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned y = __shfl_up(upto, d);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();
+  if (lane == 63) sums[w] = upto;
+  __syncthreads();
+  unsigned before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) {
+    before += i < w ? sums[i] : 0;
+    total += sums[i];
+  }
+  return before + upto - n;
+}
+// The digit at which the count from the top reaches `need`, and how many are still needed of it.  All threads, `found` and `sums` in LDS.
+template <int THREADS>
+static __device__ __forceinline__ void find_digit(const unsigned *hist, int pass, unsigned &prefix, unsigned &need, unsigned *found, unsigned *sums) {
+  constexpr int PER = kBins / THREADS;
+  unsigned n[PER], mine = 0, total;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine += n[i] = hist[kBins - 1 - (PER * threadIdx.x + i)];
+  unsigned above = prefix_sum<THREADS>(mine, sums, total);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (above < need && need <= above + n[i]) {
+      found[0] = kBins - 1 - (PER * threadIdx.x + i);
+      found[1] = need - above;
+    }
+    above += n[i];
+  }
+  __syncthreads();
+  prefix |= found[0] << shift_of(pass);
+  need = found[1];
+  __syncthreads();
+}
+// Counts a digit.  (Equal weights, of slots that nothing has looked at yet for instance, would queue up at one place.)
+static __device__ __forceinline__ void count_digit(unsigned *hist, bool counts, unsigned digit) {
+  const uint64_t who = __ballot(counts);
+  if (who == 0) return;
+  const int first = __ffsll((long long)who) - 1;
+  if (__ballot(counts && digit == (unsigned)__builtin_amdgcn_readlane((int)digit, first)) == who) {
+    if ((int)(threadIdx.x & 63) == first) atomicAdd(&hist[digit], (unsigned)__popcll(who));
+  } else if (counts) {
+    atomicAdd(&hist[digit], 1u);
+  }
+}
+
+// Caches of 8192 slots at most: one sequence and key head to a workgroup of 1024, which holds its weights in registers, slot 1024 i + t in register i of thread t.
 __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
-  constexpr int PER = 64, BINS = 2048, CHUNK = PER * 1024;
-  __shared__ unsigned hist[BINS];
-  __shared__ unsigned wave_sums[16];
-  __shared__ unsigned found[2];               // the digit, what is still to be taken of it
-  __shared__ unsigned stays[PER][16], ties[PER][16];      // [register][wave]: how many; then how many ahead of them
+  constexpr int PER = 8;
+  __shared__ unsigned hist[kBins], sums[16], found[2], stays[PER * 16], ties[PER * 16];      // [register][wave]: how many; then how many ahead of them
   const Paged &p = a.p;
-  const int bh = blockIdx.x, b = bh / p.Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int held = p.held(b);
+  const int bh = blockIdx.x, b = bh / p.Hkv, lane = threadIdx.x & 63, w = threadIdx.x >> 6, held = p.held(b);
   const float *x = a.weights + (int64_t)bh * p.capacity();
   int32_t *kept = a.kept + (int64_t)bh * a.keep;
   if (bh % p.Hkv == 0 && threadIdx.x == 0) a.len_out[b] = min(held, a.keep);
@@ -124,122 +180,158 @@ __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
   }
   const int lo = a.first, hi = held - a.last, wanted = a.keep - a.first - a.last;      // candidates lo .. hi - 1, how many of them stay
   unsigned u[PER];
-  auto load = [&](int j0) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) u[i] = 1024 * i + (int)threadIdx.x < held ? ordered(x[1024 * i + threadIdx.x]) : 0;
+  unsigned prefix = 0, need = wanted;         // the leading digits of the last weight that stays, and how many stay of those that share them
+  for (int pass = 0; pass < 3 && wanted > 0; ++pass) {
+    hist[2 * threadIdx.x] = hist[2 * threadIdx.x + 1] = 0;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (j0 + 1024 * i >= held) break;
-      const int j = j0 + 1024 * i + threadIdx.x;
-      u[i] = j < held ? ordered(x[j]) : 0;
-    }
-  };
-  const bool once = held <= CHUNK;
-  if (once) load(0);
-  // the sum over the threads ahead of this one, and over all
-  auto prefix_sum = [&](unsigned n, unsigned &total) {
-    unsigned upto = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const unsigned y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
-    }
-    if (lane == 63) wave_sums[w] = upto;
-    __syncthreads();
-    unsigned before = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      before += i < w ? wave_sums[i] : 0;
-      total += wave_sums[i];
+      const int j = 1024 * i + threadIdx.x;
+      if (1024 * i < held) count_digit(hist, j >= lo && j < hi && (u[i] & known_bits(pass)) == prefix, digit_of(u[i], pass));
     }
     __syncthreads();
-    return before + upto - n;
-  };
-  unsigned prefix = 0, need = wanted;         // the leading digits of the last weight that stays, and how many stay of those that share them
-  if (wanted > 0) {
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      const unsigned above = pass == 0 ? 0 : ~0u << (shift + bits);      // digits that are known
-      hist[2 * threadIdx.x] = hist[2 * threadIdx.x + 1] = 0;
-      __syncthreads();
-      for (int j0 = 0; j0 < held; j0 += CHUNK) {
-        if (!once) load(j0);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          if (j0 + 1024 * i >= held) break;
-          const int j = j0 + 1024 * i + threadIdx.x;
-          const bool counts = j >= lo && j < hi && (u[i] & above) == prefix;
-          const unsigned digit = (u[i] >> shift) & ((1u << bits) - 1);
-          const uint64_t who = __ballot(counts);
-          if (who == 0) continue;
-          // (equal weights, of slots that nothing has looked at yet for instance, would queue up at one place)
-          const int first = __ffsll((long long)who) - 1;
-          if (__ballot(counts && digit == __builtin_amdgcn_readlane(digit, first)) == who) {
-            if (lane == first) atomicAdd(&hist[digit], (unsigned)__popcll(who));
-          } else if (counts) {
-            atomicAdd(&hist[digit], 1u);
-          }
-        }
-      }
-      __syncthreads();
-      // from the largest digit down: thread t has digits 2047 - 2 t and 2046 - 2 t
-      const unsigned n0 = hist[BINS - 1 - 2 * threadIdx.x], n1 = hist[BINS - 2 - 2 * threadIdx.x];
-      unsigned total;
-      const unsigned before = prefix_sum(n0 + n1, total);
-      if (before < need && need <= before + n0 + n1) {
-        const bool second = need > before + n0;
-        found[0] = BINS - 1 - 2 * threadIdx.x - second;
-        found[1] = need - before - (second ? n0 : 0);
-      }
-      __syncthreads();
-      prefix |= found[0] << shift;
-      need = found[1];
-    }
+    find_digit<1024>(hist, pass, prefix, need, found, sums);
   }
   // slots that stay, in order: outside of the candidates, above the last weight, and the first `need` of those that equal it
-  unsigned base = 0, tie_base = 0;
-  for (int j0 = 0; j0 < held; j0 += CHUNK) {
-    if (!once) load(j0);
-    // 0: goes, 1: stays, 2: a tie
-    auto kind = [&](int i) {
-      const int j = j0 + 1024 * i + threadIdx.x;
-      if (j >= held) return 0;
-      if (j < lo || j >= hi) return 1;
-      return wanted == 0 || u[i] < prefix ? 0 : u[i] > prefix ? 1 : 2;
-    };
-    __syncthreads();
+  auto kind = [&](int i) {                    // 0: goes, 1: stays, 2: a tie
+    const int j = 1024 * i + threadIdx.x;
+    return j >= held ? 0 : j < lo || j >= hi ? 1 : wanted == 0 || u[i] < prefix ? 0 : u[i] > prefix ? 1 : 2;
+  };
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      unsigned s = 0, t = 0;
-      if (j0 + 1024 * i < held) {
-        const int k = kind(i);
-        s = __popcll(__ballot(k == 1));
-        t = __popcll(__ballot(k == 2));
-      }
-      if (lane == 0) {
-        stays[i][w] = s;
-        ties[i][w] = t;
+  for (int i = 0; i < PER; ++i) {
+    const int k = kind(i);
+    const unsigned s = __popcll(__ballot(k == 1)), t = __popcll(__ballot(k == 2));
+    if (lane == 0) {
+      stays[16 * i + w] = s;
+      ties[16 * i + w] = t;
+    }
+  }
+  __syncthreads();
+  const bool entry = threadIdx.x < PER * 16;
+  unsigned total;
+  const unsigned my_ties = entry ? ties[threadIdx.x] : 0, ties_before = prefix_sum<1024>(my_ties, sums, total);
+  const unsigned mine = entry ? stays[threadIdx.x] + min(ties_before < need ? need - ties_before : 0u, my_ties) : 0, before = prefix_sum<1024>(mine, sums, total);
+  if (entry) {
+    ties[threadIdx.x] = ties_before;
+    stays[threadIdx.x] = before;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = kind(i);
+    const uint64_t below = ((uint64_t)1 << lane) - 1, tied = __ballot(k == 2);
+    const bool stay = k == 1 || (k == 2 && ties[16 * i + w] + __popcll(tied & below) < need);
+    const uint64_t all = __ballot(stay);
+    if (stay) kept[stays[16 * i + w] + __popcll(all & below)] = 1024 * i + threadIdx.x;
+  }
+}
+
+// Longer caches: 2048 slots to a workgroup, a launch for every step.  The counts of all slots of a sequence and key head meet in the workspace.
+constexpr int kChunk = 2048;
+__global__ __launch_bounds__(256) void evict_clear_kernel(unsigned *hist, int n) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) hist[i] = 0;
+}
+// A workgroup's slots: of thread t those from first + 8 t on.
+struct Chunk {
+  int bh, chunk, b, held, first, lo, hi, wanted;
+  bool all;
+  unsigned u[8];
+  __device__ __forceinline__ Chunk(const EvictArgs &a) {
+    const Paged &p = a.p;
+    bh = blockIdx.x / a.chunks;
+    chunk = blockIdx.x % a.chunks;
+    b = bh / p.Hkv;
+    held = p.held(b);
+    first = chunk * kChunk + 8 * threadIdx.x;
+    lo = a.first;
+    hi = held - a.last;
+    wanted = a.keep - a.first - a.last;
+    all = held <= a.keep;
+  }
+  __device__ __forceinline__ void load(const EvictArgs &a) {
+    const float *x = a.weights + (int64_t)bh * a.p.capacity() + first;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = first + i < held ? ordered(x[i]) : 0;
+  }
+  __device__ __forceinline__ bool candidate(int i) const { return first + i >= lo && first + i < hi; }
+  // 0: goes, 1: stays, 2: a tie
+  __device__ __forceinline__ int kind(int i, unsigned prefix) const {
+    return first + i >= held ? 0 : all || !candidate(i) ? 1 : wanted == 0 || u[i] < prefix ? 0 : u[i] > prefix ? 1 : 2;
+  }
+};
+__global__ __launch_bounds__(256) void evict_count_kernel(EvictArgs a, int pass) {
+  __shared__ unsigned hist[kBins], sums[4], found[2];
+  Chunk c(a);
+  if (c.all || c.wanted == 0 || c.chunk * kChunk >= c.hi || (c.chunk + 1) * kChunk <= c.lo) return;
+  unsigned prefix = 0, need = c.wanted;
+  c.load(a);
+  for (int q = 0; q < pass; ++q) find_digit<256>(a.hist + ((int64_t)c.bh * 3 + q) * kBins, q, prefix, need, found, sums);
+#pragma unroll
+  for (int i = 0; i < kBins / 256; ++i) hist[threadIdx.x + 256 * i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) count_digit(hist, c.candidate(i) && (c.u[i] & known_bits(pass)) == prefix, digit_of(c.u[i], pass));
+  __syncthreads();
+  unsigned *to = a.hist + ((int64_t)c.bh * 3 + pass) * kBins;
+#pragma unroll
+  for (int i = 0; i < kBins / 256; ++i) {
+    const unsigned n = hist[threadIdx.x + 256 * i];
+    if (n) atomicAdd(&to[threadIdx.x + 256 * i], n);
+  }
+}
+// LIST = false: how many slots of the chunk stay and how many are ties, and the last weight that stays.  LIST = true: the slots that stay.
+template <bool LIST>
+__global__ __launch_bounds__(256) void evict_list_kernel(EvictArgs a) {
+  __shared__ unsigned sums[4], found[2];
+  Chunk c(a);
+  int32_t *kept = a.kept + (int64_t)c.bh * a.keep;
+  unsigned *counts = a.counts + (int64_t)c.bh * a.chunks * 2, *last = a.last_weight + (int64_t)c.bh * 2, prefix = 0, need = c.wanted, total;
+  c.load(a);
+  if constexpr (LIST) {
+    prefix = last[0];
+    need = last[1];
+  } else if (!c.all && c.wanted > 0) {
+    for (int q = 0; q < 3; ++q) find_digit<256>(a.hist + ((int64_t)c.bh * 3 + q) * kBins, q, prefix, need, found, sums);
+  }
+  unsigned n_stay = 0, n_tie = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int k = c.kind(i, prefix);
+    n_stay += k == 1;
+    n_tie += k == 2;
+  }
+  const unsigned ties_here = prefix_sum<256>(n_tie, sums, total), all_ties = total, stays_here = prefix_sum<256>(n_stay, sums, total), all_stays = total;
+  if constexpr (!LIST) {
+    if (threadIdx.x == 0) {
+      counts[2 * c.chunk] = all_stays;
+      counts[2 * c.chunk + 1] = all_ties;
+      if (c.chunk == 0) {
+        last[0] = prefix;
+        last[1] = need;
+        if (c.bh % a.p.Hkv == 0) a.len_out[c.b] = min(c.held, a.keep);
       }
     }
-    __syncthreads();
-    // entry t of the register-major list: ties ahead of it say how many of its own stay
-    unsigned *all_stay = &stays[0][0], *all_ties = &ties[0][0], total_ties, total;
-    const unsigned my_ties = all_ties[threadIdx.x], ties_before = tie_base + prefix_sum(my_ties, total_ties);
-    const unsigned mine = all_stay[threadIdx.x] + min(ties_before < need ? need - ties_before : 0u, my_ties);
-    const unsigned before = base + prefix_sum(mine, total);
-    all_ties[threadIdx.x] = ties_before;
-    all_stay[threadIdx.x] = before;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      if (j0 + 1024 * i >= held) break;
-      const int k = kind(i);
-      const uint64_t below = ((uint64_t)1 << lane) - 1, tied = __ballot(k == 2);
-      const bool stay = k == 1 || (k == 2 && ties[i][w] + __popcll(tied & below) < need);
-      const uint64_t all = __ballot(stay);
-      if (stay) kept[stays[i][w] + __popcll(all & below)] = j0 + 1024 * i + threadIdx.x;
+  } else {
+    // of the chunks ahead
+    unsigned stays = 0, ties = 0;
+    for (int i = threadIdx.x; i < c.chunk; i += 256) {
+      stays += counts[2 * i];
+      ties += counts[2 * i + 1];
     }
-    base += total;
-    tie_base += total_ties;
+    prefix_sum<256>(ties, sums, total);
+    unsigned tie = total + ties_here;
+    prefix_sum<256>(stays, sums, total);
+    unsigned at = total + stays_here + min(tie, need);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = c.kind(i, prefix);
+      if (k == 1 || (k == 2 && tie < need)) kept[at++] = c.first + i;
+      tie += k == 2;
+    }
+    // (all chunks share what is behind the last slot that stays)
+    for (int j = c.held + c.chunk * 256 + threadIdx.x; j < a.keep; j += a.chunks * 256) kept[j] = -1;
   }
 }
 
@@ -296,6 +388,45 @@ hipError_t launch_append(const AppendArgs &a, bool next, bool norm, hipStream_t 
   return hipGetLastError();
 }
 
+// One workgroup chooses of 8192 slots at most; more are counted by many, in seven launches.
+struct EvictPlan {
+  int chunks;                 // 0: one workgroup
+  size_t off_counts, off_last, total;
+};
+EvictPlan evict_plan(const ha_paged_problem &p) {
+  EvictPlan f{};
+  const int64_t slots = (int64_t)p.max_pages * p.page, groups = (int64_t)p.B * p.H_kv;
+  if (slots <= 8192) return f;
+  f.chunks = (int)((slots + kChunk - 1) / kChunk);
+  f.off_counts = round256((size_t)groups * 3 * kBins * 4);
+  f.off_last = f.off_counts + round256((size_t)groups * f.chunks * 8);
+  f.total = f.off_last + round256((size_t)groups * 8);
+  return f;
+}
+hipError_t launch_choice(EvictArgs a, const EvictPlan &f, char *ws, hipStream_t st) {
+  const unsigned groups = (unsigned)a.p.B * a.p.Hkv;
+  if (f.chunks == 0) {
+    evict_choose_kernel<<<groups, 1024, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  a.chunks = f.chunks;
+  a.hist = reinterpret_cast<unsigned *>(ws);
+  a.counts = reinterpret_cast<unsigned *>(ws + f.off_counts);
+  a.last_weight = reinterpret_cast<unsigned *>(ws + f.off_last);
+  const unsigned grid = groups * f.chunks;
+  hipError_t e;
+  evict_clear_kernel<<<std::min(groups * 3 * kBins / 256, 1024u), 256, 0, st>>>(a.hist, (int)(groups * 3 * kBins));
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  for (int pass = 0; pass < 3; ++pass) {
+    evict_count_kernel<<<grid, 256, 0, st>>>(a, pass);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  evict_list_kernel<false><<<grid, 256, 0, st>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  evict_list_kernel<true><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 }  // namespace ha
 
@@ -329,9 +460,8 @@ extern "C" ha_status hybrid_attn_paged_append(const ha_paged_problem *p, const h
 }
 
 extern "C" size_t hybrid_attn_paged_evict_workspace_bytes(const ha_paged_problem *p, int32_t keep) {
-  (void)p;
-  (void)keep;
-  return 0;
+  if (check_paged(p) != HA_OK || keep < 1) return 0;
+  return evict_plan(*p).total;
 }
 
 extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t keep, int32_t keep_first, int32_t keep_last, const float *weights, const int32_t *out_table,
@@ -350,7 +480,8 @@ extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t 
   if ((reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(len_out) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(weights) |
        reinterpret_cast<uintptr_t>(weights_out)) & 3u)
     return HA_ERR_ALIGN;
-  if ((st = check_workspace(workspace, workspace_bytes, hybrid_attn_paged_evict_workspace_bytes(p, keep))) != HA_OK) return st;
+  const EvictPlan f = evict_plan(*p);
+  if ((st = check_workspace(workspace, workspace_bytes, f.total)) != HA_OK) return st;
   a.p = paged_of(*p);
   a.weights = weights;
   a.out_table = out_table;
@@ -363,8 +494,7 @@ extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t 
   a.weights_out = weights_out;
   a.row_blocks = (int)row_blocks;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  evict_choose_kernel<<<p->B * p->H_kv, 1024, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = launch_choice(a, f, static_cast<char *>(workspace), stream);
   if (e != hipSuccess) return device_error(e);
   if (slots == 0) return HA_OK;
   const unsigned grid = (unsigned)(p->B * p->H_kv * row_blocks);

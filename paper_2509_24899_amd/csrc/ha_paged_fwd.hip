@@ -51,9 +51,12 @@ struct FwdArgs {
   Paged p;
   View q, k, v, out;
   float *lse;
-  int n_split, tiles;         // ranges of the slots; tile: tiles of a key head
+  int n_split, tiles;         // tile: ranges of the slots, tiles of a key head
   int leave_few;              // tile: sequences of 32 rows or fewer are another launch's
-  float *po, *pm, *pl;        // n_split > 1: [group][range][rows][D], [group][range][rows]
+  int wanted, line_blocks;    // few: ranges that a key head's sequences are to be cut into, together; fours of rows that a sequence may have
+  int32_t *map;               // few, more than 64 sequences: [2][B + 1] ranges and places of the sequences ahead of each
+  int32_t *heads;             // few: [place] sequence and ranges where it is a sequence's first place, otherwise -1
+  float *po, *pm, *pl;        // sums of ranges: [place][rows][D], [place][rows]
   float scale, scale_log2e;
   unsigned items, share;
 };
@@ -71,19 +74,95 @@ struct RowsOf {
   }
 };
 
-// The numbers of the two pages that hold slots key .. key + 15 and key + 16 .. key + 31 (key a multiple of 32).
+// 32 slots from `key` on (-1: none) and the pages that hold the first and the last sixteen of them (-1: it is not there).
 struct Step {
   int key, id0, id1;
 };
+// Walks the slots of a sequence for one key head, 32 at a time, steps at .. end - 1 with a distance of `by`.  SMALL: pages of 16 slots, two to a step; otherwise a step lies in one
+// page, and a step next to the last one is as far from it in memory as its slots are.
+template <int D, bool SMALL>
+struct Cursor {
+  const Paged &p;
+  PageWalk walk;
+  int at, end, by, limit, left, id;
+  const char *k, *v;          // of the head; then of the step
+  const View &kv, &vv;
+  const char *k0, *v0, *k1, *v1;
+  int rows0, rows1;           // that someone sees of the step (SMALL: of its halves)
+  __device__ __forceinline__ Cursor(const FwdArgs &a, int b, int hk, int at_, int end_, int by_, int limit_, int lane)
+      : p(a.p), walk(a.p, b, lane), at(at_), end(end_), by(by_), limit(limit_), left(0), id(-1), k(a.k.p + hk * a.k.sh * 2), v(a.v.p + hk * a.v.sh * 2), kv(a.k), vv(a.v), k0(k), v0(v), k1(k), v1(v), rows0(0), rows1(0) {}
+  __device__ __forceinline__ int64_t offset(const View &x, int page, int slot) const { return (page * x.sb + (int64_t)(slot & (p.page - 1)) * x.sn) * 2; }
+  __device__ __forceinline__ Step next() {
+    Step s{-1, -1, -1};
+    rows0 = rows1 = 0;
+    if (at < end) {
+      const int key = 32 * at;
+      s.key = key;
+      if constexpr (SMALL) {
+        const int index = key >> 4;
+        s.id0 = walk.at(index);
+        s.id1 = index + 1 < p.max_pages ? walk.at(index + 1) : -1;
+        rows0 = s.id0 < 0 ? 0 : min(limit - key, 16);
+        rows1 = s.id1 < 0 ? 0 : min(limit - key - 16, 16);
+        k0 = k + max(s.id0, 0) * kv.sb * 2;
+        v0 = v + max(s.id0, 0) * vv.sb * 2;
+        k1 = k + max(s.id1, 0) * kv.sb * 2;
+        v1 = v + max(s.id1, 0) * vv.sb * 2;
+      } else {
+        if (left <= 0) {
+          id = walk.at(key >> p.page_log2);
+          left = (p.page - (key & (p.page - 1))) >> 5;
+          k0 = k + offset(kv, max(id, 0), key);
+          v0 = v + offset(vv, max(id, 0), key);
+        } else {
+          k0 += (int64_t)(64 * by) * kv.sn;
+          v0 += (int64_t)(64 * by) * vv.sn;
+        }
+        left -= by;
+        s.id0 = s.id1 = id;
+        rows0 = id < 0 ? 0 : min(limit - key, 32);
+      }
+    }
+    at += by;
+    return s;
+  }
+};
+// A wave's requests of rows of a step: chunk i of its CHUNKS (every NW-th of the tile's) into `to`, from the half or the step that it lies in.
+template <int D, bool SMALL, int NW>
+struct Requests {
+  typedef Tile<D> T;
+  static constexpr int CHUNKS = T::chunks(32) / NW;
+  int second[CHUNKS], off[CHUNKS];
+  unsigned to[CHUNKS];
+  __device__ __forceinline__ Requests(const char *lds, int stride_bytes, int w, int lane) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int chunk = i * NW + w, first = chunk * T::ROWS_PER_CHUNK, row = first + lane / T::PIECES;
+      second[i] = first / 16;
+      off[i] = (SMALL ? row % 16 : row) * stride_bytes + (((lane % T::PIECES) ^ T::swz(row)) << 4);
+      to[i] = __builtin_amdgcn_readfirstlane(lds_offset(lds) + chunk * 1024);
+    }
+  }
+  __device__ __forceinline__ void operator()(const char *p0, const char *p1, int rows0, int rows1, int stride_bytes, int further) const {
+    const i32x4 r0 = rows_rsrc<D>(p0, rows0, stride_bytes), r1 = SMALL ? rows_rsrc<D>(p1, rows1, stride_bytes) : r0;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      i32x4 r = r0;
+      if (SMALL && second[i]) r = r1;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to[i] + further), "v"(off[i]), "s"(r) : "memory");
+    }
+  }
+};
+
+// Bytes of a slot's row from the pool's first (the head's part is in `base`).
+static __device__ __forceinline__ int64_t slot_offset(const Paged &p, const View &v, int id, int slot, int esz) {
+  return ((int64_t)id * v.sb + (int64_t)(slot & (p.page - 1)) * v.sn) * esz;
+}
 static __device__ __forceinline__ Step step_at(const Paged &p, PageWalk &walk, int key) {
   const int index = key >> p.page_log2;
   Step s{key, walk.at(index), -1};
   s.id1 = p.page > 16 ? s.id0 : index + 1 < p.max_pages ? walk.at(index + 1) : -1;
   return s;
-}
-// Bytes of a slot's row from the pool's first (the head's part is in `base`).
-static __device__ __forceinline__ int64_t slot_offset(const Paged &p, const View &v, int id, int slot, int esz) {
-  return ((int64_t)id * v.sb + (int64_t)(slot & (p.page - 1)) * v.sn) * esz;
 }
 // Logits of slots that this lane's row does not see.
 static __device__ __forceinline__ void mask_step(f32x16 &sc, const Step &s, int see, int all_see, int g) {
@@ -97,11 +176,114 @@ static __device__ __forceinline__ void mask_step(f32x16 &sc, const Step &s, int 
 static __device__ __forceinline__ float log_sum(float m, float l, float scale) { return l > 0.f ? m * scale + logf(l) : l == 0.f ? -INFINITY : l; }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
+// Steps of 32 slots that the rows of sequence b see, -1 where it has no rows or more than 32 of them.
+static __device__ __forceinline__ int few_steps(const Paged &p, int b) {
+  const NewRows n(p, b);
+  if (n.n <= 0 || n.n * p.G > 32) return -1;
+  const int held = p.held(b);
+  return ((p.causal ? max(min(held, held - n.all + n.n), 0) : held) + 31) / 32;
+}
+// Every sequence is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
+// ones do not take longer.  Those with several have a place for each range's sums, `wanted` at most.
+static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted) {
+  if (steps < 8) return steps < 0 ? 0 : 1;
+  // (the quotient of whole numbers below 2^42 is not rounded up to the next one)
+  return max(1, min(min(64, steps / 4), (int)((double)wanted * steps / all)));
+}
+// What a lane adds to the sums of the lanes up to it.
+static __device__ __forceinline__ int sum_upto(int x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+struct Share {
+  int b, n, range, place;     // sequence (-1: none), its ranges, this one, the place of its first range's sums
+  int places;                 // of all sequences
+};
+// Range x of all.  Up to 64 sequences are a lane each; of more a kernel has written the sums.
+static __device__ __forceinline__ Share share_of(const FwdArgs &a, int x, int lane) {
+  const Paged &p = a.p;
+  Share s{-1, 0, 0, 0, 0};
+  if (a.map) {
+    const int32_t *ranges = a.map, *places = a.map + p.B + 1;
+    s.places = places[p.B];
+    if (x >= ranges[p.B]) return s;
+    s.b = last_not_above(p.B, x, lane, [&](int b) { return ranges[b]; });
+    s.n = ranges[s.b + 1] - ranges[s.b];
+    s.place = places[s.b];
+    s.range = x - ranges[s.b];
+    return s;
+  }
+  const int steps = lane < p.B ? few_steps(p, lane) : -1;
+  double all = max(steps, 0);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+  const int n = ranges_of(steps, all, a.wanted), places = n > 1 ? n : 0, upto_places = sum_upto(places, lane), upto = sum_upto(n, lane);
+  s.places = __shfl(upto_places, 63);
+  const uint64_t found = __ballot(upto > x);
+  if (!found) return s;
+  s.b = __ffsll((long long)found) - 1;
+  s.n = __shfl(n, s.b);
+  s.place = __shfl(upto_places - places, s.b);
+  s.range = x - __shfl(upto - n, s.b);
+  return s;
+}
+// The share of a workgroup of the kernels of few rows.  It says what the places are for: the first of a sequence's, or (the x-th range's workgroup, of place x) that there is none.
+static __device__ __forceinline__ Share my_share(const FwdArgs &a, int lane) {
+  const int x = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
+  const Share s = share_of(a, x, lane);
+  if (threadIdx.x == 0 && a.wanted > 1) {
+    int32_t *heads = a.heads + (int64_t)hk * a.wanted * 2;
+    if (x < a.wanted && x >= s.places) heads[2 * x] = -1;
+    if (s.b >= 0 && s.n > 1) {
+      heads[2 * (s.place + s.range)] = s.range ? -1 : s.b;
+      heads[2 * (s.place + s.range) + 1] = s.n;
+    }
+  }
+  return s;
+}
+__global__ __launch_bounds__(1024) void paged_map_kernel(FwdArgs a) {
+  __shared__ double part[16];
+  __shared__ int sums[2][16];
+  const Paged &p = a.p;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  double all = 0.;
+  for (int b = threadIdx.x; b < p.B; b += 1024) all += max(few_steps(p, b), 0);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+  if (lane == 0) part[w] = all;
+  __syncthreads();
+  all = 0.;
+  for (int i = 0; i < 16; ++i) all += part[i];
+  int before[2] = {0, 0};
+  for (int b0 = 0; b0 < p.B; b0 += 1024) {
+    const int b = b0 + threadIdx.x, n = b < p.B ? ranges_of(few_steps(p, b), all, a.wanted) : 0, upto[2] = {sum_upto(n, lane), sum_upto(n > 1 ? n : 0, lane)};
+    __syncthreads();
+    if (lane == 63) {
+      sums[0][w] = upto[0];
+      sums[1][w] = upto[1];
+    }
+    __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+      int ahead = before[k];
+      for (int i = 0; i < 16; ++i) {
+        ahead += i < w ? sums[k][i] : 0;
+        before[k] += sums[k][i];
+      }
+      if (b < p.B) a.map[k * (p.B + 1) + b + 1] = ahead + upto[k];
+    }
+  }
+  if (threadIdx.x < 2) a.map[threadIdx.x * (p.B + 1)] = 0;
+}
+
 template <int D>
 static constexpr int image_bytes() { return 4 * 32 * D * 4; }
 // The sums of four waves that walked slots of one range: joined through LDS (`image`: 4 x 32 D values) and stored.
 template <int D, bool F32>
-__device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D / 32], float m, float l, char *lds, float (&stats)[2][4][32], int item, const RowsOf &row, int w, int lane) {
+__device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D / 32], float m, float l, char *lds, float (&stats)[2][4][32], int place, const RowsOf &row, int w, int lane) {
   constexpr int RB = D / 32, IMAGE = RB * 4 * 64;
   const int r = lane & 31, g = lane >> 5;
   const float c = a.scale_log2e;
@@ -130,8 +312,8 @@ __device__ __forceinline__ void join_waves(const FwdArgs &a, const f32x16 (&o)[D
 #pragma unroll
     for (int x4 = 0; x4 < 4; ++x4) y[x4] += image[i * IMAGE + (w * 4 + x4) * 64 + lane] * f;
   }
-  if (a.n_split > 1) {
-    const int64_t at = (int64_t)item * 32 + r;
+  if (place >= 0) {
+    const int64_t at = (int64_t)place * 32 + r;
 #pragma unroll
     for (int x4 = 0; x4 < 4; ++x4) *reinterpret_cast<f32x4 *>(a.po + at * D + 32 * w + 8 * x4 + 4 * g) = y[x4];
     if (w == 0 && g == 0) {
@@ -167,47 +349,40 @@ static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &
     for (int x = 0; x < 16; ++x) o[rb][x] *= f;
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void paged_few_kernel(FwdArgs a) {
+// A wave has 32 slots' keys and values in LDS, and asks for the next keys when it has read these, and for the next values likewise, so that one or the other is
+// always on its way; two workgroups to a CU.
+template <int D, bool SMALL>
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOT = 2 * TILE, REQUESTS = 2 * T::chunks(32);
-  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * SLOT];      // [wave][stage][k | v]; then [wave][register image]
-  static_assert(image_bytes<D>() <= 4 * 2 * SLOT, "the images fit the stages");
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), REQUESTS = T::chunks(32);
+  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TILE];      // [wave][k | v]; then [wave][register image]
+  static_assert(image_bytes<D>() <= 4 * 2 * TILE, "the images fit the stages");
   __shared__ float stats[2][4][32];
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / p.Hkv, hk = bh % p.Hkv;
+  const int hk = blockIdx.x % p.Hkv;
+  const Share share = my_share(a, lane);
+  const int b = __builtin_amdgcn_readfirstlane(share.b), n_split = __builtin_amdgcn_readfirstlane(share.n), range = __builtin_amdgcn_readfirstlane(share.range);
+  if (b < 0) return;
   const NewRows n(p, b);
-  if (n.n <= 0 || n.n * p.G > 32) return;
   const int held = p.held(b);
   const RowsOf row(p, n, held, hk, r);
   const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
   const int steps = (limit + 31) / 32;
-  int at = (int)((int64_t)range * steps / a.n_split) + w;
-  const int end = (int)((int64_t)(range + 1) * steps / a.n_split);
-  PageWalk walk(p, b, lane);
-  const char *kbase = a.k.p + hk * a.k.sh * 2, *vbase = a.v.p + hk * a.v.sh * 2;
+  Cursor<D, SMALL> cursor(a, b, hk, (int)((int64_t)range * steps / n_split) + w, (int)((int64_t)(range + 1) * steps / n_split), 4, limit, lane);
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
-  char *mine = lds + w * (2 * SLOT);
-  auto request = [&](const Step &s, int stage) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int id = i ? s.id1 : s.id0, key = s.key + 16 * i, rows = id < 0 ? 0 : min(limit - key, 16), page = max(id, 0);
-      char *to = mine + stage * SLOT + i * T::bytes(16);
-      request_rows<D, 16, 1>(rows_rsrc<D>(kbase + slot_offset(p, a.k, page, key, 2), rows, ksn), ksn, to, 0, lane);
-      request_rows<D, 16, 1>(rows_rsrc<D>(vbase + slot_offset(p, a.v, page, key, 2), rows, vsn), vsn, to + TILE, 0, lane);
-    }
-  };
-  Step now{};
-  if (at < end) {
-    now = step_at(p, walk, 32 * at);
-    request(now, 0);
+  char *mine = lds + w * (2 * TILE);
+  const Requests<D, SMALL, 1> keys(mine, ksn, 0, lane), values(mine + TILE, vsn, 0, lane);
+  Step now = cursor.next();
+  if (now.key >= 0) {
+    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
+    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
   }
   bf16x8 qf[KS];
   const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
-  const unsigned rows0 = T::rows_base(mine, lane), cols0 = T::cols_base(mine, lane);
+  const unsigned rows0 = T::rows_base(mine, lane), cols0 = T::cols_base(mine + TILE, lane);
   const float c = a.scale_log2e;
   float m = -INFINITY, mc = 0.f, l = 0.f;
   f32x16 o[RB];
@@ -215,25 +390,20 @@ __global__ __launch_bounds__(256) void paged_few_kernel(FwdArgs a) {
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
-  for (int stage = 0; at < end; stage ^= 1) {
-    Step next{};
-    at += 4;
-    if (at < end) {
-      next = step_at(p, walk, 32 * at);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the last step's reads of that stage are done)
-      request(next, stage ^ 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
-    const unsigned kt = rows0 + stage * SLOT, vt = cols0 + stage * SLOT;
+  while (now.key >= 0) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
     f32x16 sc;
 #pragma unroll
     for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mfma32(T::rows_at(kt, 0, ks), qf[ks], sc);
+    for (int ks = 0; ks < KS; ++ks) sc = mfma32(T::rows_at(rows0, 0, ks), qf[ks], sc);
+    const Step next = cursor.next();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // (the keys have been read)
+    // (behind the last step nothing is read, but as many requests are made: the waits count them)
+    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
     mask_step(sc, now, row.see, all_see, g);
     follow(sc, c, m, mc, l, o);
+    bf16x8 pb[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x8 pr;
@@ -242,13 +412,19 @@ __global__ __launch_bounds__(256) void paged_few_kernel(FwdArgs a) {
         pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
         l += pr[x];
       }
-      const bf16x8 pb = __builtin_convertvector(pr, bf16x8);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) o[rb] = mfma32(T::cols_at(vt, rb, 16 * u, TILE), pb, o[rb]);
+      pb[u] = __builtin_convertvector(pr, bf16x8);
     }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb] = mfma32(T::cols_at(cols0, rb, 16 * u), pb[u], o[rb]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
     now = next;
   }
-  join_waves<D, false>(a, o, m, l, lds, stats, blockIdx.x, row, w, lane);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (the stages become the images)
+  join_waves<D, false>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
 }
 
 // The same of fp32 tensors, which are split into pieces in registers: a slot's row of keys to a lane, eight rows of a column of the values.  Keys are asked for a
@@ -260,15 +436,17 @@ __global__ __launch_bounds__(256, 1) void paged_few_f32_kernel(FwdArgs a) {
   __shared__ float stats[2][4][32];
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int range = blockIdx.x % a.n_split, bh = blockIdx.x / a.n_split, b = bh / p.Hkv, hk = bh % p.Hkv;
+  const int hk = blockIdx.x % p.Hkv;
+  const Share share = my_share(a, lane);
+  const int b = __builtin_amdgcn_readfirstlane(share.b), n_split = __builtin_amdgcn_readfirstlane(share.n), range = __builtin_amdgcn_readfirstlane(share.range);
+  if (b < 0) return;
   const NewRows n(p, b);
-  if (n.n <= 0 || n.n * p.G > 32) return;
   const int held = p.held(b);
   const RowsOf row(p, n, held, hk, r);
   const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
   const int steps = (limit + 31) / 32;
-  int at = (int)((int64_t)range * steps / a.n_split) + w;
-  const int end = (int)((int64_t)(range + 1) * steps / a.n_split);
+  int at = (int)((int64_t)range * steps / n_split) + w;
+  const int end = (int)((int64_t)(range + 1) * steps / n_split);
   PageWalk walk(p, b, lane);
   const char *kbase = a.k.p + (hk * a.k.sh + 8 * g) * 4, *vbase = a.v.p + (hk * a.v.sh + r) * 4;
   const f32x4 none = {0.f, 0.f, 0.f, 0.f};
@@ -349,7 +527,7 @@ __global__ __launch_bounds__(256, 1) void paged_few_f32_kernel(FwdArgs a) {
     }
     now = next;
   }
-  join_waves<D, true>(a, o, m, l, lds, stats, blockIdx.x, row, w, lane);
+  join_waves<D, true>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
 }
 
 // ---- tiles of rows ---------------------------------------------------------------------------------------------------
@@ -416,10 +594,10 @@ __device__ __forceinline__ void store_partial(const FwdArgs &a, const f32x16 (&o
 // bf16: 32 slots to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next slots under the exponentials of its own,
 // then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work of one wave at the same time, and of two
 // with two workgroups to a CU.
-template <int D>
+template <int D, bool SMALL>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOTS = 4, AHEAD = 3, CHUNKS = T::chunks(32) / 4, REQUESTS = 2 * CHUNKS;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOTS = 4, AHEAD = 3, REQUESTS = 2 * T::chunks(32) / 4;
   constexpr auto k_at = [](int step) { return step % SLOTS * 2 * TILE; };
   constexpr auto v_at = [](int step) { return step % SLOTS * 2 * TILE + TILE; };
   __shared__ __attribute__((aligned(1024))) char lds[SLOTS * 2 * TILE];
@@ -438,36 +616,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
   const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
   const int steps = (limit + 31) / 32, end = (int)((int64_t)(tile.range + 1) * steps / a.n_split);
-  int at = (int)((int64_t)tile.range * steps / a.n_split);
-  PageWalk walk(p, b, lane);
-  const char *kbase = a.k.p + hk * a.k.sh * 2, *vbase = a.v.p + hk * a.v.sh * 2;
+  Cursor<D, SMALL> cursor(a, b, hk, (int)((int64_t)tile.range * steps / a.n_split), end, 1, limit, lane);
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
-  auto next_step = [&]() {
-    Step s{-1, -1, -1};
-    if (at < end) s = step_at(p, walk, 32 * at);
-    ++at;
+  const Requests<D, SMALL, 4> keys(lds, ksn, w, lane), values(lds + TILE, vsn, w, lane);
+  // (behind the last step nothing is read, but as many requests are made: the waits count them)
+  auto request = [&](int step) {
+    const Step s = cursor.next();
+    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, k_at(step));
+    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, k_at(step));
     return s;
   };
-  // (behind the last step zeros are requested: every step has as many requests, which is what the waits count)
-  int line[CHUNKS], off_k[CHUNKS], off_v[CHUNKS];      // a chunk's place: its half's 16 slots, this lane's row and piece
-#pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) {
-    const int first = (4 * i + w) * T::ROWS_PER_CHUNK, row_ = first + lane / T::PIECES;
-    line[i] = first / 16;
-    off_k[i] = (row_ % 16) * ksn + (((lane % T::PIECES) ^ T::swz(row_)) << 4);
-    off_v[i] = (row_ % 16) * vsn + (((lane % T::PIECES) ^ T::swz(row_)) << 4);
-  }
-  auto request = [&](const Step &s, int step) {
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      const int id = line[i] ? s.id1 : s.id0, key = max(s.key, 0) + 16 * line[i], rows = id < 0 ? 0 : min(limit - key, 16), page = max(id, 0);
-      const unsigned to = __builtin_amdgcn_readfirstlane(lds_offset(lds) + k_at(step) + (4 * i + w) * 1024);
-      const i32x4 kr = rows_rsrc<D>(kbase + slot_offset(p, a.k, page, key, 2), rows, ksn), vr = rows_rsrc<D>(vbase + slot_offset(p, a.v, page, key, 2), rows, vsn);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off_k[i]), "s"(kr) : "memory");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + TILE), "v"(off_v[i]), "s"(vr) : "memory");
-    }
-  };
-  Step s0 = next_step(), s1 = next_step(), s2 = next_step();
   const float c = a.scale_log2e;
   float m = -INFINITY, top = -INFINITY, l = 0.f;      // what the sums are expressed against, the largest logit and the sum of weights (this lane's slots)
   f32x16 o[RB];
@@ -475,10 +633,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
+  Step s0 = request(0), s1 = request(1), s2 = request(2);
   if (s0.key >= 0) {
-    request(s0, 0);
-    request(s1, 1);
-    request(s2, 2);
     bf16x8 qf[KS];
     const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
 #pragma unroll
@@ -538,8 +694,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
       bf16x8 kf[KS], vf[2 * RB], pb[2];
       kf[0] = read_k(next, 0);
       kf[1] = read_k(next, 1);
-      const Step further = next_step();
-      request(further, now + AHEAD);
+      const Step further = request(now + AHEAD);
       constexpr int PER = 16 / KS;         // logits to a product: 2 at d = 128, 4 at d = 64
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -583,8 +738,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
       step(s_b, s_a, std::integral_constant<int, 3>{});
       if (s0.key < 0) break;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   l = xhalf_sum(l);
   if (a.n_split > 1) {
     store_partial<D>(a, o, m, l, item, w, lane);
@@ -728,24 +883,28 @@ __global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
   constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, c4 = 4 * (lane % LPR);
-  const int line = __builtin_amdgcn_readfirstlane(blockIdx.x % (ROWS / 4) * 4 + (threadIdx.x >> 6)), group = blockIdx.x / (ROWS / 4);
-  int b, hk, R, n_rows;
+  const int blocks = ROWS == 32 ? a.line_blocks : ROWS / 4, line = __builtin_amdgcn_readfirstlane(blockIdx.x % blocks * 4 + (threadIdx.x >> 6)), group = blockIdx.x / blocks;
+  int b, hk, R, n_rows, n_split;
+  int64_t at0;                // place of the row in the first range's sums; range i's: at0 + i ROWS
   if constexpr (ROWS == 32) {
-    b = group / p.Hkv;
-    hk = group % p.Hkv;
+    hk = group / a.wanted;
+    b = a.heads[2 * group];
+    n_split = a.heads[2 * group + 1];
+    if (b < 0) return;
     R = line;
     n_rows = NewRows(p, b).n * p.G;
-    if (n_rows > 32) return;
+    at0 = (int64_t)group * ROWS + line;
   } else {
     const TileOf tile(p, a, (unsigned)group * a.n_split, lane);
     b = tile.b;
     hk = tile.hk;
     R = tile.row0 + line;
     n_rows = tile.n_rows;
+    n_split = a.n_split;
+    at0 = (int64_t)group * n_split * ROWS + line;
   }
   if (R >= n_rows) return;
-  const bool has = lane < a.n_split;
-  const int64_t at0 = (int64_t)group * a.n_split * ROWS + line;      // range i: at0 + i ROWS
+  const bool has = lane < n_split;
   const float mi = has ? a.pm[at0 + (int64_t)lane * ROWS] : -INFINITY;
   float m = mi;
 #pragma unroll
@@ -755,18 +914,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < a.n_split; i0 += 4 * AT_ONCE) {
+  for (int i0 = 0; i0 < n_split; i0 += 4 * AT_ONCE) {
     f32x4 x[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int i = min(i0 + u * AT_ONCE + lane / LPR, a.n_split - 1);
+      const int i = min(i0 + u * AT_ONCE + lane / LPR, n_split - 1);
       x[u] = *reinterpret_cast<const f32x4 *>(a.po + (at0 + (int64_t)i * ROWS) * D + c4);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int i = i0 + u * AT_ONCE + lane / LPR;
       const float fi = __shfl(f, min(i, 63));
-      if (i < a.n_split) o += x[u] * fi;
+      if (i < n_split) o += x[u] * fi;
     }
   }
 #pragma unroll
@@ -783,78 +942,93 @@ __global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
   else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(a.out.p) + to) = __builtin_convertvector(o, bf16x4);
 }
 
-struct Part {
-  bool runs;
-  int n_split, groups;
-  size_t off_po, off_pm, off_pl;
+struct Sums {
+  size_t po, pm, pl, heads;   // offsets
 };
 struct FwdPlan {
-  Part few, tile;
-  size_t total;
+  bool few, tile;             // which launches there are
+  int wanted, n_split, groups;      // few: see FwdArgs; tile: ranges, tiles of all key heads
+  Sums few_sums, tile_sums;
+  bool map;                   // few: more than 64 sequences
+  size_t off_map, total;
 };
 
 FwdPlan plan_forward(const ha_paged_problem &p) {
   FwdPlan f{};
   const int64_t G = p.H / p.H_kv, steps = ((int64_t)p.max_pages * p.page + 31) / 32;
-  f.few.runs = p.T > 0 && p.max_new > 0 && (p.max_new * G <= 32 || p.q_offset);
-  f.tile.runs = p.max_new * G > 32;
+  f.few = p.T > 0 && p.max_new > 0 && (p.max_new * G <= 32 || p.q_offset);
+  f.tile = p.max_new * G > 32;
   size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t here = at;
-    at += round256(bytes);
-    return here;
+  auto take = [&](size_t places, int rows) {
+    Sums s;
+    s.po = at;
+    at += round256(places * rows * p.d_head * 4);
+    s.pm = at;
+    at += round256(places * rows * 4);
+    s.pl = at;
+    at += round256(places * rows * 4);
+    s.heads = at;
+    if (rows == 32) at += round256(places * 8);
+    return s;
   };
-  // Parts until every CU has a workgroup that keeps `least` steps of 32 slots; tiles: two workgroups where each keeps 64.
-  auto split = [&](Part &part, int64_t groups, int64_t least, int rows) {
-    part.groups = (int)groups;
-    int64_t parts = groups > 0 ? std::min(256 / groups, steps / least) : 1;
-    if (rows == 128 && groups > 0) parts = std::max(parts, std::min(512 / groups, steps / (p.dtype == HA_F32 ? 4 : 64)));
-    part.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
-    if (part.runs && part.n_split > 1) {
-      const size_t n = (size_t)groups * part.n_split * rows;
-      part.off_po = take(n * p.d_head * 4);
-      part.off_pm = take(n * 4);
-      part.off_pl = take(n * 4);
-    }
-  };
-  split(f.few, (int64_t)p.B * p.H_kv, 4, 32);
-  split(f.tile, (p.T * G / 128 + p.B) * p.H_kv, 8, 128);
+  f.wanted = steps >= 8 ? std::max(1, 512 / p.H_kv) : 1;
+  if (f.few && f.wanted > 1) f.few_sums = take((size_t)f.wanted * p.H_kv, 32);
+  if ((f.map = f.few && p.B > 64)) {
+    f.off_map = at;
+    at += round256((size_t)(p.B + 1) * 8);
+  }
+  // Parts until every CU has a workgroup that keeps eight steps of 32 slots; two workgroups where each keeps 64 (fp32: 4).
+  const int64_t groups = (p.T * G / 128 + p.B) * p.H_kv;
+  int64_t parts = std::max(std::min(256 / groups, steps / 8), std::min(512 / groups, steps / (p.dtype == HA_F32 ? 4 : 64)));
+  f.groups = (int)groups;
+  f.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
+  if (f.tile && f.n_split > 1) f.tile_sums = take((size_t)groups * f.n_split, 128);
   f.total = at;
   return f;
 }
 
 template <int D, bool F32, int ROWS>
 hipError_t launch_join(const FwdArgs &a, int groups, hipStream_t st) {
-  paged_join_kernel<D, F32, ROWS><<<(unsigned)groups * (ROWS / 4), 256, 0, st>>>(a);
+  paged_join_kernel<D, F32, ROWS><<<(unsigned)groups * (ROWS == 32 ? a.line_blocks : ROWS / 4), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 template <int D, bool F32>
 hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st) {
   hipError_t e = hipSuccess;
-  auto part = [&](const Part &x) {
-    a.n_split = x.n_split;
-    a.po = reinterpret_cast<float *>(ws + x.off_po);
-    a.pm = reinterpret_cast<float *>(ws + x.off_pm);
-    a.pl = reinterpret_cast<float *>(ws + x.off_pl);
+  auto sums = [&](const Sums &x) {
+    a.po = reinterpret_cast<float *>(ws + x.po);
+    a.pm = reinterpret_cast<float *>(ws + x.pm);
+    a.pl = reinterpret_cast<float *>(ws + x.pl);
+    a.heads = reinterpret_cast<int32_t *>(ws + x.heads);
   };
-  if (f.tile.runs) {
-    part(f.tile);
-    a.leave_few = f.few.runs;
-    a.tiles = f.tile.groups / a.p.Hkv;
-    a.items = (unsigned)f.tile.groups * f.tile.n_split;
+  if (f.tile) {
+    sums(f.tile_sums);
+    a.n_split = f.n_split;
+    a.leave_few = f.few;
+    a.tiles = f.groups / a.p.Hkv;
+    a.items = (unsigned)f.groups * f.n_split;
     a.share = xcd_share(a.items);
     if constexpr (F32) paged_tile_f32_kernel<D><<<8 * a.share, 256, 0, st>>>(a);
-    else paged_tile_kernel<D><<<8 * a.share, 256, 0, st>>>(a);
+    else if (a.p.page == 16) paged_tile_kernel<D, true><<<8 * a.share, 256, 0, st>>>(a);
+    else paged_tile_kernel<D, false><<<8 * a.share, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.n_split > 1 && (e = launch_join<D, F32, 128>(a, f.tile.groups, st)) != hipSuccess) return e;
+    if (f.n_split > 1 && (e = launch_join<D, F32, 128>(a, f.groups, st)) != hipSuccess) return e;
   }
-  if (f.few.runs) {
-    part(f.few);
-    const unsigned n = (unsigned)f.few.groups * f.few.n_split;
+  if (f.few) {
+    sums(f.few_sums);
+    a.wanted = f.wanted;
+    a.line_blocks = (std::min(32, a.p.max_new * a.p.G) + 3) / 4;
+    a.map = f.map ? reinterpret_cast<int32_t *>(ws + f.off_map) : nullptr;
+    if (f.map) {
+      paged_map_kernel<<<1, 1024, 0, st>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    const unsigned n = (unsigned)(f.wanted + a.p.B) * a.p.Hkv;      // (ranges of all sequences: their shares rounded down, or one)
     if constexpr (F32) paged_few_f32_kernel<D><<<n, 256, 0, st>>>(a);
-    else paged_few_kernel<D><<<n, 256, 0, st>>>(a);
+    else if (a.p.page == 16) paged_few_kernel<D, true><<<n, 256, 0, st>>>(a);
+    else paged_few_kernel<D, false><<<n, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.n_split > 1) e = launch_join<D, F32, 32>(a, f.few.groups, st);
+    if (f.wanted > 1) e = launch_join<D, F32, 32>(a, f.wanted * a.p.Hkv, st);
   }
   return e;
 }

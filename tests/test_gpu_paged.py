@@ -156,6 +156,19 @@ def test_many_sequences_and_a_split_long_one():
     check(cache(12, [5000], [140], H=3, Hkv=1, page=64))
 
 
+@pytest.mark.parametrize("dtype,d,page", [(BF, 64, 16), (F32, 64, 32)])
+@pytest.mark.parametrize("B", [65, 1100])
+def test_more_sequences_than_a_wave_has_lanes(B, dtype, d, page):
+    """One long sequence among short and empty ones, single tokens and chunks; B = 1100 is more than the sums over sequences take at once."""
+    gen = torch.Generator().manual_seed(B)
+    lengths, new = torch.randint(0, 60, (B,), generator=gen).tolist(), torch.randint(0, 3, (B,), generator=gen).tolist()
+    lengths[B // 2], new[B // 2], lengths[-1], new[-1] = 3000, 1, 1500, 1
+    check(cache(B, lengths, new, H=2, Hkv=1, d=d, dtype=dtype, page=page))
+    if B == 65:
+        new[3], lengths[3] = 70, 90
+        check(cache(B, lengths, new, H=2, Hkv=1, d=d, dtype=dtype, page=page))
+
+
 def test_values_that_are_not_finite_stay_in_their_slots():
     """An infinite value under a weight shows in the rows that see it, and no row of another sequence."""
     c = cache(13, [100, 100], [1, 1], page=32)
@@ -223,10 +236,10 @@ def test_append_as_it_is():
 
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64), (F32, 128)])
 @pytest.mark.parametrize("keep,first,last", [(1, 0, 0), (1, 1, 0), (40, 4, 8), (100, 0, 100), (64, 64, 0), (130, 1, 2), (1000, 3, 3)])
-@pytest.mark.parametrize("kind", ["many", "few"])
-def test_evict(keep, first, last, dtype, d, kind):
-    """Weights of many values, and of three with NaN, infinities and both zeros among them: ties go to the lower slot."""
-    c = cache(16, [300, 0, 39, 1, 129, 300], [0] * 6, Hkv=3, d=d, dtype=dtype, spare=6 * 65, layout="bnhd" if d == 64 else "bhnd")
+@pytest.mark.parametrize("kind,max_pages", [("many", None), ("few", None), ("few", 600)])
+def test_evict(keep, first, last, dtype, d, kind, max_pages):
+    """Weights of many values, and of few with NaN, infinities and both zeros among them: ties go to the lower slot.  Tables of more than 8192 slots are chosen from in another way."""
+    c = cache(16, [300, 0, 39, 1, 129, 300], [0] * 6, Hkv=3, d=d, dtype=dtype, spare=6 * 65, layout="bnhd" if d == 64 else "bhnd", max_pages=max_pages)
     w = c["where"]
     slots = w["page_table"].shape[1] * 16
     x = torch.randn((6, 3, slots), generator=c["gen"])
@@ -245,17 +258,17 @@ def test_evict(keep, first, last, dtype, d, kind):
         assert torch.equal(a.cpu().nan_to_num(9.0, 8.0, 7.0), b.nan_to_num(9.0, 8.0, 7.0)), name
 
 
-def test_evict_a_long_sequence():
-    gen = torch.Generator().manual_seed(17)
-    n, keep, page = 20011, 15003, 128
+@pytest.mark.parametrize("n,keep,values", [(20011, 15003, 1000), (70001, 123, 10 ** 9), (9000, 8999, 1), (8192, 5000, 3)])
+def test_evict_a_long_sequence(n, keep, values):
+    gen, page = torch.Generator().manual_seed(17), 128
     pages, width = -(-n // page), -(-keep // page)
     k = torch.randn(pages + width, 1, page, 64, generator=gen).bfloat16().cuda()
     v, table = k.flip(0).contiguous(), torch.arange(pages, dtype=torch.int32, device="cuda")[None]
-    weights = torch.rand(1, 1, pages * page, generator=gen).mul(1000).floor().cuda()      # many ties
+    weights = torch.rand(1, 1, pages * page, generator=gen).mul(values).floor().cuda()      # ties, and nothing but ties
     length, out, kept = ha.hybrid_attn_paged_evict(k, v, weights, table, torch.tensor([n], dtype=torch.int32, device="cuda"), keep,
-                                                   torch.arange(pages, pages + width, dtype=torch.int32, device="cuda")[None], 100, 200)
+                                                   torch.arange(pages, pages + width, dtype=torch.int32, device="cuda")[None], 10, 100)
     score = weights[0, 0, :n].clone()
-    score[:100] = score[n - 200:] = math.inf
+    score[:10] = score[n - 100:] = math.inf
     want = torch.sort(score, descending=True, stable=True).indices[:keep].sort().values
     assert int(length) == keep and torch.equal(kept[0, 0].long(), want) and torch.equal(out[0, 0, :keep], weights[0, 0, want]) and not out[0, 0, keep:].any()
     for pool in (k, v):
