@@ -47,6 +47,9 @@ ha_status check_pool(const ha_paged_problem &p, const ha_view *v, bool written, 
 
 namespace {
 
+// The first step of range i of n, n <= 64 (of 2^25 steps at most: the product fits 32 bits).
+static __device__ __forceinline__ int part_of(int i, int steps, int n) { return (int)((unsigned)i * (unsigned)steps / (unsigned)n); }
+
 struct FwdArgs {
   Paged p;
   View q, k, v, out;
@@ -80,7 +83,7 @@ struct Step {
 };
 // Walks the slots of a sequence for one key head, 32 at a time, steps at .. end - 1 with a distance of `by`.  SMALL: pages of 16 slots, two to a step; otherwise a step lies in one
 // page, and a step next to the last one is as far from it in memory as its slots are.
-template <int D, bool SMALL>
+template <int ESZ, bool SMALL>
 struct Cursor {
   const Paged &p;
   PageWalk walk;
@@ -90,8 +93,8 @@ struct Cursor {
   const char *k0, *v0, *k1, *v1;
   int rows0, rows1;           // that someone sees of the step (SMALL: of its halves)
   __device__ __forceinline__ Cursor(const FwdArgs &a, int b, int hk, int at_, int end_, int by_, int limit_, int lane)
-      : p(a.p), walk(a.p, b, lane), at(at_), end(end_), by(by_), limit(limit_), left(0), id(-1), k(a.k.p + hk * a.k.sh * 2), v(a.v.p + hk * a.v.sh * 2), kv(a.k), vv(a.v), k0(k), v0(v), k1(k), v1(v), rows0(0), rows1(0) {}
-  __device__ __forceinline__ int64_t offset(const View &x, int page, int slot) const { return (page * x.sb + (int64_t)(slot & (p.page - 1)) * x.sn) * 2; }
+      : p(a.p), walk(a.p, b, lane), at(at_), end(end_), by(by_), limit(limit_), left(0), id(-1), k(a.k.p + hk * a.k.sh * ESZ), v(a.v.p + hk * a.v.sh * ESZ), kv(a.k), vv(a.v), k0(k), v0(v), k1(k), v1(v), rows0(0), rows1(0) {}
+  __device__ __forceinline__ int64_t offset(const View &x, int page, int slot) const { return (page * x.sb + (int64_t)(slot & (p.page - 1)) * x.sn) * ESZ; }
   __device__ __forceinline__ Step next() {
     Step s{-1, -1, -1};
     rows0 = rows1 = 0;
@@ -104,10 +107,10 @@ struct Cursor {
         s.id1 = index + 1 < p.max_pages ? walk.at(index + 1) : -1;
         rows0 = s.id0 < 0 ? 0 : min(limit - key, 16);
         rows1 = s.id1 < 0 ? 0 : min(limit - key - 16, 16);
-        k0 = k + max(s.id0, 0) * kv.sb * 2;
-        v0 = v + max(s.id0, 0) * vv.sb * 2;
-        k1 = k + max(s.id1, 0) * kv.sb * 2;
-        v1 = v + max(s.id1, 0) * vv.sb * 2;
+        k0 = k + max(s.id0, 0) * kv.sb * ESZ;
+        v0 = v + max(s.id0, 0) * vv.sb * ESZ;
+        k1 = k + max(s.id1, 0) * kv.sb * ESZ;
+        v1 = v + max(s.id1, 0) * vv.sb * ESZ;
       } else {
         if (left <= 0) {
           id = walk.at(key >> p.page_log2);
@@ -115,8 +118,8 @@ struct Cursor {
           k0 = k + offset(kv, max(id, 0), key);
           v0 = v + offset(vv, max(id, 0), key);
         } else {
-          k0 += (int64_t)(64 * by) * kv.sn;
-          v0 += (int64_t)(64 * by) * vv.sn;
+          k0 += (int64_t)(32 * ESZ * by) * kv.sn;
+          v0 += (int64_t)(32 * ESZ * by) * vv.sn;
         }
         left -= by;
         s.id0 = s.id1 = id;
@@ -127,10 +130,10 @@ struct Cursor {
     return s;
   }
 };
-// A wave's requests of rows of a step: chunk i of its CHUNKS (every NW-th of the tile's) into `to`, from the half or the step that it lies in.
-template <int D, bool SMALL, int NW>
+// A wave's requests of rows of a step (2 W bytes each): chunk i of its CHUNKS (every NW-th of the tile's) into `to`, from the half or the step that it lies in.
+template <int W, bool SMALL, int NW>
 struct Requests {
-  typedef Tile<D> T;
+  typedef Tile<W> T;
   static constexpr int CHUNKS = T::chunks(32) / NW;
   int second[CHUNKS], off[CHUNKS];
   unsigned to[CHUNKS];
@@ -144,7 +147,7 @@ struct Requests {
     }
   }
   __device__ __forceinline__ void operator()(const char *p0, const char *p1, int rows0, int rows1, int stride_bytes, int further) const {
-    const i32x4 r0 = rows_rsrc<D>(p0, rows0, stride_bytes), r1 = SMALL ? rows_rsrc<D>(p1, rows1, stride_bytes) : r0;
+    const i32x4 r0 = rows_rsrc<W>(p0, rows0, stride_bytes), r1 = SMALL ? rows_rsrc<W>(p1, rows1, stride_bytes) : r0;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       i32x4 r = r0;
@@ -183,10 +186,12 @@ static __device__ __forceinline__ int few_steps(const Paged &p, int b) {
   const int held = p.held(b);
   return ((p.causal ? max(min(held, held - n.all + n.n), 0) : held) + 31) / 32;
 }
-// Every sequence is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
+// One token of 12 heads, d = 128: 500 slots uncut 9.1 us, in four ranges 10.0 with the join; 1000 slots 10.9 and 10.1.
+constexpr int kSplitFrom = 32;
+// Every sequence of as many steps is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
 // ones do not take longer.  Those with several have a place for each range's sums, `wanted` at most.
 static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted) {
-  if (steps < 8) return steps < 0 ? 0 : 1;
+  if (steps < kSplitFrom) return steps < 0 ? 0 : 1;
   // (the quotient of whole numbers below 2^42 is not rounded up to the next one)
   return max(1, min(min(64, steps / 4), (int)((double)wanted * steps / all)));
 }
@@ -350,11 +355,12 @@ static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &
 }
 
 // A wave has 32 slots' keys and values in LDS, and asks for the next keys when it has read these, and for the next values likewise, so that one or the other is
-// always on its way; two workgroups to a CU.
-template <int D, bool SMALL>
-__global__ __launch_bounds__(256, 2) void paged_few_kernel(FwdArgs a) {
-  typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), REQUESTS = T::chunks(32);
+// always on its way; two workgroups to a CU (fp32, whose rows are split into pieces behind LDS: one).
+template <int D, bool F32, bool SMALL>
+__global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
+  constexpr int ESZ = F32 ? 4 : 2, W = D * ESZ / 2, KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1;      // W: a row in twos of bytes
+  typedef Tile<W> T;
+  constexpr int TILE = T::bytes(32), REQUESTS = T::chunks(32);
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TILE];      // [wave][k | v]; then [wave][register image]
   static_assert(image_bytes<D>() <= 4 * 2 * TILE, "the images fit the stages");
   __shared__ float stats[2][4][32];
@@ -369,20 +375,44 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(FwdArgs a) {
   const RowsOf row(p, n, held, hk, r);
   const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
   const int steps = (limit + 31) / 32;
-  Cursor<D, SMALL> cursor(a, b, hk, (int)((int64_t)range * steps / n_split) + w, (int)((int64_t)(range + 1) * steps / n_split), 4, limit, lane);
-  const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
+  Cursor<ESZ, SMALL> cursor(a, b, hk, part_of(range, steps, n_split) + w, part_of(range + 1, steps, n_split), 4, limit, lane);
+  const int ksn = (int)a.k.sn * ESZ, vsn = (int)a.v.sn * ESZ;
   char *mine = lds + w * (2 * TILE);
-  const Requests<D, SMALL, 1> keys(mine, ksn, 0, lane), values(mine + TILE, vsn, 0, lane);
+  const Requests<W, SMALL, 1> keys(mine, ksn, 0, lane), values(mine + TILE, vsn, 0, lane);
   Step now = cursor.next();
   if (now.key >= 0) {
     keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
     values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
   }
-  bf16x8 qf[KS];
-  const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
+  bf16x8 qf[KS][NS];
+  const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * ESZ;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+  for (int ks = 0; ks < KS; ++ks) {
+    if constexpr (F32) split8_cut(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
+    else qf[ks][0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
+  }
   const unsigned rows0 = T::rows_base(mine, lane), cols0 = T::cols_base(mine + TILE, lane);
+  auto key_piece = [&](int ks, bf16x8 (&kf)[NS]) {
+    if constexpr (F32) {      // eight columns of the lane's row: two pieces of 16 bytes
+      const char *line = mine + r * T::PITCH;
+      split8_cut(*reinterpret_cast<const f32x4 *>(line + (((4 * ks + 2 * g) ^ T::swz(r)) << 4)), *reinterpret_cast<const f32x4 *>(line + (((4 * ks + 2 * g + 1) ^ T::swz(r)) << 4)), kf);
+    } else {
+      kf[0] = T::rows_at(rows0, 0, ks);
+    }
+  };
+  auto value_piece = [&](int rb, int u, bf16x8 (&vf)[NS]) {
+    if constexpr (F32) {      // eight rows of the lane's column
+      f32x8 x;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int line = crow(8 * u + y, g);
+        x[y] = *reinterpret_cast<const float *>(mine + TILE + line * T::PITCH + (((8 * rb + (r >> 2)) ^ T::swz(line)) << 4) + (r & 3) * 4);
+      }
+      split8_cut(__builtin_shufflevector(x, x, 0, 1, 2, 3), __builtin_shufflevector(x, x, 4, 5, 6, 7), vf);
+    } else {
+      vf[0] = T::cols_at(cols0, rb, 16 * u);
+    }
+  };
   const float c = a.scale_log2e;
   float m = -INFINITY, mc = 0.f, l = 0.f;
   f32x16 o[RB];
@@ -396,14 +426,18 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(FwdArgs a) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mfma32(T::rows_at(rows0, 0, ks), qf[ks], sc);
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 kf[NS];
+      key_piece(ks, kf);
+      sc = mfma_split<NS>(kf, qf[ks], sc);
+    }
     const Step next = cursor.next();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // (the keys have been read)
     // (behind the last step nothing is read, but as many requests are made: the waits count them)
     keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
     mask_step(sc, now, row.see, all_see, g);
     follow(sc, c, m, mc, l, o);
-    bf16x8 pb[2];
+    bf16x8 pb[2][NS];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x8 pr;
@@ -412,122 +446,23 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(FwdArgs a) {
         pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
         l += pr[x];
       }
-      pb[u] = __builtin_convertvector(pr, bf16x8);
+      split8<NS>(pr, pb[u]);
     }
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) o[rb] = mfma32(T::cols_at(cols0, rb, 16 * u), pb[u], o[rb]);
+      for (int rb = 0; rb < RB; ++rb) {
+        bf16x8 vf[NS];
+        value_piece(rb, u, vf);
+        o[rb] = mfma_split<NS>(vf, pb[u], o[rb]);
+      }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
     now = next;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (the stages become the images)
-  join_waves<D, false>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
-}
-
-// The same of fp32 tensors, which are split into pieces in registers: a slot's row of keys to a lane, eight rows of a column of the values.  Keys are asked for a
-// step ahead.
-template <int D>
-__global__ __launch_bounds__(256, 1) void paged_few_f32_kernel(FwdArgs a) {
-  constexpr int KS = D / 16, RB = D / 32;
-  __shared__ __attribute__((aligned(1024))) char lds[image_bytes<D>()];
-  __shared__ float stats[2][4][32];
-  const Paged &p = a.p;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int hk = blockIdx.x % p.Hkv;
-  const Share share = my_share(a, lane);
-  const int b = __builtin_amdgcn_readfirstlane(share.b), n_split = __builtin_amdgcn_readfirstlane(share.n), range = __builtin_amdgcn_readfirstlane(share.range);
-  if (b < 0) return;
-  const NewRows n(p, b);
-  const int held = p.held(b);
-  const RowsOf row(p, n, held, hk, r);
-  const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
-  const int steps = (limit + 31) / 32;
-  int at = (int)((int64_t)range * steps / n_split) + w;
-  const int end = (int)((int64_t)(range + 1) * steps / n_split);
-  PageWalk walk(p, b, lane);
-  const char *kbase = a.k.p + (hk * a.k.sh + 8 * g) * 4, *vbase = a.v.p + (hk * a.v.sh + r) * 4;
-  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-  f32x4 kr[KS][2];
-  auto request = [&](const Step &s) {      // (zeros for slots that nobody sees)
-    const int id = r < 16 ? s.id0 : s.id1;
-    const bool there = id >= 0 && s.key + r < limit;
-    const float *x = reinterpret_cast<const float *>(kbase + (there ? slot_offset(p, a.k, id, s.key + r, 4) : 0));
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) kr[ks][i] = there ? *reinterpret_cast<const f32x4 *>(x + 16 * ks + 4 * i) : none;
-  };
-  Step now{};
-  if (at < end) {
-    now = step_at(p, walk, 32 * at);
-    request(now);
-  }
-  bf16x8 qf[KS][3];
-  const float *qp = reinterpret_cast<const float *>(a.q.p) + row.h * a.q.sh + row.token * a.q.sn + 8 * g;
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(qp + 16 * ks), *reinterpret_cast<const f32x4 *>(qp + 16 * ks + 4), qf[ks]);
-  const float c = a.scale_log2e;
-  float m = -INFINITY, mc = 0.f, l = 0.f;
-  f32x16 o[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
-  while (at < end) {
-    float vr[2][RB][8];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int id = u ? now.id1 : now.id0;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int slot = now.key + crow(8 * u + x, g);
-        const bool there = id >= 0 && slot < limit;
-        const float *y = reinterpret_cast<const float *>(vbase + (there ? slot_offset(p, a.v, id, slot, 4) : 0));
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) vr[u][rb][x] = there ? y[32 * rb] : 0.f;
-      }
-    }
-    f32x16 sc;
-#pragma unroll
-    for (int x = 0; x < 16; ++x) sc[x] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      bf16x8 kf[3];
-      split8_any(kr[ks][0], kr[ks][1], kf);
-      sc = mfma_split<3>(kf, qf[ks], sc);
-    }
-    Step next{};
-    at += 4;
-    if (at < end) {
-      next = step_at(p, walk, 32 * at);
-      request(next);
-    }
-    mask_step(sc, now, row.see, all_see, g);
-    follow(sc, c, m, mc, l, o);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x8 pr;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
-        l += pr[x];
-      }
-      bf16x8 pb[3];
-      split8<3>(pr, pb);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const float(&v)[8] = vr[u][rb];
-        bf16x8 vf[3];
-        split8_any(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]}, vf);
-        o[rb] = mfma_split<3>(vf, pb, o[rb]);
-      }
-    }
-    now = next;
-  }
-  join_waves<D, true>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
+  join_waves<D, F32>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
 }
 
 // ---- tiles of rows ---------------------------------------------------------------------------------------------------
@@ -615,8 +550,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   const int last = min(tile.row0 + 127, tile.n_rows - 1) / p.G;      // the tile's last token
   const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
   const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
-  const int steps = (limit + 31) / 32, end = (int)((int64_t)(tile.range + 1) * steps / a.n_split);
-  Cursor<D, SMALL> cursor(a, b, hk, (int)((int64_t)tile.range * steps / a.n_split), end, 1, limit, lane);
+  const int steps = (limit + 31) / 32, end = part_of(tile.range + 1, steps, a.n_split);
+  Cursor<2, SMALL> cursor(a, b, hk, part_of(tile.range, steps, a.n_split), end, 1, limit, lane);
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
   const Requests<D, SMALL, 4> keys(lds, ksn, w, lane), values(lds + TILE, vsn, w, lane);
   // (behind the last step nothing is read, but as many requests are made: the waits count them)
@@ -775,8 +710,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
   const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
   const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
   const int steps = (limit + 31) / 32;
-  int at = (int)((int64_t)tile.range * steps / a.n_split);
-  const int end = (int)((int64_t)(tile.range + 1) * steps / a.n_split);
+  int at = part_of(tile.range, steps, a.n_split);
+  const int end = part_of(tile.range + 1, steps, a.n_split);
   PageWalk walk(p, b, lane);
   const char *kbase = a.k.p + hk * a.k.sh * ESZ, *vbase = a.v.p + hk * a.v.sh * ESZ;
   Row8 kr[PER], vr[PER];
@@ -798,10 +733,10 @@ __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
       const int at_ = threadIdx.x + 256 * i, line = at_ / T::PIECES, piece = at_ % T::PIECES;
       char *to = lds + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
       bf16x8 x[3];
-      split8_any(kr[i].a, kr[i].b, x);
+      split8_cut(kr[i].a, kr[i].b, x);
 #pragma unroll
       for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = x[s];
-      split8_any(vr[i].a, vr[i].b, x);
+      split8_cut(vr[i].a, vr[i].b, x);
 #pragma unroll
       for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + (3 + s) * STAGE) = x[s];
     }
@@ -814,7 +749,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
   bf16x8 qf[KS][NS];
   const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * ESZ;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
+  for (int ks = 0; ks < KS; ++ks) split8_cut(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
   const unsigned rows0 = T::rows_base(lds, lane), cols0 = T::cols_base(lds, lane);
   const float c = a.scale_log2e;
   float m = -INFINITY, mc = 0.f, l = 0.f;
@@ -971,15 +906,20 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     if (rows == 32) at += round256(places * 8);
     return s;
   };
-  f.wanted = steps >= 8 ? std::max(1, 512 / p.H_kv) : 1;
+  f.wanted = steps >= kSplitFrom ? std::max(1, 512 / p.H_kv) : 1;
   if (f.few && f.wanted > 1) f.few_sums = take((size_t)f.wanted * p.H_kv, 32);
   if ((f.map = f.few && p.B > 64)) {
     f.off_map = at;
     at += round256((size_t)(p.B + 1) * 8);
   }
-  // Parts until every CU has a workgroup that keeps eight steps of 32 slots; two workgroups where each keeps 64 (fp32: 4).
+  // Parts until every CU has a workgroup that keeps eight steps of 32 slots; two workgroups where each keeps 64, of 64-wide heads three where each keeps 32 (four prompts of 128 to
+  // 512 tokens over 8192 slots, 12 heads on 4: 60 us for 82 with two that keep 64; a frame of 1560 tokens of 12 128-wide heads over 34320: 410 us, with three 450).
   const int64_t groups = (p.T * G / 128 + p.B) * p.H_kv;
-  int64_t parts = std::max(std::min(256 / groups, steps / 8), std::min(512 / groups, steps / (p.dtype == HA_F32 ? 4 : 64)));
+#ifndef HA_PF
+#define HA_PF 4
+#endif
+  const int64_t resident = p.dtype == HA_BF16 && p.d_head == 64 ? 768 : 512, least = p.dtype == HA_F32 ? HA_PF : p.d_head == 64 ? 32 : 64;
+  const int64_t parts = std::max(std::min(256 / groups, steps / 8), std::min(resident / groups, steps / least));
   f.groups = (int)groups;
   f.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
   if (f.tile && f.n_split > 1) f.tile_sums = take((size_t)groups * f.n_split, 128);
@@ -1024,9 +964,8 @@ hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st)
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const unsigned n = (unsigned)(f.wanted + a.p.B) * a.p.Hkv;      // (ranges of all sequences: their shares rounded down, or one)
-    if constexpr (F32) paged_few_f32_kernel<D><<<n, 256, 0, st>>>(a);
-    else if (a.p.page == 16) paged_few_kernel<D, true><<<n, 256, 0, st>>>(a);
-    else paged_few_kernel<D, false><<<n, 256, 0, st>>>(a);
+    if (a.p.page == 16) paged_few_kernel<D, F32, true><<<n, 256, 0, st>>>(a);
+    else paged_few_kernel<D, F32, false><<<n, 256, 0, st>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (f.wanted > 1) e = launch_join<D, F32, 32>(a, f.wanted * a.p.Hkv, st);
   }

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
     const char *qp = a.q.p + (row.query + 8 * g) * ESZ;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      if constexpr (F32) split8_any(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
+      if constexpr (F32) split8_cut(*reinterpret_cast<const f32x4 *>(qp + 64 * ks), *reinterpret_cast<const f32x4 *>(qp + 64 * ks + 16), qf[ks]);
       else qf[ks][0] = *reinterpret_cast<const bf16x8 *>(qp + 32 * ks);
     }
     if (threadIdx.x < 32) {
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           bf16x8 kf[3];
-          split8_any(x[ks][0], x[ks][1], kf);
+          split8_cut(x[ks][0], x[ks][1], kf);
           sc = mfma_split<3>(qf[ks], kf, sc);
         }
       } else {
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
         char *to = lds[stage] + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
         if constexpr (F32) {
           bf16x8 y[3];
-          split8_any(x[i].a, x[i].b, y);
+          split8_cut(x[i].a, x[i].b, y);
 #pragma unroll
           for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = y[s];
         } else {
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
           lo = *reinterpret_cast<const f32x4 *>(kp + 64 * ks);
           hi = *reinterpret_cast<const f32x4 *>(kp + 64 * ks + 16);
         }
-        split8_any(lo, hi, kf[ks]);
+        split8_cut(lo, hi, kf[ks]);
       } else {
         kf[ks][0] = bf16x8{};
         if (id >= 0) kf[ks][0] = *reinterpret_cast<const bf16x8 *>(kp + 32 * ks);

@@ -67,9 +67,10 @@ static __device__ __forceinline__ Row8 weight8(const float *w, int ca, int cb) {
   return Row8{*reinterpret_cast<const f32x4 *>(w + ca), *reinterpret_cast<const f32x4 *>(w + cb)};
 }
 
-template <int D, bool F32, bool NEXT, bool NORM>
+// U: heads whose rows are asked for at once.  Four where there are many tokens (12 + 12 heads of 2 x 75600 tokens: forward 341 us with four, 345 with one, gradients 541 and 564), one
+// where the launch is short and what counts is the code that has to be fetched (two heads of 1024 tokens: 3.5 us with one, 3.8 with four).
+template <int D, bool F32, bool NEXT, bool NORM, int U, bool ONCE>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
-  constexpr int U = 4;        // heads whose rows are asked for at once
   typedef Group<D> G;
   const int t = threadIdx.x % G::TPR;
   const int64_t b = blockIdx.x / a.groups;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     for (int u = 0; u < U; ++u) {
       const int hh = min(h0 + u, a.heads - 1), k = hh >= a.H;
       const View &v = a.x[k];
-      x[u] = load_row8<F32, NEXT>(v.p, b * v.sb + (hh - (k ? a.H : 0)) * v.sh + n * v.sn, ca, cb);
+      x[u] = load_row8<F32, NEXT, ONCE>(v.p, b * v.sb + (hh - (k ? a.H : 0)) * v.sh + n * v.sn, ca, cb);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -102,15 +103,14 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
       if constexpr (NORM) x[u] = times(times(x[u], inverse_rms<D>(x[u], a.eps)), k ? w[1] : w[0]);
       const Row8 y = turn<NEXT>(x[u], c, s, pairs);
       const View &v = a.y[k];
-      if (there) store_row8<F32, NEXT>(v.p, b * v.sb + (hh - (k ? a.H : 0)) * v.sh + n * v.sn, ca, cb, y);
+      if (there) store_row8<F32, NEXT, ONCE>(v.p, b * v.sb + (hh - (k ? a.H : 0)) * v.sh + n * v.sn, ca, cb, y);
     }
   }
 }
 
 // The gradient.  A workgroup walks groups of tokens and leaves its sums over rows of the weights' gradients, which a second kernel adds up.
-template <int D, bool F32, bool NEXT, bool SUMS>
+template <int D, bool F32, bool NEXT, bool SUMS, int U, bool ONCE>
 __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all_groups) {
-  constexpr int U = 2;
   typedef Group<D> G;
   __shared__ float lds[SUMS ? G::ROWS * D : 1];
   const int t = threadIdx.x % G::TPR, row = threadIdx.x / G::TPR;
@@ -133,8 +133,8 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all
       for (int u = 0; u < U; ++u) {
         const int hh = min(h0 + u, a.heads - 1), k = hh >= a.H;
         const int64_t h = hh - (k ? a.H : 0);
-        x[u] = load_row8<F32, NEXT>(a.x[k].p, b * a.x[k].sb + h * a.x[k].sh + n * a.x[k].sn, ca, cb);
-        g[u] = load_row8<F32, NEXT>(a.g[k].p, b * a.g[k].sb + h * a.g[k].sh + n * a.g[k].sn, ca, cb);
+        x[u] = load_row8<F32, NEXT, ONCE>(a.x[k].p, b * a.x[k].sb + h * a.x[k].sh + n * a.x[k].sn, ca, cb);
+        g[u] = load_row8<F32, NEXT, ONCE>(a.g[k].p, b * a.g[k].sb + h * a.g[k].sh + n * a.g[k].sn, ca, cb);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all
         const float mean = row_sum<D>(dot4(gw.a, nx.a) + dot4(gw.b, nx.b)) * (1.f / D);
         const Row8 y = Row8{(gw.a - nx.a * mean) * r, (gw.b - nx.b * mean) * r};
         if (there) {
-          store_row8<F32, NEXT>(a.y[k].p, b * a.y[k].sb + h * a.y[k].sh + n * a.y[k].sn, ca, cb, y);
+          store_row8<F32, NEXT, ONCE>(a.y[k].p, b * a.y[k].sb + h * a.y[k].sh + n * a.y[k].sn, ca, cb, y);
           if constexpr (SUMS) {
             if (k) {
               sum[1].a += gt.a * nx.a;
@@ -224,34 +224,49 @@ ha_status check_both(const ha_rows_problem *p, const ha_rotary *r, RowsArgs &a) 
 }
 ha_status check_weight(const float *w) { return reinterpret_cast<uintptr_t>(w) & 15u ? HA_ERR_ALIGN : HA_OK; }
 
-// Workgroups: a group of tokens each, of all heads; where those are few, the heads are dealt to several.
-dim3 grid_of(unsigned all_groups, int heads, int unroll) {
-  unsigned y = 1;
-  if (all_groups < 512) y = std::min<unsigned>((heads + unroll - 1) / unroll, (512 + all_groups - 1) / all_groups);
-  return dim3(all_groups, y);
-}
-dim3 grad_grid(const ha_rows_problem &p) {
+// Workgroups: a group of tokens each, of all heads; where those are few, the heads are dealt to several and taken one at a time.
+bool is_short(int64_t groups) { return groups < 512; }
+dim3 grid_of(int64_t groups, int heads) { return dim3((unsigned)groups, is_short(groups) ? (unsigned)std::min<int64_t>(heads, (512 + groups - 1) / groups) : 1); }
+int64_t groups_of(const ha_rows_problem &p) {
   const int rows = 256 / (p.d_head / 8);
-  const int64_t groups = (int64_t)p.B * ((p.N + rows - 1) / rows);
-  return grid_of((unsigned)std::min<int64_t>(std::max<int64_t>(groups, 1), 2048), p.H + p.H_kv, 2);
+  return (int64_t)p.B * ((p.N + rows - 1) / rows);
 }
+dim3 grad_grid(const ha_rows_problem &p) { return grid_of(std::min<int64_t>(std::max<int64_t>(groups_of(p), 1), 1024), p.H + p.H_kv); }
 
-template <int D, bool F32>
-hipError_t launch_rows(const RowsArgs &a, dim3 grid, bool next, bool norm, hipStream_t st) {
-  if (next) { if (norm) rows_kernel<D, F32, true, true><<<grid, 256, 0, st>>>(a); else rows_kernel<D, F32, true, false><<<grid, 256, 0, st>>>(a); }
-  else { if (norm) rows_kernel<D, F32, false, true><<<grid, 256, 0, st>>>(a); else rows_kernel<D, F32, false, false><<<grid, 256, 0, st>>>(a); }
+enum Form { kShort, kMany, kOnce };
+Form form_of(const ha_rows_problem &p, int streams) {
+  if (is_short(groups_of(p))) return kShort;
+  return stream_once((int64_t)streams * p.B * (p.H + p.H_kv) * p.N * p.d_head * (p.dtype == HA_F32 ? 4 : 2)) ? kOnce : kMany;
+}
+template <int D, bool F32, bool NEXT, bool NORM>
+hipError_t launch_rows(const RowsArgs &a, dim3 grid, Form form, hipStream_t st) {
+  if (form == kShort) rows_kernel<D, F32, NEXT, NORM, 1, false><<<grid, 256, 0, st>>>(a);
+  else if (form == kMany) rows_kernel<D, F32, NEXT, NORM, 4, false><<<grid, 256, 0, st>>>(a);
+  else rows_kernel<D, F32, NEXT, NORM, 4, true><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
+}
+template <int D, bool F32>
+hipError_t launch_rows(const RowsArgs &a, dim3 grid, Form form, bool next, bool norm, hipStream_t st) {
+  if (next) return norm ? launch_rows<D, F32, true, true>(a, grid, form, st) : launch_rows<D, F32, true, false>(a, grid, form, st);
+  return norm ? launch_rows<D, F32, false, true>(a, grid, form, st) : launch_rows<D, F32, false, false>(a, grid, form, st);
 }
 hipError_t launch_rows(const ha_rows_problem &p, const RowsArgs &a, bool next, bool norm, hipStream_t st) {
-  const dim3 grid = grid_of((unsigned)p.B * a.groups, a.heads, 4);
-  if (p.d_head == 128) return p.dtype == HA_F32 ? launch_rows<128, true>(a, grid, next, norm, st) : launch_rows<128, false>(a, grid, next, norm, st);
-  return p.dtype == HA_F32 ? launch_rows<64, true>(a, grid, next, norm, st) : launch_rows<64, false>(a, grid, next, norm, st);
+  const dim3 grid = grid_of(groups_of(p), a.heads);
+  const Form form = form_of(p, 2);
+  if (p.d_head == 128) return p.dtype == HA_F32 ? launch_rows<128, true>(a, grid, form, next, norm, st) : launch_rows<128, false>(a, grid, form, next, norm, st);
+  return p.dtype == HA_F32 ? launch_rows<64, true>(a, grid, form, next, norm, st) : launch_rows<64, false>(a, grid, form, next, norm, st);
+}
+template <int D, bool F32, bool NEXT, bool SUMS>
+hipError_t launch_grad(const RowsArgs &a, dim3 grid, unsigned groups, Form form, hipStream_t st) {
+  if (form == kShort) rows_grad_kernel<D, F32, NEXT, SUMS, 1, false><<<grid, 256, 0, st>>>(a, groups);
+  else if (form == kMany) rows_grad_kernel<D, F32, NEXT, SUMS, 4, false><<<grid, 256, 0, st>>>(a, groups);
+  else rows_grad_kernel<D, F32, NEXT, SUMS, 4, true><<<grid, 256, 0, st>>>(a, groups);
+  return hipGetLastError();
 }
 template <int D, bool F32>
-hipError_t launch_grad(const RowsArgs &a, dim3 grid, unsigned groups, bool next, hipStream_t st) {
-  if (a.partial) { if (next) rows_grad_kernel<D, F32, true, true><<<grid, 256, 0, st>>>(a, groups); else rows_grad_kernel<D, F32, false, true><<<grid, 256, 0, st>>>(a, groups); }
-  else { if (next) rows_grad_kernel<D, F32, true, false><<<grid, 256, 0, st>>>(a, groups); else rows_grad_kernel<D, F32, false, false><<<grid, 256, 0, st>>>(a, groups); }
-  return hipGetLastError();
+hipError_t launch_grad(const RowsArgs &a, dim3 grid, unsigned groups, Form form, bool next, hipStream_t st) {
+  if (a.partial) return next ? launch_grad<D, F32, true, true>(a, grid, groups, form, st) : launch_grad<D, F32, false, true>(a, grid, groups, form, st);
+  return next ? launch_grad<D, F32, true, false>(a, grid, groups, form, st) : launch_grad<D, F32, false, false>(a, grid, groups, form, st);
 }
 
 }  // namespace
@@ -331,8 +346,10 @@ extern "C" ha_status hybrid_attn_norm_rotate_grad(const ha_rows_problem *p, cons
   hipError_t e;
   const unsigned groups = (unsigned)p->B * a.groups;      // (without tokens the sums are those of no rows)
   if (p->N == 0 && !a.partial) return HA_OK;
-  if (d == 128) e = p->dtype == HA_F32 ? launch_grad<128, true>(a, grid, groups, r->interleaved, stream) : launch_grad<128, false>(a, grid, groups, r->interleaved, stream);
-  else e = p->dtype == HA_F32 ? launch_grad<64, true>(a, grid, groups, r->interleaved, stream) : launch_grad<64, false>(a, grid, groups, r->interleaved, stream);
+  const Form form = form_of(*p, 3);
+  const bool next = r->interleaved;
+  if (d == 128) e = p->dtype == HA_F32 ? launch_grad<128, true>(a, grid, groups, form, next, stream) : launch_grad<128, false>(a, grid, groups, form, next, stream);
+  else e = p->dtype == HA_F32 ? launch_grad<64, true>(a, grid, groups, form, next, stream) : launch_grad<64, false>(a, grid, groups, form, next, stream);
   if (e != hipSuccess) return device_error(e);
   if (a.partial) {
     weight_sums_kernel<<<2 * d / 16, 1024, 0, stream>>>(a.partial, (int)(grid.x * grid.y), 2 * d, d, grad_w_q, grad_w_k);

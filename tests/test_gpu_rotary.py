@@ -70,7 +70,7 @@ def test_norm_rotate_and_gradients(B, H, Hkv, N, d, dtype, layout, rot, interlea
     q2, k2 = ha.hybrid_attn_norm_rotate(q, k, w_q, w_k, r, at, eps)
     dq, dk, dw_q, dw_k = ha.hybrid_attn_norm_rotate_grad(gq, gk, q, k, w_q, w_k, r, at, eps)
     groups = B * -(-N // (2048 // d))
-    terms = (H + Hkv) * -(-groups // min(groups, 2048))
+    terms = (H + Hkv) * -(-groups // min(groups, 1024))
     for x, y, w, g, dx, dw, name in ((q, q2, w_q, gq, dq, dw_q, "q"), (k, k2, w_k, gk, dk, dw_k, "k")):
         close(y, *O.norm_rotate(x, w, eps, r, at), name)
         want = O.norm_rotate_grad(g, x, w, eps, r, at, terms)
