@@ -57,6 +57,7 @@ struct FwdArgs {
   int n_split, tiles;         // tile: ranges of the slots, tiles of a key head
   int leave_few;              // tile: sequences of 32 rows or fewer are another launch's
   int wanted, line_blocks;    // few: ranges that a key head's sequences are to be cut into, together; fours of rows that a sequence may have
+  int split_from;             // few: steps of a sequence that is cut
   int32_t *map;               // few, more than 64 sequences: [2][B + 1] ranges and places of the sequences ahead of each
   int32_t *heads;             // few: [place] sequence and ranges where it is a sequence's first place, otherwise -1
   float *po, *pm, *pl;        // sums of ranges: [place][rows][D], [place][rows]
@@ -81,52 +82,95 @@ struct RowsOf {
 struct Step {
   int key, id0, id1;
 };
-// Walks the slots of a sequence for one key head, 32 at a time, steps at .. end - 1 with a distance of `by`.  SMALL: pages of 16 slots, two to a step; otherwise a step lies in one
-// page, and a step next to the last one is as far from it in memory as its slots are.
-template <int ESZ, bool SMALL>
+// Walks the slots of a sequence for one key head, 32 at a time, steps at .. end - 1, and describes the rows of keys and values that have to be read for each.
+// SMALL: pages of 16 slots, two to a step (k0, v0 and k1, v1), whose addresses are formed for 64 pages at once, one in each lane; otherwise a step lies in one page, and the next
+// one of that page is 32 rows further.  There is one scalar unit for all waves of a CU, so that what a step does here is kept short.
+template <int ESZ, int D, bool SMALL>
 struct Cursor {
+  static constexpr int ROWS = SMALL ? 16 : 32;
   const Paged &p;
   PageWalk walk;
-  int at, end, by, limit, left, id;
-  const char *k, *v;          // of the head; then of the step
   const View &kv, &vv;
-  const char *k0, *v0, *k1, *v1;
-  int rows0, rows1;           // that someone sees of the step (SMALL: of its halves)
-  __device__ __forceinline__ Cursor(const FwdArgs &a, int b, int hk, int at_, int end_, int by_, int limit_, int lane)
-      : p(a.p), walk(a.p, b, lane), at(at_), end(end_), by(by_), limit(limit_), left(0), id(-1), k(a.k.p + hk * a.k.sh * ESZ), v(a.v.p + hk * a.v.sh * ESZ), kv(a.k), vv(a.v), k0(k), v0(v), k1(k), v1(v), rows0(0), rows1(0) {}
-  __device__ __forceinline__ int64_t offset(const View &x, int page, int slot) const { return (page * x.sb + (int64_t)(slot & (p.page - 1)) * x.sn) * ESZ; }
+  const uint64_t k_base, v_base;      // of the head
+  int at, end, limit, left;
+  i32x4 k0, v0, k1, v1;       // descriptors of rows
+  int id;
+  uint64_t ka, va;
+  int from;
+  unsigned klo, khi, vlo, vhi;        // SMALL: this lane's page's (khi = ~0: it is not there)
+  __device__ __forceinline__ Cursor(const FwdArgs &a, int b, int hk, int at_, int end_, int limit_, int lane)
+      : p(a.p), walk(a.p, b, lane), kv(a.k), vv(a.v), k_base(reinterpret_cast<uint64_t>(a.k.p + hk * a.k.sh * ESZ)), v_base(reinterpret_cast<uint64_t>(a.v.p + hk * a.v.sh * ESZ)),
+        at(at_), end(end_), limit(limit_), left(0), id(-1), ka(0), va(0), from(-64), klo(0), khi(0), vlo(0), vhi(0) {
+    k0 = v0 = k1 = v1 = i32x4{0, 0, 0, 0x00020000};
+  }
+  // Bytes from the first of `rows` rows of stride `sn` elements to the end of the last.
+  static __device__ __forceinline__ int span(int rows, int64_t sn) { return rows > 0 ? ((rows - 1) * (int)sn + D) * ESZ : 0; }
   __device__ __forceinline__ Step next() {
     Step s{-1, -1, -1};
-    rows0 = rows1 = 0;
-    if (at < end) {
-      const int key = 32 * at;
-      s.key = key;
-      if constexpr (SMALL) {
-        const int index = key >> 4;
-        s.id0 = walk.at(index);
-        s.id1 = index + 1 < p.max_pages ? walk.at(index + 1) : -1;
-        rows0 = s.id0 < 0 ? 0 : min(limit - key, 16);
-        rows1 = s.id1 < 0 ? 0 : min(limit - key - 16, 16);
-        k0 = k + max(s.id0, 0) * kv.sb * ESZ;
-        v0 = v + max(s.id0, 0) * vv.sb * ESZ;
-        k1 = k + max(s.id1, 0) * kv.sb * ESZ;
-        v1 = v + max(s.id1, 0) * vv.sb * ESZ;
+    if (at >= end) {
+      k0[2] = v0[2] = k1[2] = v1[2] = 0;
+      return s;
+    }
+    const int key = 32 * at, seen = limit - key;
+    s.key = key;
+    ++at;
+    if constexpr (SMALL) {
+      const int index = key >> 4;
+      if (index - from > 62) {
+        from = index;
+        const int page = index + walk.lane, number = page < p.max_pages ? walk.list[page] : -1;
+        const bool there = (unsigned)number < (unsigned)p.n_pages;
+        const uint64_t k = k_base + (uint64_t)(there ? number : 0) * kv.sb * ESZ, v = v_base + (uint64_t)(there ? number : 0) * vv.sb * ESZ;
+        klo = (unsigned)k;
+        khi = there ? (unsigned)(k >> 32) & 0xffff : ~0u;
+        vlo = (unsigned)v;
+        vhi = (unsigned)(v >> 32) & 0xffff;
+      }
+      const int i = index - from;
+      k0[0] = __builtin_amdgcn_readlane(klo, i);
+      k0[1] = __builtin_amdgcn_readlane(khi, i);
+      v0[0] = __builtin_amdgcn_readlane(vlo, i);
+      v0[1] = __builtin_amdgcn_readlane(vhi, i);
+      k1[0] = __builtin_amdgcn_readlane(klo, i + 1);
+      k1[1] = __builtin_amdgcn_readlane(khi, i + 1);
+      v1[0] = __builtin_amdgcn_readlane(vlo, i + 1);
+      v1[1] = __builtin_amdgcn_readlane(vhi, i + 1);
+      s.id0 = k0[1] < 0 ? -1 : 0;
+      s.id1 = k1[1] < 0 ? -1 : 0;
+      k0[2] = k1[2] = span(16, kv.sn);
+      v0[2] = v1[2] = span(16, vv.sn);
+      if (seen < 32) {
+        k0[2] = span(min(seen, 16), kv.sn);
+        v0[2] = span(min(seen, 16), vv.sn);
+        k1[2] = span(min(seen - 16, 16), kv.sn);
+        v1[2] = span(min(seen - 16, 16), vv.sn);
+      }
+      if (s.id0 < 0) k0[1] = k0[2] = v0[2] = 0;
+      if (s.id1 < 0) k1[1] = k1[2] = v1[2] = 0;
+    } else {
+      if (left == 0) {
+        id = walk.at(key >> p.page_log2);
+        left = (p.page - (key & (p.page - 1))) >> 5;
+        const int64_t page = max(id, 0), row = key & (p.page - 1);
+        ka = k_base + (page * kv.sb + row * kv.sn) * ESZ;
+        va = v_base + (page * vv.sb + row * vv.sn) * ESZ;
       } else {
-        if (left <= 0) {
-          id = walk.at(key >> p.page_log2);
-          left = (p.page - (key & (p.page - 1))) >> 5;
-          k0 = k + offset(kv, max(id, 0), key);
-          v0 = v + offset(vv, max(id, 0), key);
-        } else {
-          k0 += (int64_t)(32 * ESZ * by) * kv.sn;
-          v0 += (int64_t)(32 * ESZ * by) * vv.sn;
-        }
-        left -= by;
-        s.id0 = s.id1 = id;
-        rows0 = id < 0 ? 0 : min(limit - key, 32);
+        ka += 32 * ESZ * kv.sn;
+        va += 32 * ESZ * vv.sn;
+      }
+      --left;
+      s.id0 = s.id1 = id;
+      k0[0] = (int)(unsigned)ka;
+      k0[1] = (int)(unsigned)(ka >> 32) & 0xffff;
+      v0[0] = (int)(unsigned)va;
+      v0[1] = (int)(unsigned)(va >> 32) & 0xffff;
+      k0[2] = span(32, kv.sn);
+      v0[2] = span(32, vv.sn);
+      if (seen < 32 || id < 0) {
+        k0[2] = span(id < 0 ? 0 : seen, kv.sn);
+        v0[2] = span(id < 0 ? 0 : seen, vv.sn);
       }
     }
-    at += by;
     return s;
   }
 };
@@ -135,19 +179,19 @@ template <int W, bool SMALL, int NW>
 struct Requests {
   typedef Tile<W> T;
   static constexpr int CHUNKS = T::chunks(32) / NW;
-  int second[CHUNKS], off[CHUNKS];
+  int off[CHUNKS];
   unsigned to[CHUNKS];
+  bool second[CHUNKS];
   __device__ __forceinline__ Requests(const char *lds, int stride_bytes, int w, int lane) {
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int chunk = i * NW + w, first = chunk * T::ROWS_PER_CHUNK, row = first + lane / T::PIECES;
-      second[i] = first / 16;
+      second[i] = first >= 16;
       off[i] = (SMALL ? row % 16 : row) * stride_bytes + (((lane % T::PIECES) ^ T::swz(row)) << 4);
       to[i] = __builtin_amdgcn_readfirstlane(lds_offset(lds) + chunk * 1024);
     }
   }
-  __device__ __forceinline__ void operator()(const char *p0, const char *p1, int rows0, int rows1, int stride_bytes, int further) const {
-    const i32x4 r0 = rows_rsrc<W>(p0, rows0, stride_bytes), r1 = SMALL ? rows_rsrc<W>(p1, rows1, stride_bytes) : r0;
+  __device__ __forceinline__ void operator()(const i32x4 &r0, const i32x4 &r1, int further) const {
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       i32x4 r = r0;
@@ -186,12 +230,12 @@ static __device__ __forceinline__ int few_steps(const Paged &p, int b) {
   const int held = p.held(b);
   return ((p.causal ? max(min(held, held - n.all + n.n), 0) : held) + 31) / 32;
 }
-// One token of 12 heads, d = 128: 500 slots uncut 9.1 us, in four ranges 10.0 with the join; 1000 slots 10.9 and 10.1.
-constexpr int kSplitFrom = 32;
+// One token of 12 heads, d = 128: 500 slots uncut 9.1 us, in four ranges 10.0 with the join; 1000 slots 10.9 and 10.1; in fp32 250 slots 16.9 and 15.
+static inline int split_from(bool f32) { return f32 ? 8 : 32; }
 // Every sequence of as many steps is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
 // ones do not take longer.  Those with several have a place for each range's sums, `wanted` at most.
-static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted) {
-  if (steps < kSplitFrom) return steps < 0 ? 0 : 1;
+static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted, int from) {
+  if (steps < from) return steps < 0 ? 0 : 1;
   // (the quotient of whole numbers below 2^42 is not rounded up to the next one)
   return max(1, min(min(64, steps / 4), (int)((double)wanted * steps / all)));
 }
@@ -226,7 +270,7 @@ static __device__ __forceinline__ Share share_of(const FwdArgs &a, int x, int la
   double all = max(steps, 0);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-  const int n = ranges_of(steps, all, a.wanted), places = n > 1 ? n : 0, upto_places = sum_upto(places, lane), upto = sum_upto(n, lane);
+  const int n = ranges_of(steps, all, a.wanted, a.split_from), places = n > 1 ? n : 0, upto_places = sum_upto(places, lane), upto = sum_upto(n, lane);
   s.places = __shfl(upto_places, 63);
   const uint64_t found = __ballot(upto > x);
   if (!found) return s;
@@ -265,7 +309,7 @@ __global__ __launch_bounds__(1024) void paged_map_kernel(FwdArgs a) {
   for (int i = 0; i < 16; ++i) all += part[i];
   int before[2] = {0, 0};
   for (int b0 = 0; b0 < p.B; b0 += 1024) {
-    const int b = b0 + threadIdx.x, n = b < p.B ? ranges_of(few_steps(p, b), all, a.wanted) : 0, upto[2] = {sum_upto(n, lane), sum_upto(n > 1 ? n : 0, lane)};
+    const int b = b0 + threadIdx.x, n = b < p.B ? ranges_of(few_steps(p, b), all, a.wanted, a.split_from) : 0, upto[2] = {sum_upto(n, lane), sum_upto(n > 1 ? n : 0, lane)};
     __syncthreads();
     if (lane == 63) {
       sums[0][w] = upto[0];
@@ -375,14 +419,16 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
   const RowsOf row(p, n, held, hk, r);
   const int limit = p.causal ? max(min(held, held - n.all + n.n), 0) : held, all_see = p.causal ? min(held, held - n.all + 1) : held;
   const int steps = (limit + 31) / 32;
-  Cursor<ESZ, SMALL> cursor(a, b, hk, part_of(range, steps, n_split) + w, part_of(range + 1, steps, n_split), 4, limit, lane);
+  // (a wave has a quarter of the range, so that its steps follow one another)
+  const int first = part_of(range, steps, n_split), count = part_of(range + 1, steps, n_split) - first;
+  Cursor<ESZ, D, SMALL> cursor(a, b, hk, first + part_of(w, count, 4), first + part_of(w + 1, count, 4), limit, lane);
   const int ksn = (int)a.k.sn * ESZ, vsn = (int)a.v.sn * ESZ;
   char *mine = lds + w * (2 * TILE);
   const Requests<W, SMALL, 1> keys(mine, ksn, 0, lane), values(mine + TILE, vsn, 0, lane);
   Step now = cursor.next();
   if (now.key >= 0) {
-    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
-    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
+    keys(cursor.k0, cursor.k1, 0);
+    values(cursor.v0, cursor.v1, 0);
   }
   bf16x8 qf[KS][NS];
   const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * ESZ;
@@ -434,7 +480,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
     const Step next = cursor.next();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // (the keys have been read)
     // (behind the last step nothing is read, but as many requests are made: the waits count them)
-    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, 0);
+    keys(cursor.k0, cursor.k1, 0);
     mask_step(sc, now, row.see, all_see, g);
     follow(sc, c, m, mc, l, o);
     bf16x8 pb[2][NS];
@@ -458,7 +504,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
         o[rb] = mfma_split<NS>(vf, pb[u], o[rb]);
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, 0);
+    values(cursor.v0, cursor.v1, 0);
     now = next;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (the stages become the images)
@@ -551,14 +597,14 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   const int limit = p.causal ? max(min(held, held - n.all + last + 1), 0) : held;
   const int all_see = p.causal ? min(held, held - n.all + min(R0, tile.n_rows - 1) / p.G + 1) : held;
   const int steps = (limit + 31) / 32, end = part_of(tile.range + 1, steps, a.n_split);
-  Cursor<2, SMALL> cursor(a, b, hk, part_of(tile.range, steps, a.n_split), end, 1, limit, lane);
+  Cursor<2, D, SMALL> cursor(a, b, hk, part_of(tile.range, steps, a.n_split), end, limit, lane);
   const int ksn = (int)a.k.sn * 2, vsn = (int)a.v.sn * 2;
   const Requests<D, SMALL, 4> keys(lds, ksn, w, lane), values(lds + TILE, vsn, w, lane);
   // (behind the last step nothing is read, but as many requests are made: the waits count them)
   auto request = [&](int step) {
     const Step s = cursor.next();
-    keys(cursor.k0, cursor.k1, cursor.rows0, cursor.rows1, ksn, k_at(step));
-    values(cursor.v0, cursor.v1, cursor.rows0, cursor.rows1, vsn, k_at(step));
+    keys(cursor.k0, cursor.k1, k_at(step));
+    values(cursor.v0, cursor.v1, k_at(step));
     return s;
   };
   const float c = a.scale_log2e;
@@ -569,7 +615,18 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[rb][x] = 0.f;
   Step s0 = request(0), s1 = request(1), s2 = request(2);
-  if (s0.key >= 0) {
+  if (s0.key >= 0 && R0 >= tile.n_rows) {             // a wave without rows has its part of the loads and barriers only
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * REQUESTS) : "memory");
+    __syncthreads();
+    for (int now = 0; s0.key >= 0; ++now) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 2) * REQUESTS) : "memory");
+      __syncthreads();
+      const Step further = request(now + AHEAD);
+      s0 = s1;
+      s1 = s2;
+      s2 = further;
+    }
+  } else if (s0.key >= 0) {
     bf16x8 qf[KS];
     const char *qp = a.q.p + (row.h * a.q.sh + row.token * a.q.sn + 8 * g) * 2;
 #pragma unroll
@@ -840,12 +897,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
   }
   if (R >= n_rows) return;
   const bool has = lane < n_split;
-  const float mi = has ? a.pm[at0 + (int64_t)lane * ROWS] : -INFINITY;
+  const float mi = has ? a.pm[at0 + (int64_t)lane * ROWS] : -INFINITY, li = has ? a.pl[at0 + (int64_t)lane * ROWS] : 0.f;
   float m = mi;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
   const float f = mi == m ? 1.f : fast_exp2((mi - m) * a.scale_log2e);
-  float l = has ? a.pl[at0 + (int64_t)lane * ROWS] * f : 0.f;      // (a range that saw nothing has 0, or the NaN that has to show)
+  float l = has ? li * f : 0.f;                                // (a range that saw nothing has 0, or the NaN that has to show)
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -906,7 +963,7 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     if (rows == 32) at += round256(places * 8);
     return s;
   };
-  f.wanted = steps >= kSplitFrom ? std::max(1, 512 / p.H_kv) : 1;
+  f.wanted = steps >= split_from(p.dtype == HA_F32) ? std::max(1, 512 / p.H_kv) : 1;
   if (f.few && f.wanted > 1) f.few_sums = take((size_t)f.wanted * p.H_kv, 32);
   if ((f.map = f.few && p.B > 64)) {
     f.off_map = at;
@@ -957,6 +1014,7 @@ hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st)
   if (f.few) {
     sums(f.few_sums);
     a.wanted = f.wanted;
+    a.split_from = split_from(F32);
     a.line_blocks = (std::min(32, a.p.max_new * a.p.G) + 3) / 4;
     a.map = f.map ? reinterpret_cast<int32_t *>(ws + f.off_map) : nullptr;
     if (f.map) {

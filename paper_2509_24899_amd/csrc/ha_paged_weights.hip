@@ -21,6 +21,9 @@ struct WeightArgs {
   float scale_log2e;
   int parts;                  // workgroups of a sequence and key head
   int few;                    // tile: sequences of 32 rows or fewer are another launch's
+  int row_parts;              // tile: parts of the rows, whose sums are joined where there are several
+  float *sums;                // [row_parts][B H_kv][slots]
+  float inv_G;
 };
 
 // Row R of a sequence: its query, - lse log2 e (- infinity where it sees nothing or is none), and how many slots it sees.
@@ -30,7 +33,8 @@ struct WeightRow {
   int see;
   __device__ __forceinline__ WeightRow(const WeightArgs &a, const NewRows &n, int held, int hk, int R) {
     const Paged &p = a.p;
-    const int n_rows = n.n * p.G, Rc = min(R, n_rows - 1), i = Rc / p.G, h = hk * p.G + Rc - i * p.G;
+    const int n_rows = n.n * p.G, Rc = min(R, n_rows - 1);
+    const int i = (int)((Rc + 0.5f) * a.inv_G), h = hk * p.G + Rc - i * p.G;      // (Rc / G: the quotient is 0.5 / G from a whole number, and off by 2^-22 of itself, Rc < 2^20)
     const int64_t token = n.first + i;
     const float x = a.lse[token * p.H + h];
     query = h * a.q.sh + token * a.q.sn;
@@ -133,6 +137,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
   }
 }
 
+// Rows are asked for two steps of 32 ahead.  Where the slots make few workgroups the rows are cut into parts, whose sums a second kernel adds up.
 template <int D, bool F32>
 __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a) {
   typedef Tile<D> T;
@@ -142,52 +147,58 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
   __shared__ int see[2][32];
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int bh = blockIdx.x / a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, first = (blockIdx.x % a.parts) * 128, slot0 = first + 32 * w, slot = slot0 + r, capacity = p.capacity();
+  const int row_part = blockIdx.x % a.row_parts, item = blockIdx.x / a.row_parts;
+  const int bh = item / a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, first = (item % a.parts) * 128, slot0 = first + 32 * w, slot = slot0 + r, capacity = p.capacity();
   const NewRows n(p, b);
   const int held = p.held(b), n_rows = n.n * p.G, before = held - n.all;      // before: slots ahead of the first new token's
   if (a.few && n_rows <= 32) return;
-  const int64_t out = (int64_t)bh * capacity + slot;
   const int id = slot < held ? p.page_of(b, slot) : -1;
   float sum = 0.f;
-  // rows that see the workgroup's first slot, from a multiple of 32 on
-  int R0 = first >= held ? n_rows : p.causal ? max(first - before, 0) * p.G / 32 * 32 : 0;
-  if (R0 < n_rows) {
-    Row8 x[PER];
-    float next_shift = 0.f;
-    int next_see = 0;
-    auto request = [&](int R) {
+  // steps of rows that see the workgroup's first slot, this part's
+  const int steps = (n_rows + 31) / 32, step0 = first >= held ? steps : p.causal ? max(first - before, 0) * p.G / 32 : 0, count = max(steps - step0, 0);
+  int R0 = 32 * (step0 + count * row_part / a.row_parts);
+  const int R_end = 32 * (step0 + count * (row_part + 1) / a.row_parts);
+  if (R0 < R_end) {
+    struct Ahead {
+      Row8 x[PER];
+      float shift;
+      int see;
+    };
+    auto request = [&](Ahead &y, int R) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int at = threadIdx.x + 256 * i, piece = at % T::PIECES;
         const WeightRow row(a, n, held, hk, R + at / T::PIECES);
-        x[i] = load_row8<F32, true>(a.q.p, row.query, 8 * piece, 8 * piece + 4);
+        y.x[i] = load_row8<F32, true>(a.q.p, row.query, 8 * piece, 8 * piece + 4);
       }
       if (threadIdx.x < 32) {
         const WeightRow row(a, n, held, hk, R + r);
-        next_shift = row.shift;
-        next_see = row.see;
+        y.shift = row.shift;
+        y.see = row.see;
       }
     };
-    auto deposit = [&](int stage) {
+    auto deposit = [&](const Ahead &y, int stage) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int at = threadIdx.x + 256 * i, line = at / T::PIECES, piece = at % T::PIECES;
         char *to = lds[stage] + line * T::PITCH + ((piece ^ T::swz(line)) << 4);
         if constexpr (F32) {
-          bf16x8 y[3];
-          split8_cut(x[i].a, x[i].b, y);
+          bf16x8 z[3];
+          split8_cut(y.x[i].a, y.x[i].b, z);
 #pragma unroll
-          for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = y[s];
+          for (int s = 0; s < 3; ++s) *reinterpret_cast<bf16x8 *>(to + s * STAGE) = z[s];
         } else {
-          *reinterpret_cast<bf16x8 *>(to) = __builtin_convertvector(__builtin_shufflevector(x[i].a, x[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+          *reinterpret_cast<bf16x8 *>(to) = __builtin_convertvector(__builtin_shufflevector(y.x[i].a, y.x[i].b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
         }
       }
       if (threadIdx.x < 32) {
-        shift[stage][r] = next_shift;
-        see[stage][r] = next_see;
+        shift[stage][r] = y.shift;
+        see[stage][r] = y.see;
       }
     };
-    request(R0);
+    Ahead even{}, odd{};        // rows of the steps with an even and an odd distance from the first
+    request(even, R0);
+    request(odd, min(R0 + 32, R_end - 32));
     const char *kp = a.k.p + (hk * a.k.sh + (id < 0 ? 0 : id * a.k.sb + (int64_t)(slot & (p.page - 1)) * a.k.sn) + 8 * g) * ESZ;
     bf16x8 kf[KS][NS];
 #pragma unroll
@@ -204,10 +215,10 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
         if (id >= 0) kf[ks][0] = *reinterpret_cast<const bf16x8 *>(kp + 32 * ks);
       }
     }
-    deposit(0);
+    deposit(even, 0);
     __syncthreads();
-    for (int stage = 0; R0 < n_rows; R0 += 32, stage ^= 1) {
-      if (R0 + 32 < n_rows) request(R0 + 32);
+    auto step = [&](Ahead &now, const Ahead &next, int stage) {      // (now: has been deposited, takes the rows of two steps on)
+      if (R0 + 64 < R_end) request(now, R0 + 64);
       const unsigned rows0 = T::rows_base(lds[stage], lane);
       f32x16 sc;
 #pragma unroll
@@ -223,13 +234,55 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
       const int first_sees = p.causal ? min(held, before + R0 / p.G + 1) : held;
       sum += slot0 + 32 <= first_sees && R0 + 32 <= n_rows ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
                                                            : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g);
-      if (R0 + 32 < n_rows) deposit(stage ^ 1);
+      if (R0 + 32 < R_end) deposit(next, stage ^ 1);
       __syncthreads();
+      R0 += 32;
+    };
+    while (true) {
+      step(even, odd, 0);
+      if (R0 >= R_end) break;
+      step(odd, even, 1);
+      if (R0 >= R_end) break;
     }
     if (id < 0) sum = 0.f;
   }
   sum = xhalf_sum(sum);
-  if (g == 0 && slot < capacity) add_weight(a, out, sum);
+  if (g == 0 && slot < capacity) {
+    const int64_t at = (int64_t)bh * capacity + slot;
+    if (a.row_parts > 1) a.sums[(int64_t)row_part * p.B * p.Hkv * capacity + at] = sum;
+    else add_weight(a, at, sum);
+  }
+}
+__global__ __launch_bounds__(256) void paged_weights_join_kernel(WeightArgs a) {
+  const Paged &p = a.p;
+  const int64_t capacity = p.capacity(), all = (int64_t)p.B * p.Hkv * capacity, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= all || (a.few && NewRows(p, (int)(at / capacity / p.Hkv)).n * p.G <= 32)) return;
+  float sum = 0.f;
+  for (int i = 0; i < a.row_parts; ++i) sum += a.sums[i * all + at];
+  add_weight(a, at, sum);
+}
+
+struct WeightPlan {
+  bool few, tile;
+  int blocks, row_parts;      // of 128 slots, of the rows
+  size_t total;
+};
+WeightPlan weight_plan(const ha_paged_problem &p) {
+  WeightPlan f{};
+  const int64_t slots = (int64_t)p.max_pages * p.page, groups = (int64_t)p.B * p.H_kv, rows = (int64_t)p.max_new * (p.H / p.H_kv);
+  f.blocks = (int)((slots + 127) / 128);
+  f.few = rows <= 32 || p.q_offset;
+  f.tile = rows > 32;
+#ifndef HA_RP
+#define HA_RP 512
+#endif
+#ifndef HA_RS
+#define HA_RS 4
+#endif
+  // Parts until there are two workgroups to a CU, each with four steps of 32 rows.
+  f.row_parts = f.tile && slots > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>(HA_RP / (groups * f.blocks), (rows + 31) / 32 / HA_RS)) : 1;
+  if (f.row_parts > 1) f.total = round256((size_t)f.row_parts * groups * slots * 4);
+  return f;
 }
 
 }  // namespace
@@ -238,8 +291,8 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
 using namespace ha;
 
 extern "C" size_t hybrid_attn_paged_weights_workspace_bytes(const ha_paged_problem *p) {
-  (void)p;
-  return 0;
+  if (check_paged(p) != HA_OK) return 0;
+  return weight_plan(*p).total;
 }
 
 extern "C" ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const ha_view *q, const ha_view *k_pages, const float *lse, const float *weights, float *weights_out,
@@ -248,30 +301,38 @@ extern "C" ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const 
   if (st != HA_OK) return st;
   WeightArgs a{};
   if ((st = check_packed(*p, q, p->H, false, a.q)) != HA_OK || (st = check_pool(*p, k_pages, false, a.k)) != HA_OK) return st;
-  const int64_t slots = (int64_t)p->max_pages * p->page, blocks = (slots + 127) / 128, groups = (int64_t)p->B * p->H_kv, rows = (int64_t)p->max_new * (p->H / p->H_kv);
-  if (groups * blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
+  const int64_t slots = (int64_t)p->max_pages * p->page, groups = (int64_t)p->B * p->H_kv;
+  const WeightPlan f = weight_plan(*p);
+  if (groups * f.blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
   if ((p->T > 0 && !lse) || (slots > 0 && !weights_out)) return HA_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out)) & 3u) return HA_ERR_ALIGN;
-  if ((st = check_workspace(workspace, workspace_bytes, hybrid_attn_paged_weights_workspace_bytes(p))) != HA_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, f.total)) != HA_OK) return st;
   if (slots == 0) return HA_OK;
   a.p = paged_of(*p);
   a.lse = lse;
   a.weights = weights;
   a.out = weights_out;
   a.scale_log2e = p->softmax_scale * kLog2e;
+  a.inv_G = 1.f / (float)a.p.G;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const bool f32 = p->dtype == HA_F32, few = rows <= 32 || p->q_offset;
+  const bool f32 = p->dtype == HA_F32;
   hipError_t e;
-  if (rows > 32) {
-    a.parts = (int)blocks;
-    a.few = few;
-    const unsigned grid = (unsigned)(groups * blocks);
+  if (f.tile) {
+    a.parts = f.blocks;
+    a.few = f.few;
+    a.row_parts = f.row_parts;
+    a.sums = static_cast<float *>(workspace);
+    const unsigned grid = (unsigned)(groups * f.blocks * f.row_parts);
     if (p->d_head == 128) { if (f32) paged_weights_tile_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
     else { if (f32) paged_weights_tile_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+    if (f.row_parts > 1) {
+      paged_weights_join_kernel<<<(unsigned)((groups * slots + 255) / 256), 256, 0, stream>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
+    }
   }
-  if (few) {
-    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 2048 / groups));
+  if (f.few) {
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(f.blocks, 2048 / groups));
     const unsigned grid = (unsigned)(groups * a.parts);
     if (p->d_head == 128) { if (f32) paged_weights_few_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
     else { if (f32) paged_weights_few_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
