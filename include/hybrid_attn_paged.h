@@ -52,7 +52,8 @@ ha_status hybrid_attn_paged_append(const ha_paged_problem *p, const ha_rotary *r
 
 /* Enqueues softmax attention of the new tokens over their sequences: out = sum_j p_j v_j, p_j = exp(scale q . k_j - lse), j over the slots that the token sees.  A token
  * that sees none has out = 0 and lse = -infinity.  lse: device fp32 [T, H], or NULL.  What the pools hold in slots that no token of a sequence sees is never used; a NaN or
- * infinity in a slot that some token of a tile of neighbouring ones sees may reach all of that tile.  workspace: device, 256-byte aligned,
+ * infinity in a slot that some token of a tile of neighbouring ones sees may reach all of that tile.  Logits beyond 2^28 in magnitude may give infinities or NaN, and so may
+ * values whose sum, with weights of 2^8 at most, leaves fp32's range before it is divided.  workspace: device, 256-byte aligned,
  * hybrid_attn_paged_workspace_bytes() bytes (0 is possible).  Results are the same bit for bit every time. */
 size_t hybrid_attn_paged_workspace_bytes(const ha_paged_problem *p);
 ha_status hybrid_attn_paged_forward(const ha_paged_problem *p, const ha_view *q, const ha_view *k_pages, const ha_view *v_pages, const ha_view *out, float *lse,

@@ -52,6 +52,7 @@ ha_status hybrid_attn_rotate(const ha_rows_problem *p, const ha_rotary *r, const
  *
  *   n = x / sqrt(mean of x^2 over the row's d_head channels + eps),   out = rotation of (w n)
  *
+ * (A row of zeros with eps = 0, or one whose mean square leaves fp32's range, magnitudes beyond some 2^63, has no norm: it gives zeros, infinities or NaN.)
  * w_q, w_k: device fp32 [d_head] for all heads, 16-byte aligned, or NULL: ones.  q_out may be q itself and k_out k. */
 ha_status hybrid_attn_norm_rotate(const ha_rows_problem *p, const ha_rotary *r, const ha_view *q, const ha_view *k, const float *w_q, const float *w_k,
                                   const ha_view *q_out, const ha_view *k_out, void *hip_stream);

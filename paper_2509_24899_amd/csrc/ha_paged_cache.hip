@@ -225,7 +225,8 @@ __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
     const uint64_t below = ((uint64_t)1 << lane) - 1, tied = __ballot(k == 2);
     const bool stay = k == 1 || (k == 2 && ties[16 * i + w] + __popcll(tied & below) < need);
     const uint64_t all = __ballot(stay);
-    if (stay) kept[stays[16 * i + w] + __popcll(all & below)] = 1024 * i + threadIdx.x;
+    const unsigned to = stays[16 * i + w] + __popcll(all & below);
+    if (stay && to < (unsigned)a.keep) kept[to] = 1024 * i + threadIdx.x;
   }
 }
 
@@ -328,7 +329,10 @@ __global__ __launch_bounds__(256) void evict_list_kernel(EvictArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int k = c.kind(i, prefix);
-      if (k == 1 || (k == 2 && tie < need)) kept[at++] = c.first + i;
+      if (k == 1 || (k == 2 && tie < need)) {
+        if (at < (unsigned)a.keep) kept[at] = c.first + i;      // (always, unless the weights changed from one launch to the next)
+        ++at;
+      }
       tie += k == 2;
     }
     // (all chunks share what is behind the last slot that stays)
@@ -345,7 +349,7 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int esz) {
   const int stay = min(p.held(b), a.keep);
   if (threadIdx.x < 64) {
     const int i = i0 + threadIdx.x;
-    if (i < capacity) a.weights_out[(int64_t)bh * capacity + i] = i < stay ? a.weights[(int64_t)bh * capacity + a.kept[(int64_t)bh * a.keep + i]] : 0.f;
+    if (i < capacity) a.weights_out[(int64_t)bh * capacity + i] = i < stay ? a.weights[(int64_t)bh * capacity + min(max(a.kept[(int64_t)bh * a.keep + i], 0), capacity - 1)] : 0.f;
   }
   if (i0 >= stay) return;
   const int c = threadIdx.x % TPR * 16;
@@ -360,7 +364,7 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a, int esz) {
       k[u] = v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (i < stay) {
         const int slot = a.kept[(int64_t)bh * a.keep + i];
-        const int id = p.page_of(b, slot), out = a.out_table[(int64_t)b * a.out_pages + (i >> p.page_log2)];
+        const int id = (unsigned)slot < (unsigned)capacity ? p.page_of(b, slot) : -1, out = a.out_table[(int64_t)b * a.out_pages + (i >> p.page_log2)];
         if ((unsigned)out < (unsigned)p.n_pages) to[u] = out;
         if (id >= 0) {
           const int64_t row = slot & (p.page - 1);
@@ -391,7 +395,7 @@ hipError_t launch_append(const AppendArgs &a, bool next, bool norm, hipStream_t 
   const unsigned rows = 256 / (D / 8), groups = (a.p.T + rows - 1) / rows, heads = a.Hq + 2 * a.p.Hkv;
   if (groups >= 512) return launch_append<D, F32, 4>(a, dim3(groups), next, norm, st);
   const unsigned each = groups >= 64 ? 4 : 1;
-  const dim3 grid(groups, std::min((heads + each - 1) / each, (512 + groups - 1) / groups));
+  const dim3 grid(groups, std::min((heads + each - 1) / each, (1024 + groups - 1) / groups));
   return each == 4 ? launch_append<D, F32, 4>(a, grid, next, norm, st) : launch_append<D, F32, 1>(a, grid, next, norm, st);
 }
 

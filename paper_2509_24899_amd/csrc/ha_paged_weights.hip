@@ -273,14 +273,8 @@ WeightPlan weight_plan(const ha_paged_problem &p) {
   f.blocks = (int)((slots + 127) / 128);
   f.few = rows <= 32 || p.q_offset;
   f.tile = rows > 32;
-#ifndef HA_RP
-#define HA_RP 512
-#endif
-#ifndef HA_RS
-#define HA_RS 4
-#endif
   // Parts until there are two workgroups to a CU, each with four steps of 32 rows.
-  f.row_parts = f.tile && slots > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>(HA_RP / (groups * f.blocks), (rows + 31) / 32 / HA_RS)) : 1;
+  f.row_parts = f.tile && slots > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / (groups * f.blocks), (rows + 31) / 32 / 4)) : 1;
   if (f.row_parts > 1) f.total = round256((size_t)f.row_parts * groups * slots * 4);
   return f;
 }
