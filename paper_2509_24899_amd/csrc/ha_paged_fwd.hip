@@ -3,9 +3,10 @@
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i),   j over the slots that new token i sees
 //
 // All query heads of a key head are rows of one product (row R of a sequence is token R / G, head R % G of the group), so that keys and values are read once for a
-// group.  Logits, sums and the output's sums are fp32; of bf16 tensors the weights are rounded to bf16 for the second product (half a step, 2^-8 of each, the sum
+// group.  Logits, sums and the output's sums are fp32; of bf16 tensors the weights of tiles are rounded to bf16 for the second product (half a step, 2^-8 of each, the sum
 // that divides is that of the unrounded ones), of fp32 tensors every operand is three bf16 pieces, six products each.
-//   few   32 rows at most (single tokens): bound by memory.  A workgroup takes a range of a sequence's slots for a key head, every wave slots of its own.
+//   few   32 rows at most (single tokens): bound by memory, which leaves time for weights in two pieces (a result is off by 0.17 % on the average, the rounding of the
+//         output alone, where weights in one piece make it 0.22).  A workgroup takes a range of a sequence's slots for a key head, every wave slots of its own.
 //   tile  128 rows, 32 to a wave: bound by the matrix cores.  All waves read the same slots out of LDS.
 // Where either leaves compute units idle the slots are cut into ranges, whose sums a second kernel joins.
 #include <cmath>
@@ -412,7 +413,7 @@ static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &
 // the slots' weights are formed from next: 394 MB of both 66 us for 77, up to 260 MB the same to within 1 us.
 template <int D, bool F32, bool SMALL>
 __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
-  constexpr int ESZ = F32 ? 4 : 2, W = D * ESZ / 2, KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1;      // W: a row in twos of bytes
+  constexpr int ESZ = F32 ? 4 : 2, W = D * ESZ / 2, KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1, PS = F32 ? 3 : 2;      // W: a row in twos of bytes; pieces of a value, of a weight
   typedef Tile<W> T;
   constexpr int TILE = T::bytes(32), REQUESTS = T::chunks(32);
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TILE];      // [wave][k | v]; then [wave][register image]
@@ -493,7 +494,7 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
     keys(cursor.k0, cursor.k1, 0);
     mask_step(sc, now, row.see, all_see, g);
     follow(sc, c, m, mc, l, o);
-    bf16x8 pb[2][NS];
+    bf16x8 pb[2][PS];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x8 pr;
@@ -502,7 +503,18 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
         pr[x] = fast_exp2(__builtin_fmaf(sc[8 * u + x], c, -mc));
         l += pr[x];
       }
-      split8<NS>(pr, pb[u]);
+      if constexpr (F32) {
+        split8<PS>(pr, pb[u]);
+      } else {              // cut off, and what that leaves, which is never 0 of a weight that is not: an infinite value's product with it would be NaN
+        f32x8 cut;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          cut[x] = __uint_as_float(__float_as_uint(pr[x]) & 0xffff0000u);
+          pr[x] = fmaxf(pr[x] - cut[x], pr[x] * 0x1p-20f);
+        }
+        pb[u][0] = __builtin_convertvector(cut, bf16x8);
+        pb[u][1] = __builtin_convertvector(pr, bf16x8);
+      }
     }
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(REQUESTS) : "memory");
 #pragma unroll
@@ -511,7 +523,12 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
       for (int rb = 0; rb < RB; ++rb) {
         bf16x8 vf[NS];
         value_piece(rb, u, vf);
-        o[rb] = mfma_split<NS>(vf, pb[u], o[rb]);
+        if constexpr (F32) {
+          o[rb] = mfma_split<NS>(vf, pb[u], o[rb]);
+        } else {
+          o[rb] = mfma32(vf[0], pb[u][1], o[rb]);
+          o[rb] = mfma32(vf[0], pb[u][0], o[rb]);
+        }
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     values.once(cursor.v0, cursor.v1);
