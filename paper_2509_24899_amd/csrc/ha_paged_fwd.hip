@@ -990,7 +990,9 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     if (rows == 32) at += round256(places * 8);
     return s;
   };
-  f.wanted = steps >= split_from(p.dtype == HA_F32) ? std::max(1, 512 / p.H_kv) : 1;
+  // (ranges of all sequences and key heads: two workgroups to a CU, of 128-wide fp32 heads one: 16 sequences of 4000 slots, 4 key heads, 54 us for 63 with two)
+  const int resident_few = p.dtype == HA_F32 && p.d_head == 128 ? 256 : 512;
+  f.wanted = steps >= split_from(p.dtype == HA_F32) ? std::max(1, resident_few / p.H_kv) : 1;
   if (f.few && f.wanted > 1) f.few_sums = take((size_t)f.wanted * p.H_kv, 32);
   if ((f.map = f.few && p.B > 64)) {
     f.off_map = at;
