@@ -41,8 +41,8 @@ static __device__ __forceinline__ int last_not_above(int B, int x, int lane, At 
 }
 
 // Three bf16 pieces of eight fp32 values.  The first is cut off, so that the largest finite values do not become infinite, the second is the rounding of what that leaves, and the
-// third holds the rest exactly: 8 + 8 + 8 bits.  Infinities and NaN have one piece (infinity less infinity is none).  No branches: kernels that split many
-// values are a fourth as long as with those of split8_any, which counts where a launch is short.  Of the nine products of two splits the three that are left out
+// third holds the rest exactly: 8 + 8 + 8 bits.  Infinities and NaN have one piece (infinity less infinity is none).  No branches: a kernel that splits many
+// values is half as long as with those of split8_any (29 KB for 64), which counts where a launch is short.  Of the nine products of two splits the three that are left out
 // are 2^-23, 2^-23 and 2^-32 of theirs.
 static __device__ __forceinline__ void split8_cut(f32x4 lo, f32x4 hi, bf16x8 (&out)[3]) {
   f32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), first;

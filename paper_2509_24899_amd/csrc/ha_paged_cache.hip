@@ -21,12 +21,6 @@ struct AppendArgs {
   float eps;
 };
 
-static __device__ __forceinline__ Row8 times(const Row8 &x, float f) { return Row8{x.a * f, x.b * f}; }
-static __device__ __forceinline__ Row8 times(const Row8 &x, const Row8 &w) { return Row8{x.a * w.a, x.b * w.b}; }
-static __device__ __forceinline__ Row8 weight8(const float *w, int ca, int cb) {
-  if (!w) return Row8{f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{1.f, 1.f, 1.f, 1.f}};
-  return Row8{*reinterpret_cast<const f32x4 *>(w + ca), *reinterpret_cast<const f32x4 *>(w + cb)};
-}
 
 // U: heads whose rows are asked for at once: four where there are many tokens, one where there are few (one token: 4.2 us for 5.6).
 template <int D, bool F32, bool NEXT, bool NORM, int U>

@@ -539,8 +539,8 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
 }
 
 // ---- tiles of rows ---------------------------------------------------------------------------------------------------
-// Rows of T before a sequence, in tiles of 128 rows: the tiles of sequence b are those from here on, as many as it needs.
-static __device__ __forceinline__ int first_tile(const Paged &p, int b) { return p.offset(b) * p.G / 128 + b; }
+// The tiles of 128 rows of sequence b are those from here on, as many as it needs; with offsets on the device there are some between them that hold nothing.
+static __device__ __forceinline__ int first_tile(const Paged &p, int b) { return p.q_offset ? p.offset(b) * p.G / 128 + b : b * ((p.max_new * p.G + 127) / 128); }
 
 // Writes a 32-row tile held as C^T (the row is the lane's) times `f` through `stage` (this wave's own LDS) to the rows at to(r), those below `rows`.
 template <int D, bool F32, typename To>
@@ -972,6 +972,27 @@ struct FwdPlan {
   size_t off_map, total;
 };
 
+// Ranges of the slots of `tiles` tiles: as many as take the least time by this reckoning.  A CU that has all workgroups it can hold takes a step of them all in the time 1, one with fewer
+// the share `alone` of it at least; a workgroup starts in the time of `start` steps; and joining takes that of 16 and of 0.007 for each workgroup (fp32, whose steps
+// take four times as long: 12 and 0.0025).  From times of 1 to 64 ranges of 25 batches (8 to 320 tiles of 64 to 1073 steps): what this chooses is within 5 % of the best of them in all.
+// 300 tiles of 512 steps, 128-wide: 358 us in five ranges, 476 in one; 256 of 1073: 606 in two, 988 in one; 12 fp32 ones of 256: 69 in 32, 131 in ten.
+int ranges_of_tiles(const ha_paged_problem &p, int64_t tiles, int64_t steps) {
+  const bool f32 = p.dtype == HA_F32, wide = p.d_head == 128;
+  const int resident = !f32 && !wide ? 3 : 2;
+  const double alone = f32 ? 0.8 : wide ? 0.7 : 0.5, start = f32 ? 0. : wide ? 8. : 4., join = f32 ? 12. : 16., join_each = f32 ? 0.0025 : 0.007;
+  int best = 1;
+  double least = 0.;
+  for (int n = 1; n <= 64 && n <= steps && (n == 1 || tiles * n <= 2048); ++n) {
+    const int64_t most = (tiles * n + 255) / 256, left = most % resident;      // workgroups of the CU that has the most
+    const double time = (most / resident + (left ? alone + (1. - alone) * left / resident : 0.)) * ((steps + n - 1) / n + start) + (n > 1 ? join + join_each * (tiles * n) : 0.);
+    if (n == 1 || time < least) {
+      best = n;
+      least = time;
+    }
+  }
+  return best;
+}
+
 FwdPlan plan_forward(const ha_paged_problem &p) {
   FwdPlan f{};
   const int64_t G = p.H / p.H_kv, steps = ((int64_t)p.max_pages * p.page + 31) / 32;
@@ -998,13 +1019,9 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     f.off_map = at;
     at += round256((size_t)(p.B + 1) * 8);
   }
-  // Parts until every CU has a workgroup that keeps eight steps of 32 slots; two workgroups where each keeps 64, of 64-wide heads three where each keeps 32 (four prompts of 128 to
-  // 512 tokens over 8192 slots, 12 heads on 4: 60 us for 82 with two that keep 64; a frame of 1560 tokens of 12 128-wide heads over 34320: 410 us, with three 450).
-  const int64_t groups = (p.T * G / 128 + p.B) * p.H_kv;
-  const int64_t resident = p.dtype == HA_BF16 && p.d_head == 64 ? 768 : 512, least = p.dtype == HA_F32 ? 4 : p.d_head == 64 ? 32 : 64;
-  const int64_t parts = std::max(std::min(256 / groups, steps / 8), std::min(resident / groups, steps / least));
+  const int64_t full = p.B * ((p.max_new * G + 127) / 128) * p.H_kv, groups = p.q_offset ? (p.T * G / 128 + p.B) * p.H_kv : full;
   f.groups = (int)groups;
-  f.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(64, parts));
+  f.n_split = f.tile ? ranges_of_tiles(p, std::min(groups, full), steps) : 1;
   if (f.tile && f.n_split > 1) f.tile_sums = take((size_t)groups * f.n_split, 128);
   f.total = at;
   return f;

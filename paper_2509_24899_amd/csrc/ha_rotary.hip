@@ -60,12 +60,6 @@ template <int D>
 struct Group {
   static constexpr int TPR = D / 8, ROWS = 256 / TPR;      // threads to a row, tokens to a workgroup
 };
-static __device__ __forceinline__ Row8 times(const Row8 &x, float f) { return Row8{x.a * f, x.b * f}; }
-static __device__ __forceinline__ Row8 times(const Row8 &x, const Row8 &w) { return Row8{x.a * w.a, x.b * w.b}; }
-static __device__ __forceinline__ Row8 weight8(const float *w, int ca, int cb) {
-  if (!w) return Row8{f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{1.f, 1.f, 1.f, 1.f}};
-  return Row8{*reinterpret_cast<const f32x4 *>(w + ca), *reinterpret_cast<const f32x4 *>(w + cb)};
-}
 
 // U: heads whose rows are asked for at once.  Four where there are many tokens (12 + 12 heads of 2 x 75600 tokens: forward 341 us with four, 345 with one, gradients 541 and 564), one
 // where the launch is short and what counts is the code that has to be fetched (two heads of 1024 tokens: 3.5 us with one, 3.8 with four).
@@ -108,7 +102,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
   }
 }
 
-// The gradient.  A workgroup walks groups of tokens and leaves its sums over rows of the weights' gradients, which a second kernel adds up.
+// The gradient.  A workgroup walks groups of tokens and leaves its sums over rows of the weights' gradients, which a second kernel adds up.  (12 + 12 heads of 2 x 75600 tokens: 507 us
+// for three streams, 5.5 TB/s; the forward 342 us for two, 5.4.  Sums by atomics would be in another order every time.)
 template <int D, bool F32, bool NEXT, bool SUMS, int U, bool ONCE>
 __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all_groups) {
   typedef Group<D> G;
@@ -178,7 +173,7 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all
   }
 }
 
-// Sum of the workgroups' sums, 16 columns to a workgroup, in double.
+// Sum of the workgroups' sums, 16 columns to a workgroup, in double (1024 of them: 6.7 us).
 __global__ __launch_bounds__(1024) void weight_sums_kernel(const float *partial, int n, int width, int D, float *dw_q, float *dw_k) {
   constexpr int U = 8;        // loads in flight
   __shared__ double lds[64][17];

@@ -28,6 +28,12 @@ static __device__ __forceinline__ void own_channels(int t, int rot, int &ca, int
 struct Row8 {
   f32x4 a, b;
 };
+static __device__ __forceinline__ Row8 times(const Row8 &x, float f) { return Row8{x.a * f, x.b * f}; }
+static __device__ __forceinline__ Row8 times(const Row8 &x, const Row8 &w) { return Row8{x.a * w.a, x.b * w.b}; }
+static __device__ __forceinline__ Row8 weight8(const float *w, int ca, int cb) {
+  if (!w) return Row8{f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{1.f, 1.f, 1.f, 1.f}};
+  return Row8{*reinterpret_cast<const f32x4 *>(w + ca), *reinterpret_cast<const f32x4 *>(w + cb)};
+}
 // Streams that are read or written once and that the memory-side cache cannot hold go past it (ONCE).  Loads only where one instruction takes whole lines: 12 + 12 heads of
 // 2 x 75600 bf16 tokens, forward and gradients 861 us for 911, of which the stores make 18; fp32 gradients of 5003 tokens 32 us with such loads and 25 without.
 template <bool ONCE, typename T>
