@@ -291,8 +291,8 @@ static __device__ __forceinline__ Share share_of(const FwdArgs &a, int x, int la
   return s;
 }
 // The share of a workgroup of the kernels of few rows.  It says what the places are for: the first of a sequence's, or (the x-th range's workgroup, of place x) that there is none.
-static __device__ __forceinline__ Share my_share(const FwdArgs &a, int lane) {
-  const int x = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
+static __device__ __forceinline__ Share my_share(const FwdArgs &a, unsigned block, int lane) {
+  const int x = block / a.p.Hkv, hk = block % a.p.Hkv;
   const Share s = share_of(a, x, lane);
   if (threadIdx.x == 0 && a.wanted > 1) {
     int32_t *heads = a.heads + (int64_t)hk * a.wanted * 2;
@@ -411,18 +411,18 @@ static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &
 // A wave has 32 slots' keys and values in LDS, and asks for the next keys when it has read these, and for the next values likewise, so that one or the other is
 // always on its way; two workgroups to a CU (fp32, whose rows are split into pieces behind LDS: one).  Values are asked for past the caches, which leaves those to the keys, that
 // the slots' weights are formed from next: 394 MB of both 66 us for 77, up to 260 MB the same to within 1 us.
+template <int D, bool F32>
+static constexpr int few_bytes() { return 4 * 2 * Tile<D * (F32 ? 4 : 2) / 2>::bytes(32); }      // [wave][k | v]; then [wave][register image]
 template <int D, bool F32, bool SMALL>
-__global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
+__device__ __forceinline__ void few_rows(const FwdArgs &a, unsigned block, char *lds, float (&stats)[2][4][32]) {
   constexpr int ESZ = F32 ? 4 : 2, W = D * ESZ / 2, KS = D / 16, RB = D / 32, NS = F32 ? 3 : 1, PS = F32 ? 3 : 2;      // W: a row in twos of bytes; pieces of a value, of a weight
   typedef Tile<W> T;
   constexpr int TILE = T::bytes(32), REQUESTS = T::chunks(32);
-  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TILE];      // [wave][k | v]; then [wave][register image]
-  static_assert(image_bytes<D>() <= 4 * 2 * TILE, "the images fit the stages");
-  __shared__ float stats[2][4][32];
+  static_assert(image_bytes<D>() <= few_bytes<D, F32>(), "the images fit the stages");
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int hk = blockIdx.x % p.Hkv;
-  const Share share = my_share(a, lane);
+  const int hk = block % p.Hkv;
+  const Share share = my_share(a, block, lane);
   const int b = __builtin_amdgcn_readfirstlane(share.b), n_split = __builtin_amdgcn_readfirstlane(share.n), range = __builtin_amdgcn_readfirstlane(share.range);
   if (b < 0) return;
   const NewRows n(p, b);
@@ -537,6 +537,12 @@ __global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (the stages become the images)
   join_waves<D, F32>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
 }
+template <int D, bool F32, bool SMALL>
+__global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[few_bytes<D, F32>()];
+  __shared__ float stats[2][4][32];
+  few_rows<D, F32, SMALL>(a, blockIdx.x, lds, stats);
+}
 
 // ---- tiles of rows ---------------------------------------------------------------------------------------------------
 // The tiles of 128 rows of sequence b are those from here on, as many as it needs; with offsets on the device there are some between them that hold nothing.
@@ -602,15 +608,17 @@ __device__ __forceinline__ void store_partial(const FwdArgs &a, const f32x16 (&o
 // bf16: 32 slots to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next slots under the exponentials of its own,
 // then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work of one wave at the same time, and of two
 // with two workgroups to a CU.
+constexpr int kTileSlots = 4;
+template <int D>
+static constexpr int tile_bytes() { return kTileSlots * 2 * Tile<D>::bytes(32); }
 template <int D, bool SMALL>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
+__device__ __forceinline__ void tile_rows(const FwdArgs &a, unsigned block, char *lds) {
   typedef Tile<D> T;
-  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOTS = 4, AHEAD = 3, REQUESTS = 2 * T::chunks(32) / 4;
+  constexpr int KS = D / 16, RB = D / 32, TILE = T::bytes(32), SLOTS = kTileSlots, AHEAD = 3, REQUESTS = 2 * T::chunks(32) / 4;
   constexpr auto k_at = [](int step) { return step % SLOTS * 2 * TILE; };
   constexpr auto v_at = [](int step) { return step % SLOTS * 2 * TILE + TILE; };
-  __shared__ __attribute__((aligned(1024))) char lds[SLOTS * 2 * TILE];
-  static_assert(4 * store_bytes<D, false>() <= SLOTS * 2 * TILE, "the stores' staging areas fit");
-  const unsigned item = xcd_item(blockIdx.x, a.share);
+  static_assert(4 * store_bytes<D, false>() <= tile_bytes<D>(), "the stores' staging areas fit");
+  const unsigned item = xcd_item(block, a.share);
   if (item >= a.items) return;
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
@@ -772,6 +780,22 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
   });
 }
 
+template <int D, bool SMALL>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(FwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[tile_bytes<D>()];
+  tile_rows<D, SMALL>(a, blockIdx.x, lds);
+}
+// Chunks beside single tokens: both in one launch, the few rows in the places that tiles leave, and behind them (64-wide, 12 heads on 4, over 8192 slots: a batch of four prompts and
+// four tokens 57.6 us, with the few rows first 63.5, in launches of their own 68; one prompt of 512 beside 31 tokens over 4096, 128-wide, 32 on 8: 102, 140 and 150).
+template <int D, bool SMALL>
+__global__ __launch_bounds__(256, 2) void paged_both_kernel(FwdArgs few, FwdArgs tile) {
+  constexpr int FEW = few_bytes<D, false>(), TILE = tile_bytes<D>();
+  __shared__ __attribute__((aligned(1024))) char lds[FEW > TILE ? FEW : TILE];
+  __shared__ float stats[2][4][32];
+  if (blockIdx.x < 8 * tile.share) tile_rows<D, SMALL>(tile, blockIdx.x, lds);
+  else few_rows<D, false, SMALL>(few, blockIdx.x - 8 * tile.share, lds, stats);
+}
+
 // fp32: 32 slots to a step, in registers a step ahead and in one stage of LDS in three pieces.
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
@@ -898,11 +922,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
 
 // Joins the ranges of a row, at most 64: a wave to a row.  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
 template <int D, bool F32, int ROWS>
-__global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
+__device__ __forceinline__ void join_ranges(const FwdArgs &a, unsigned block) {
   constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, c4 = 4 * (lane % LPR);
-  const int blocks = ROWS == 32 ? a.line_blocks : ROWS / 4, line = __builtin_amdgcn_readfirstlane(blockIdx.x % blocks * 4 + (threadIdx.x >> 6)), group = blockIdx.x / blocks;
+  const int blocks = ROWS == 32 ? a.line_blocks : ROWS / 4, line = __builtin_amdgcn_readfirstlane(block % blocks * 4 + (threadIdx.x >> 6)), group = block / blocks;
   int b, hk, R, n_rows, n_split;
   int64_t at0;                // place of the row in the first range's sums; range i's: at0 + i ROWS
   if constexpr (ROWS == 32) {
@@ -959,6 +983,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs a) {
   const int64_t to = h * a.out.sh + token * a.out.sn + c4;
   if constexpr (F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out.p) + to) = o;
   else *reinterpret_cast<bf16x4 *>(reinterpret_cast<__bf16 *>(a.out.p) + to) = __builtin_convertvector(o, bf16x4);
+}
+
+// tile_blocks workgroups join those of tiles, the others those of few rows.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void paged_join_kernel(FwdArgs few, FwdArgs tile, unsigned tile_blocks) {
+  if (blockIdx.x < tile_blocks) join_ranges<D, F32, 128>(tile, blockIdx.x);
+  else join_ranges<D, F32, 32>(few, blockIdx.x - tile_blocks);
 }
 
 struct Sums {
@@ -1027,48 +1058,60 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
   return f;
 }
 
-template <int D, bool F32, int ROWS>
-hipError_t launch_join(const FwdArgs &a, int groups, hipStream_t st) {
-  paged_join_kernel<D, F32, ROWS><<<(unsigned)groups * (ROWS == 32 ? a.line_blocks : ROWS / 4), 256, 0, st>>>(a);
-  return hipGetLastError();
-}
 template <int D, bool F32>
-hipError_t launch_forward(FwdArgs a, const FwdPlan &f, char *ws, hipStream_t st) {
+hipError_t launch_forward(const FwdArgs &all, const FwdPlan &f, char *ws, hipStream_t st) {
   hipError_t e = hipSuccess;
-  auto sums = [&](const Sums &x) {
+  FwdArgs few = all, tile = all;
+  auto sums = [&](FwdArgs &a, const Sums &x) {
     a.po = reinterpret_cast<float *>(ws + x.po);
     a.pm = reinterpret_cast<float *>(ws + x.pm);
     a.pl = reinterpret_cast<float *>(ws + x.pl);
     a.heads = reinterpret_cast<int32_t *>(ws + x.heads);
   };
-  if (f.tile) {
-    sums(f.tile_sums);
-    a.n_split = f.n_split;
-    a.leave_few = f.few;
-    a.tiles = f.groups / a.p.Hkv;
-    a.items = (unsigned)f.groups * f.n_split;
-    a.share = xcd_share(a.items);
-    if constexpr (F32) paged_tile_f32_kernel<D><<<8 * a.share, 256, 0, st>>>(a);
-    else if (a.p.page == 16) paged_tile_kernel<D, true><<<8 * a.share, 256, 0, st>>>(a);
-    else paged_tile_kernel<D, false><<<8 * a.share, 256, 0, st>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (f.n_split > 1 && (e = launch_join<D, F32, 128>(a, f.groups, st)) != hipSuccess) return e;
-  }
+  const Paged &p = all.p;
+  unsigned few_blocks = 0, few_joins = 0, tile_joins = 0;
   if (f.few) {
-    sums(f.few_sums);
-    a.wanted = f.wanted;
-    a.split_from = split_from(F32);
-    a.line_blocks = (std::min(32, a.p.max_new * a.p.G) + 3) / 4;
-    a.map = f.map ? reinterpret_cast<int32_t *>(ws + f.off_map) : nullptr;
+    sums(few, f.few_sums);
+    few.wanted = f.wanted;
+    few.split_from = split_from(F32);
+    few.line_blocks = (std::min(32, p.max_new * p.G) + 3) / 4;
+    few.map = f.map ? reinterpret_cast<int32_t *>(ws + f.off_map) : nullptr;
+    few_blocks = (unsigned)(f.wanted + p.B) * p.Hkv;      // (ranges of all sequences: their shares rounded down, or one)
+    if (f.wanted > 1) few_joins = (unsigned)f.wanted * p.Hkv * few.line_blocks;
     if (f.map) {
-      paged_map_kernel<<<1, 1024, 0, st>>>(a);
+      paged_map_kernel<<<1, 1024, 0, st>>>(few);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    const unsigned n = (unsigned)(f.wanted + a.p.B) * a.p.Hkv;      // (ranges of all sequences: their shares rounded down, or one)
-    if (a.p.page == 16) paged_few_kernel<D, F32, true><<<n, 256, 0, st>>>(a);
-    else paged_few_kernel<D, F32, false><<<n, 256, 0, st>>>(a);
+  }
+  if (f.tile) {
+    sums(tile, f.tile_sums);
+    tile.n_split = f.n_split;
+    tile.tiles = f.groups / p.Hkv;
+    tile.leave_few = f.few;
+    tile.items = (unsigned)f.groups * f.n_split;
+    tile.share = xcd_share(tile.items);
+    if (f.n_split > 1) tile_joins = (unsigned)f.groups * 32;
+  }
+  if (!F32 && f.few && f.tile) {
+    if (p.page == 16) paged_both_kernel<D, true><<<8 * tile.share + few_blocks, 256, 0, st>>>(few, tile);
+    else paged_both_kernel<D, false><<<8 * tile.share + few_blocks, 256, 0, st>>>(few, tile);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (f.wanted > 1) e = launch_join<D, F32, 32>(a, f.wanted * a.p.Hkv, st);
+  } else {
+    if (f.tile) {
+      if constexpr (F32) paged_tile_f32_kernel<D><<<8 * tile.share, 256, 0, st>>>(tile);
+      else if (p.page == 16) paged_tile_kernel<D, true><<<8 * tile.share, 256, 0, st>>>(tile);
+      else paged_tile_kernel<D, false><<<8 * tile.share, 256, 0, st>>>(tile);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (f.few) {
+      if (p.page == 16) paged_few_kernel<D, F32, true><<<few_blocks, 256, 0, st>>>(few);
+      else paged_few_kernel<D, F32, false><<<few_blocks, 256, 0, st>>>(few);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (tile_joins + few_joins > 0) {
+    paged_join_kernel<D, F32><<<tile_joins + few_joins, 256, 0, st>>>(few, tile, tile_joins);
+    e = hipGetLastError();
   }
   return e;
 }
