@@ -19,7 +19,7 @@ struct WeightArgs {
   const float *lse, *weights;
   float *out;
   float scale_log2e;
-  int parts;                  // workgroups of a sequence and key head
+  int parts, few_parts;       // workgroups of a sequence and key head
   int few;                    // tile: sequences of 32 rows or fewer are another launch's
   int row_parts;              // tile: parts of the rows, whose sums are joined where there are several
   float *sums;                // [row_parts][B H_kv][slots]
@@ -63,15 +63,14 @@ static __device__ __forceinline__ float sum_rows(const f32x16 &sc, const float *
 }
 
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
+static constexpr int few_weight_bytes() { return F32 ? 16 : 4 * Tile<D>::bytes(32); }
+template <int D, bool F32>
+__device__ __forceinline__ void weights_of_few(const WeightArgs &a, unsigned block, char *lds, float *shift, int *see) {
   typedef Tile<D> T;
   constexpr int KS = D / 16, NS = F32 ? 3 : 1, ESZ = F32 ? 4 : 2;
-  __shared__ __attribute__((aligned(1024))) char lds[F32 ? 16 : 4 * T::bytes(32)];
-  __shared__ float shift[32];
-  __shared__ int see[32];
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int bh = blockIdx.x / a.parts, part = blockIdx.x % a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, capacity = p.capacity();
+  const int bh = block / a.few_parts, part = block % a.few_parts, b = bh / p.Hkv, hk = bh % p.Hkv, capacity = p.capacity();
   const NewRows n(p, b);
   const int held = p.held(b), n_rows = n.n * p.G;
   if (n_rows > 32) return;
@@ -94,7 +93,7 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
   char *mine = lds + w * T::bytes(32);
   const unsigned rows0 = F32 ? 0 : T::rows_base(mine, lane);
   const char *kbase = a.k.p + hk * a.k.sh * ESZ;
-  for (int slot0 = (part * 4 + w) * 32; slot0 < capacity; slot0 += a.parts * 128) {
+  for (int slot0 = (part * 4 + w) * 32; slot0 < capacity; slot0 += a.few_parts * 128) {
     const int slot = slot0 + r;
     float sum = 0.f;
     if (slot0 < held && n_rows > 0) {
@@ -139,15 +138,15 @@ __global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
 
 // Rows are asked for two steps of 32 ahead.  Where the slots make few workgroups the rows are cut into parts, whose sums a second kernel adds up.
 template <int D, bool F32>
-__global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a) {
+static constexpr int tile_weight_bytes() { return 2 * (F32 ? 3 : 1) * Tile<D>::bytes(32); }
+template <int D, bool F32>
+__device__ __forceinline__ void weights_of_tiles(const WeightArgs &a, unsigned block, char *lds_, float (&shift)[2][32], int (&see)[2][32]) {
   typedef Tile<D> T;
   constexpr int KS = D / 16, NS = F32 ? 3 : 1, ESZ = F32 ? 4 : 2, STAGE = T::bytes(32), PER = 32 * T::PIECES / 256;
-  __shared__ __attribute__((aligned(1024))) char lds[2][NS * STAGE];
-  __shared__ float shift[2][32];
-  __shared__ int see[2][32];
+  char *const lds[2] = {lds_, lds_ + NS * STAGE};
   const Paged &p = a.p;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-  const int row_part = blockIdx.x % a.row_parts, item = blockIdx.x / a.row_parts;
+  const int row_part = block % a.row_parts, item = block / a.row_parts;
   const int bh = item / a.parts, b = bh / p.Hkv, hk = bh % p.Hkv, first = (item % a.parts) * 128, slot0 = first + 32 * w, slot = slot0 + r, capacity = p.capacity();
   const NewRows n(p, b);
   const int held = p.held(b), n_rows = n.n * p.G, before = held - n.all;      // before: slots ahead of the first new token's
@@ -253,6 +252,30 @@ __global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a
     else add_weight(a, at, sum);
   }
 }
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void paged_weights_few_kernel(WeightArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[few_weight_bytes<D, F32>()];
+  __shared__ float shift[32];
+  __shared__ int see[32];
+  weights_of_few<D, F32>(a, blockIdx.x, lds, shift, see);
+}
+template <int D, bool F32>
+__global__ __launch_bounds__(256, 2) void paged_weights_tile_kernel(WeightArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[tile_weight_bytes<D, F32>()];
+  __shared__ float shift[2][32];
+  __shared__ int see[2][32];
+  weights_of_tiles<D, F32>(a, blockIdx.x, lds, shift, see);
+}
+// Chunks beside single tokens: both in one launch, the first `tile_blocks` workgroups for tiles.
+template <int D, bool F32>
+__global__ __launch_bounds__(256, 2) void paged_weights_both_kernel(WeightArgs a, unsigned tile_blocks) {
+  constexpr int FEW = few_weight_bytes<D, F32>(), TILE = tile_weight_bytes<D, F32>();
+  __shared__ __attribute__((aligned(1024))) char lds[FEW > TILE ? FEW : TILE];
+  __shared__ float shift[2][32];
+  __shared__ int see[2][32];
+  if (blockIdx.x < tile_blocks) weights_of_tiles<D, F32>(a, blockIdx.x, lds, shift, see);
+  else weights_of_few<D, F32>(a, blockIdx.x - tile_blocks, lds, shift[0], see[0]);
+}
 __global__ __launch_bounds__(256) void paged_weights_join_kernel(WeightArgs a) {
   const Paged &p = a.p;
   const int64_t capacity = p.capacity(), all = (int64_t)p.B * p.Hkv * capacity, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -277,6 +300,14 @@ WeightPlan weight_plan(const ha_paged_problem &p) {
   f.row_parts = f.tile && slots > 0 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / (groups * f.blocks), (rows + 31) / 32 / 4)) : 1;
   if (f.row_parts > 1) f.total = round256((size_t)f.row_parts * groups * slots * 4);
   return f;
+}
+
+template <int D, bool F32>
+hipError_t launch_weights(const WeightArgs &a, unsigned tile_blocks, unsigned few_blocks, hipStream_t st) {
+  if (tile_blocks && few_blocks) paged_weights_both_kernel<D, F32><<<tile_blocks + few_blocks, 256, 0, st>>>(a, tile_blocks);
+  else if (tile_blocks) paged_weights_tile_kernel<D, F32><<<tile_blocks, 256, 0, st>>>(a);
+  else paged_weights_few_kernel<D, F32><<<few_blocks, 256, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -311,25 +342,17 @@ extern "C" ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const 
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const bool f32 = p->dtype == HA_F32;
   hipError_t e;
-  if (f.tile) {
-    a.parts = f.blocks;
-    a.few = f.few;
-    a.row_parts = f.row_parts;
-    a.sums = static_cast<float *>(workspace);
-    const unsigned grid = (unsigned)(groups * f.blocks * f.row_parts);
-    if (p->d_head == 128) { if (f32) paged_weights_tile_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
-    else { if (f32) paged_weights_tile_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_tile_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
-    if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
-    if (f.row_parts > 1) {
-      paged_weights_join_kernel<<<(unsigned)((groups * slots + 255) / 256), 256, 0, stream>>>(a);
-      if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
-    }
-  }
-  if (f.few) {
-    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(f.blocks, 2048 / groups));
-    const unsigned grid = (unsigned)(groups * a.parts);
-    if (p->d_head == 128) { if (f32) paged_weights_few_kernel<128, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<128, false><<<grid, 256, 0, stream>>>(a); }
-    else { if (f32) paged_weights_few_kernel<64, true><<<grid, 256, 0, stream>>>(a); else paged_weights_few_kernel<64, false><<<grid, 256, 0, stream>>>(a); }
+  a.parts = f.blocks;
+  a.few = f.few;
+  a.row_parts = f.row_parts;
+  a.sums = static_cast<float *>(workspace);
+  a.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(f.blocks, 2048 / groups));
+  const unsigned tile_blocks = f.tile ? (unsigned)(groups * f.blocks * f.row_parts) : 0, few_blocks = f.few ? (unsigned)(groups * a.few_parts) : 0;
+  if (p->d_head == 128) e = f32 ? launch_weights<128, true>(a, tile_blocks, few_blocks, stream) : launch_weights<128, false>(a, tile_blocks, few_blocks, stream);
+  else e = f32 ? launch_weights<64, true>(a, tile_blocks, few_blocks, stream) : launch_weights<64, false>(a, tile_blocks, few_blocks, stream);
+  if (e != hipSuccess) return device_error(e);
+  if (f.row_parts > 1) {
+    paged_weights_join_kernel<<<(unsigned)((groups * slots + 255) / 256), 256, 0, stream>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return device_error(e);
   }
   return HA_OK;
