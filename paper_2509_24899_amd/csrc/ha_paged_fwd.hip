@@ -1003,14 +1003,14 @@ struct FwdPlan {
   size_t off_map, total;
 };
 
-// Ranges of the slots of `tiles` tiles: as many as take the least time by this reckoning.  A CU that has all workgroups it can hold takes a step of them all in the time 1, one with fewer
-// the share `alone` of it at least; a workgroup starts in the time of `start` steps; and joining takes that of 16 and of 0.007 for each workgroup (fp32, whose steps
-// take four times as long: 12 and 0.0025).  From times of 1 to 64 ranges of 25 batches (8 to 320 tiles of 64 to 1073 steps): what this chooses is within 5 % of the best of them in all.
-// 300 tiles of 512 steps, 128-wide: 358 us in five ranges, 476 in one; 256 of 1073: 606 in two, 988 in one; 12 fp32 ones of 256: 69 in 32, 131 in ten.
+// Ranges of the slots of `tiles` tiles: as many as take the least time by this reckoning, whose unit is a step of all the workgroups that a CU holds.  With fewer of them a CU takes
+// `alone` of it at least; a workgroup starts in `start`; joining takes `join` and `join_each` for every workgroup.  Fitted to times of 1 to 64 ranges of 99 batches (1 to
+// 384 tiles of 4 to 1876 steps): what this chooses takes 0.3 to 1.4 % longer than the best of them on the average of a type and width, and 15 % at most.  300 tiles of 512 steps,
+// 128-wide: 358 us in five ranges, 476 in one; 256 of 1073: 606 in two, 988 in one; six fp32 ones of 12: 17 in 12, 52 in one.
 int ranges_of_tiles(const ha_paged_problem &p, int64_t tiles, int64_t steps) {
   const bool f32 = p.dtype == HA_F32, wide = p.d_head == 128;
-  const int resident = !f32 && !wide ? 3 : 2;
-  const double alone = f32 ? 0.8 : wide ? 0.7 : 0.5, start = f32 ? 0. : wide ? 8. : 4., join = f32 ? 12. : 16., join_each = f32 ? 0.0025 : 0.007;
+  const int resident = wide ? 2 : 3;
+  const double alone = wide ? (f32 ? 0.9 : 0.85) : f32 ? 0.5 : 0.45, start = f32 || !wide ? 1. : 2., join = f32 ? 1.5 : wide ? 7. : 5.5, join_each = f32 ? (wide ? 0.005 : 0.008) : wide ? 0.04 : 0.02;
   int best = 1;
   double least = 0.;
   for (int n = 1; n <= 64 && n <= steps && (n == 1 || tiles * n <= 2048); ++n) {
