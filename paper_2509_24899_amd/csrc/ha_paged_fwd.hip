@@ -240,8 +240,9 @@ static __device__ __forceinline__ int few_steps(const Paged &p, int b) {
   const int held = p.held(b);
   return ((p.causal ? max(min(held, held - n.all + n.n), 0) : held) + 31) / 32;
 }
-// One token of 12 heads, d = 128: 500 slots uncut 9.1 us, in four ranges 10.0 with the join; 1000 slots 10.9 and 10.1; in fp32 250 slots 16.9 and 15.
-static inline int split_from(bool f32) { return f32 ? 8 : 32; }
+// One token of 12 heads, d = 128, uncut and cut: 512 slots 9.1 and 9.7 us, 640 10.1 and 9.7, 768 11.1 and 9.8, 1000 13.3 and 9.8 (d = 64: 640 8.0 and 8.6, 768 8.8 and 8.5); fp32: 192 slots 16.0
+// and 17.9, 256 16.1 and 15.1 (d = 64: 256 9.7 and 11.1, 384 12.1 and 11.2).
+static inline int split_from(bool f32, int D) { return !f32 ? 24 : D == 128 ? 8 : 12; }
 // Every sequence of as many steps is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
 // ones do not take longer.  Those with several have a place for each range's sums, `wanted` at most.
 static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted, int from) {
@@ -249,23 +250,32 @@ static __device__ __forceinline__ int ranges_of(int steps, double all, int wante
   // (the quotient of whole numbers below 2^42 is not rounded up to the next one)
   return max(1, min(min(64, steps / 4), (int)((double)wanted * steps / all)));
 }
-// What a lane adds to the sums of the lanes up to it.
-static __device__ __forceinline__ int sum_upto(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+// Sum over the lanes up to this one (all of a wave call it), by DPP moves within rows of 16 lanes and then of the last sum of a row to those behind it.
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ int dpp_add_rows(int x) { return (int)((unsigned)x + (unsigned)__builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)); }
+static __device__ __forceinline__ int sum_upto(int x) {
+  x = dpp_add_rows<0x111, 0xf>(x);      // lane - 1, - 2, - 4, - 8
+  x = dpp_add_rows<0x112, 0xf>(x);
+  x = dpp_add_rows<0x114, 0xf>(x);
+  x = dpp_add_rows<0x118, 0xf>(x);
+  x = dpp_add_rows<0x142, 0xa>(x);      // lanes 15 and 47 to the rows behind them
+  return dpp_add_rows<0x143, 0xc>(x);   // lane 31 to the upper half
 }
 struct Share {
   int b, n, range, place;     // sequence (-1: none), its ranges, this one, the place of its first range's sums
   int places;                 // of all sequences
 };
-// Range x of all.  Up to 64 sequences are a lane each; of more a kernel has written the sums.
+// Range x of all.  Where no sequence is cut, sequence x; otherwise up to 64 sequences are a lane each; of more a kernel has written the sums.
 static __device__ __forceinline__ Share share_of(const FwdArgs &a, int x, int lane) {
   const Paged &p = a.p;
   Share s{-1, 0, 0, 0, 0};
+  if (a.wanted == 1) {
+    if (x < p.B && few_steps(p, x) >= 0) {
+      s.b = x;
+      s.n = 1;
+    }
+    return s;
+  }
   if (a.map) {
     const int32_t *ranges = a.map, *places = a.map + p.B + 1;
     s.places = places[p.B];
@@ -277,17 +287,15 @@ static __device__ __forceinline__ Share share_of(const FwdArgs &a, int x, int la
     return s;
   }
   const int steps = lane < p.B ? few_steps(p, lane) : -1;
-  double all = max(steps, 0);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-  const int n = ranges_of(steps, all, a.wanted, a.split_from), places = n > 1 ? n : 0, upto_places = sum_upto(places, lane), upto = sum_upto(n, lane);
-  s.places = __shfl(upto_places, 63);
+  const unsigned all = (unsigned)__builtin_amdgcn_readlane(sum_upto(max(steps, 0)), 63);      // (64 sequences of 2^25 steps at most)
+  const int n = ranges_of(steps, all, a.wanted, a.split_from), places = n > 1 ? n : 0, upto_places = sum_upto(places), upto = sum_upto(n);
+  s.places = __builtin_amdgcn_readlane(upto_places, 63);
   const uint64_t found = __ballot(upto > x);
   if (!found) return s;
   s.b = __ffsll((long long)found) - 1;
-  s.n = __shfl(n, s.b);
-  s.place = __shfl(upto_places - places, s.b);
-  s.range = x - __shfl(upto - n, s.b);
+  s.n = __builtin_amdgcn_readlane(n, s.b);
+  s.place = __builtin_amdgcn_readlane(upto_places - places, s.b);
+  s.range = x - __builtin_amdgcn_readlane(upto - n, s.b);
   return s;
 }
 // The share of a workgroup of the kernels of few rows.  It says what the places are for: the first of a sequence's, or (the x-th range's workgroup, of place x) that there is none.
@@ -319,7 +327,7 @@ __global__ __launch_bounds__(1024) void paged_map_kernel(FwdArgs a) {
   for (int i = 0; i < 16; ++i) all += part[i];
   int before[2] = {0, 0};
   for (int b0 = 0; b0 < p.B; b0 += 1024) {
-    const int b = b0 + threadIdx.x, n = b < p.B ? ranges_of(few_steps(p, b), all, a.wanted, a.split_from) : 0, upto[2] = {sum_upto(n, lane), sum_upto(n > 1 ? n : 0, lane)};
+    const int b = b0 + threadIdx.x, n = b < p.B ? ranges_of(few_steps(p, b), all, a.wanted, a.split_from) : 0, upto[2] = {sum_upto(n), sum_upto(n > 1 ? n : 0)};
     __syncthreads();
     if (lane == 63) {
       sums[0][w] = upto[0];
@@ -1046,9 +1054,9 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
   };
   // (ranges of all sequences and key heads: two workgroups to a CU, of 128-wide fp32 heads one: 16 sequences of 4000 slots, 4 key heads, 54 us for 63 with two)
   const int resident_few = p.dtype == HA_F32 && p.d_head == 128 ? 256 : 512;
-  f.wanted = steps >= split_from(p.dtype == HA_F32) ? std::max(1, resident_few / p.H_kv) : 1;
+  f.wanted = steps >= split_from(p.dtype == HA_F32, p.d_head) ? std::max(1, resident_few / p.H_kv) : 1;
   if (f.few && f.wanted > 1) f.few_sums = take((size_t)f.wanted * p.H_kv, 32);
-  if ((f.map = f.few && p.B > 64)) {
+  if ((f.map = f.few && p.B > 64 && f.wanted > 1)) {
     f.off_map = at;
     at += round256((size_t)(p.B + 1) * 8);
   }
@@ -1075,7 +1083,7 @@ hipError_t launch_forward(const FwdArgs &all, const FwdPlan &f, char *ws, hipStr
   if (f.few) {
     sums(few, f.few_sums);
     few.wanted = f.wanted;
-    few.split_from = split_from(F32);
+    few.split_from = split_from(F32, D);
     few.line_blocks = (std::min(32, p.max_new * p.G) + 3) / 4;
     few.map = f.map ? reinterpret_cast<int32_t *>(ws + f.off_map) : nullptr;
     few_blocks = (unsigned)(f.wanted + p.B) * p.Hkv;      // (ranges of all sequences: their shares rounded down, or one)
