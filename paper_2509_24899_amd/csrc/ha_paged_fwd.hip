@@ -930,6 +930,24 @@ __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
   });
 }
 
+// Largest number and sum over a wave, in all lanes, as sum_upto goes.
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ float dpp_rows(float none, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <typename Join>
+static __device__ __forceinline__ float wave_join(float x, float none, Join join) {
+  x = join(x, dpp_rows<0x111, 0xf>(none, x));
+  x = join(x, dpp_rows<0x112, 0xf>(none, x));
+  x = join(x, dpp_rows<0x114, 0xf>(none, x));
+  x = join(x, dpp_rows<0x118, 0xf>(none, x));
+  x = join(x, dpp_rows<0x142, 0xa>(none, x));
+  x = join(x, dpp_rows<0x143, 0xc>(none, x));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+static __device__ __forceinline__ float wave_max(float x) { return wave_join(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
+static __device__ __forceinline__ float wave_sum(float x) { return wave_join(x, 0.f, [](float a, float b) { return a + b; }); }
+
 // Joins the ranges of a row, at most 64: a wave to a row (6.7 us for single tokens, 12 for a frame's 31 MB: three loads that wait for each other; four rows to a wave were no faster).  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
 template <int D, bool F32, int ROWS>
 __device__ __forceinline__ void join_ranges(const FwdArgs &a, unsigned block) {
@@ -953,27 +971,27 @@ __device__ __forceinline__ void join_ranges(const FwdArgs &a, unsigned block) {
     hk = tile.hk;
     R = tile.row0 + line;
     n_rows = tile.n_rows;
+    if (R >= n_rows) return;
     n_split = a.n_split;
     at0 = (int64_t)group * n_split * ROWS + line;
   }
-  if (R >= n_rows) return;
   const bool has = lane < n_split;
   const float mi = has ? a.pm[at0 + (int64_t)lane * ROWS] : -INFINITY, li = has ? a.pl[at0 + (int64_t)lane * ROWS] : 0.f;
-  float m = mi;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  const float f = mi == m ? 1.f : fast_exp2((mi - m) * a.scale_log2e);
-  float l = has ? li * f : 0.f;                                // (a range that saw nothing has 0, or the NaN that has to show)
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < n_split; i0 += 4 * AT_ONCE) {
-    f32x4 x[4];
+  f32x4 x[4];
+  auto request = [&](int i0) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int i = min(i0 + u * AT_ONCE + lane / LPR, n_split - 1);
       x[u] = *reinterpret_cast<const f32x4 *>(a.po + (at0 + (int64_t)i * ROWS) * D + c4);
     }
+  };
+  request(0);
+  if (ROWS == 32 && R >= n_rows) return;        // (what has been asked for is nobody's, but there)
+  const float m = wave_max(mi), f = mi == m ? 1.f : fast_exp2((mi - m) * a.scale_log2e);
+  const float l = wave_sum(has ? li * f : 0.f);                // (a range that saw nothing has 0, or the NaN that has to show)
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < n_split; i0 += 4 * AT_ONCE) {
+    if (i0 > 0) request(i0);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int i = i0 + u * AT_ONCE + lane / LPR;
