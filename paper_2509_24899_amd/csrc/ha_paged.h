@@ -40,6 +40,17 @@ static __device__ __forceinline__ int last_not_above(int B, int x, int lane, At 
   return lo;
 }
 
+// Sum over the lanes up to this one (all of a wave call it), by DPP moves within rows of 16 lanes and then of the last sum of a row to those behind it.
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ int dpp_add_rows(int x) { return (int)((unsigned)x + (unsigned)__builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)); }
+static __device__ __forceinline__ int sum_upto(int x) {
+  x = dpp_add_rows<0x111, 0xf>(x);      // lane - 1, - 2, - 4, - 8
+  x = dpp_add_rows<0x112, 0xf>(x);
+  x = dpp_add_rows<0x114, 0xf>(x);
+  x = dpp_add_rows<0x118, 0xf>(x);
+  x = dpp_add_rows<0x142, 0xa>(x);      // lanes 15 and 47 to the rows behind them
+  return dpp_add_rows<0x143, 0xc>(x);   // lane 31 to the upper half
+}
 // Three bf16 pieces of eight fp32 values.  The first is cut off, so that the largest finite values do not become infinite, the second is the rounding of what that leaves, and the
 // third holds the rest exactly: 8 + 8 + 8 bits.  Infinities and NaN have one piece (infinity less infinity is none).  No branches: a kernel that splits many
 // values is half as long as with those of split8_any (29 KB for 64), which counts where a launch is short.  Of the nine products of two splits the three that are left out

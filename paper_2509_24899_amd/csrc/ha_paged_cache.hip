@@ -108,12 +108,7 @@ static __device__ __forceinline__ unsigned known_bits(int pass) { return pass ==
 template <int THREADS>
 static __device__ __forceinline__ unsigned prefix_sum(unsigned n, unsigned *sums, unsigned &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  unsigned upto = n;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned y = __shfl_up(upto, d);
-    if (lane >= d) upto += y;
-  }
+  const unsigned upto = (unsigned)sum_upto((int)n);
   __syncthreads();
   if (lane == 63) sums[w] = upto;
   __syncthreads();

@@ -250,17 +250,6 @@ static __device__ __forceinline__ int ranges_of(int steps, double all, int wante
   // (the quotient of whole numbers below 2^42 is not rounded up to the next one)
   return max(1, min(min(64, steps / 4), (int)((double)wanted * steps / all)));
 }
-// Sum over the lanes up to this one (all of a wave call it), by DPP moves within rows of 16 lanes and then of the last sum of a row to those behind it.
-template <int CTRL, int ROWS>
-static __device__ __forceinline__ int dpp_add_rows(int x) { return (int)((unsigned)x + (unsigned)__builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)); }
-static __device__ __forceinline__ int sum_upto(int x) {
-  x = dpp_add_rows<0x111, 0xf>(x);      // lane - 1, - 2, - 4, - 8
-  x = dpp_add_rows<0x112, 0xf>(x);
-  x = dpp_add_rows<0x114, 0xf>(x);
-  x = dpp_add_rows<0x118, 0xf>(x);
-  x = dpp_add_rows<0x142, 0xa>(x);      // lanes 15 and 47 to the rows behind them
-  return dpp_add_rows<0x143, 0xc>(x);   // lane 31 to the upper half
-}
 struct Share {
   int b, n, range, place;     // sequence (-1: none), its ranges, this one, the place of its first range's sums
   int places;                 // of all sequences
