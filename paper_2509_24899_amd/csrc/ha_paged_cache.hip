@@ -220,7 +220,7 @@ __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
 }
 
 // Longer caches: 2048 slots to a workgroup, a launch for every step.  The counts of all slots of a sequence and key head meet in the workspace.  (Four sequences of up to 60000 slots, 4 heads:
-// 38 us in six launches; one workgroup to a sequence and head 129.)
+// 36 us in six launches; one workgroup to a sequence and head 129.)
 constexpr int kChunk = 2048;
 __global__ __launch_bounds__(256) void evict_clear_kernel(unsigned *hist, int n) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) hist[i] = 0;

@@ -937,7 +937,7 @@ static __device__ __forceinline__ float wave_join(float x, float none, Join join
 static __device__ __forceinline__ float wave_max(float x) { return wave_join(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
 static __device__ __forceinline__ float wave_sum(float x) { return wave_join(x, 0.f, [](float a, float b) { return a + b; }); }
 
-// Joins the ranges of a row, at most 64: a wave to a row (6.7 us for single tokens, 12 for a frame's 31 MB: three loads that wait for each other; four rows to a wave were no faster).  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
+// Joins the ranges of a row, at most 64: a wave to a row (6.1 us for single tokens, 10.7 for a frame's 31 MB: loads that wait for each other; four rows to a wave were no faster).  Lane i has range i's maximum and sum; D / 4 lanes take four columns each, ranges in turn.
 template <int D, bool F32, int ROWS>
 __device__ __forceinline__ void join_ranges(const FwdArgs &a, unsigned block) {
   constexpr int LPR = D / 4, AT_ONCE = 64 / LPR;
