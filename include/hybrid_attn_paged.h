@@ -24,7 +24,7 @@ typedef struct ha_paged_problem {
   int32_t B, H, H_kv;     /* H a multiple of H_kv */
   int32_t T;              /* rows of new tokens; 0 is allowed */
   int32_t d_head;         /* 64 or 128 */
-  int32_t dtype;          /* ha_dtype of all rows and pages.  HA_F32: as ha_sparse_problem.dtype says */
+  int32_t dtype;          /* ha_dtype of all rows and pages.  HA_F32: as ha_sparse_problem.dtype says, and an infinity counts as NaN */
   int32_t n_pages;        /* pages of the pools */
   int32_t page;           /* slots of a page: 16, 32, 64, 128 or 256 */
   int32_t max_pages;      /* columns of page_table: max_pages * page <= 2^30 */

@@ -240,9 +240,9 @@ static __device__ __forceinline__ int few_steps(const Paged &p, int b) {
   const int held = p.held(b);
   return ((p.causal ? max(min(held, held - n.all + n.n), 0) : held) + 31) / 32;
 }
-// One token of 12 heads, d = 128, uncut and cut: 512 slots 9.1 and 9.7 us, 640 10.1 and 9.7, 768 11.1 and 9.8, 1000 13.3 and 9.8 (d = 64: 640 8.0 and 8.6, 768 8.8 and 8.5); fp32: 192 slots 16.0
-// and 17.9, 256 16.1 and 15.1 (d = 64: 256 9.7 and 11.1, 384 12.1 and 11.2).
-static inline int split_from(bool f32, int D) { return !f32 ? 24 : D == 128 ? 8 : 12; }
+// One token of 12 heads, d = 128, uncut and cut: 512 slots 9.1 and 9.7 us, 640 10.1 and 9.7, 768 11.1 and 9.8, 1000 13.3 and 9.8 (d = 64: 640 8.0 and 8.6, 768 8.8 and 8.5); fp32: 192 slots 13.7
+// and 15.5, 256 13.9 and 13.4 (d = 64: 256 8.6 and 10, 384 10.8 and 10.2).
+static inline int split_from(bool f32, int D) { return !f32 ? 24 : D == 128 ? 9 : 12; }
 // Every sequence of as many steps is cut into as many ranges as is its share of `wanted`, rounded down, with four steps each and 64 ranges at most, and one at least: long ones among short
 // ones do not take longer.  Those with several have a place for each range's sums, `wanted` at most.
 static __device__ __forceinline__ int ranges_of(int steps, double all, int wanted, int from) {
@@ -406,7 +406,7 @@ static __device__ __forceinline__ void follow(const f32x16 &sc, float c, float &
 }
 
 // A wave has 32 slots' keys and values in LDS, and asks for the next keys when it has read these, and for the next values likewise, so that one or the other is
-// always on its way; two workgroups to a CU (fp32, whose rows are split into pieces behind LDS: one).  Values are asked for past the caches, which leaves those to the keys, that
+// always on its way; two workgroups to a CU (fp32, 128 wide, whose rows are split into pieces behind LDS: one).  Values are asked for past the caches, which leaves those to the keys, that
 // the slots' weights are formed from next: 394 MB of both 66 us for 77, up to 260 MB the same to within 1.5 us.  (Four tokens of 12 heads on 4 over up to 60000 128-wide slots: 61 us,
 // 6.0 TB/s.)
 template <int D, bool F32>
@@ -536,7 +536,7 @@ __device__ __forceinline__ void few_rows(const FwdArgs &a, unsigned block, char 
   join_waves<D, F32>(a, o, m, l, lds, stats, n_split > 1 ? hk * a.wanted + share.place + range : -1, row, w, lane);
 }
 template <int D, bool F32, bool SMALL>
-__global__ __launch_bounds__(256, F32 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
+__global__ __launch_bounds__(256, F32 && D == 128 ? 1 : 2) void paged_few_kernel(FwdArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[few_bytes<D, F32>()];
   __shared__ float stats[2][4][32];
   few_rows<D, F32, SMALL>(a, blockIdx.x, lds, stats);

@@ -108,3 +108,20 @@ def test_two_streams_at_once():
     got = [[ha.hybrid_attn_paged_forward(c["q"], c["k"], c["v"], **c["where"], stream=s)[0] for c, s in zip(cases, streams)] for _ in range(8)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 1, 40]])
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+def test_what_is_not_finite_stays_in_its_sequence(new, dtype, d, what):
+    c = cache(39, [300, 1500, 77], new, H=4, Hkv=2, d=d, dtype=dtype, page=32)
+    want = ha.hybrid_attn_paged_forward(c["q"], c["k"], c["v"], **c["where"], with_lse=True)
+    page = c["where"]["page_table"][1, 3].item()      # slots 96 .. 127 of the sequence in the middle
+    rows = slice(new[0], new[0] + new[1])
+    c["k"][page, 1, 5, 3] = what
+    c["v"][page, 0, 5, 3] = what
+    got = ha.hybrid_attn_paged_forward(c["q"], c["k"], c["v"], **c["where"], with_lse=True)
+    assert not torch.isfinite(got[0][rows, :2, 3]).any()          # the key head whose value it is
+    for a, b in zip(got, want):
+        a[rows] = b[rows]
+        assert torch.equal(a, b)
