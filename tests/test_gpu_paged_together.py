@@ -125,3 +125,8 @@ def test_what_is_not_finite_stays_in_its_sequence(new, dtype, d, what):
     for a, b in zip(got, want):
         a[rows] = b[rows]
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d,dtype,page", [(64, BF, 16), (128, BF, 64), (64, F32, 32)])
+def test_many_sequences_of_both_kinds_in_ranges(d, dtype, page):
+    check(cache(40, [1500, 40] + [90, 33] * 34 + [0, 2000], [33, 1] * 35 + [0, 3], H=2, Hkv=1, d=d, dtype=dtype, page=page))
