@@ -56,6 +56,7 @@ struct FwdArgs {
   View q, k, v, out;
   float *lse;
   int n_split, tiles;         // tile: ranges of the slots, tiles of a key head
+  int each;                   // tile: tiles of every sequence, or 0: as the offsets place them
   int leave_few;              // tile: sequences of 32 rows or fewer are another launch's
   int wanted, line_blocks;    // few: ranges that a key head's sequences are to be cut into, together; fours of rows that a sequence may have
   int split_from;             // few: steps of a sequence that is cut
@@ -543,8 +544,9 @@ __global__ __launch_bounds__(256, F32 && D == 128 ? 1 : 2) void paged_few_kernel
 }
 
 // ---- tiles of rows ---------------------------------------------------------------------------------------------------
-// The tiles of 128 rows of sequence b are those from here on, as many as it needs; with offsets on the device there are some between them that hold nothing.
-static __device__ __forceinline__ int first_tile(const Paged &p, int b) { return p.q_offset ? p.offset(b) * p.G / 128 + b : b * ((p.max_new * p.G + 127) / 128); }
+// The tiles of 128 rows of sequence b are those from here on, as many as it needs.  There are two ways to count them, of which the host takes the one of fewer tiles: as many for every
+// sequence as the longest may need, or by the offsets, T G / 128 + B of them; some hold nothing.
+static __device__ __forceinline__ int first_tile(const FwdArgs &a, int b) { return a.each ? b * a.each : a.p.offset(b) * a.p.G / 128 + b; }
 
 // Writes a 32-row tile held as C^T (the row is the lane's) times `f` through `stage` (this wave's own LDS) to the rows at to(r), those below `rows`.
 template <int D, bool F32, typename To>
@@ -580,9 +582,9 @@ struct TileOf {
     range = item % a.n_split;
     const int tile = item / a.n_split % a.tiles;
     hk = item / a.n_split / a.tiles;
-    b = last_not_above(p.B, tile, lane, [&](int s) { return first_tile(p, s); });
+    b = last_not_above(p.B, tile, lane, [&](int s) { return first_tile(a, s); });
     const NewRows n(p, b);
-    row0 = (tile - first_tile(p, b)) * 128;
+    row0 = (tile - first_tile(a, b)) * 128;
     n_rows = n.n * p.G;
     if (row0 < 0 || row0 >= n_rows || (a.leave_few && n_rows <= 32)) n_rows = 0;
   }
@@ -1014,7 +1016,7 @@ struct Sums {
 };
 struct FwdPlan {
   bool few, tile;             // which launches there are
-  int wanted, n_split, groups;      // few: see FwdArgs; tile: ranges, tiles of all key heads
+  int wanted, n_split, groups, each;      // few: see FwdArgs; tile: ranges, tiles of all key heads, of a sequence (see FwdArgs)
   Sums few_sums, tile_sums;
   bool map;                   // few: more than 64 sequences
   size_t off_map, total;
@@ -1067,9 +1069,11 @@ FwdPlan plan_forward(const ha_paged_problem &p) {
     f.off_map = at;
     at += round256((size_t)(p.B + 1) * 8);
   }
-  const int64_t full = p.B * ((p.max_new * G + 127) / 128) * p.H_kv, groups = p.q_offset ? (p.T * G / 128 + p.B) * p.H_kv : full;
+  // (rows of no sequence have no tiles: one chunk of 64 tokens in 8192 rows, 32 heads on 8: 43 MB of workspace for 4.4 GB with tiles for all rows)
+  const int64_t each = (p.max_new * G + 127) / 128, full = p.B * each * p.H_kv, placed = (p.T * G / 128 + p.B) * p.H_kv, groups = p.q_offset ? std::min(placed, full) : full;
+  f.each = groups == full ? (int)each : 0;
   f.groups = (int)groups;
-  f.n_split = f.tile ? ranges_of_tiles(p, std::min(groups, full), steps) : 1;
+  f.n_split = f.tile ? ranges_of_tiles(p, groups, steps) : 1;
   if (f.tile && f.n_split > 1) f.tile_sums = take((size_t)groups * f.n_split, 128);
   f.total = at;
   return f;
@@ -1103,6 +1107,7 @@ hipError_t launch_forward(const FwdArgs &all, const FwdPlan &f, char *ws, hipStr
   if (f.tile) {
     sums(tile, f.tile_sums);
     tile.n_split = f.n_split;
+    tile.each = f.each;
     tile.tiles = f.groups / p.Hkv;
     tile.leave_few = f.few;
     tile.items = (unsigned)f.groups * f.n_split;
