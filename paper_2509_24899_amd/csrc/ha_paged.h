@@ -51,6 +51,23 @@ static __device__ __forceinline__ int sum_upto(int x) {
   x = dpp_add_rows<0x142, 0xa>(x);      // lanes 15 and 47 to the rows behind them
   return dpp_add_rows<0x143, 0xc>(x);   // lane 31 to the upper half
 }
+// A sum of many positive terms, each a sum over a step of rows or slots, with what the roundings have left out: its error does not grow with their number.  (Of nearly equal terms the same part
+// is lost again and again: 32768 one behind the other are off by 2e-4, and the weights of 2^20 rows were.)
+struct LongSum {
+  float sum = 0.f, rest = 0.f;
+  __device__ __forceinline__ void add(float x) {
+    const float s = sum + x;
+    rest += x - (s - sum);
+    sum = s;
+  }
+  __device__ __forceinline__ void scale(float f) {
+    sum *= f;
+    rest *= f;
+  }
+  // (an infinity leaves no rest, but NaN)
+  __device__ __forceinline__ float value() const { return rest == rest ? sum + rest : sum; }
+};
+
 // Three bf16 pieces of eight fp32 values.  The first is cut off, so that the largest finite values do not become infinite, the second is the rounding of what that leaves, and the
 // third holds the rest exactly: 8 + 8 + 8 bits.  An infinity becomes NaN (infinity less infinity).  Five and a half instructions a value, which is what a kernel that splits many spends
 // its time on (ten, with tests for infinities and the second piece widened from another conversion: one token of 12 128-wide heads over 447 slots 19.2 us for 17.1).  Of the nine products of two splits the three

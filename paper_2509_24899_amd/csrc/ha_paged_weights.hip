@@ -152,7 +152,7 @@ __device__ __forceinline__ void weights_of_tiles(const WeightArgs &a, unsigned b
   const int held = p.held(b), n_rows = n.n * p.G, before = held - n.all;      // before: slots ahead of the first new token's
   if (a.few && n_rows <= 32) return;
   const int id = slot < held ? p.page_of(b, slot) : -1;
-  float sum = 0.f;
+  LongSum total;
   // steps of rows that see the workgroup's first slot, this part's
   const int steps = (n_rows + 31) / 32, step0 = first >= held ? steps : p.causal ? max(first - before, 0) * p.G / 32 : 0, count = max(steps - step0, 0);
   int R0 = 32 * (step0 + count * row_part / a.row_parts);
@@ -231,8 +231,8 @@ __device__ __forceinline__ void weights_of_tiles(const WeightArgs &a, unsigned b
       }
       // (a row that sees all of the wave's slots: so do those behind it)
       const int first_sees = p.causal ? min(held, before + R0 / p.G + 1) : held;
-      sum += slot0 + 32 <= first_sees && R0 + 32 <= n_rows ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
-                                                           : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g);
+      total.add(slot0 + 32 <= first_sees && R0 + 32 <= n_rows ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
+                                                              : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g));
       if (R0 + 32 < R_end) deposit(next, stage ^ 1);
       __syncthreads();
       R0 += 32;
@@ -243,9 +243,9 @@ __device__ __forceinline__ void weights_of_tiles(const WeightArgs &a, unsigned b
       step(odd, even, 1);
       if (R0 >= R_end) break;
     }
-    if (id < 0) sum = 0.f;
+    if (id < 0) total = LongSum{};
   }
-  sum = xhalf_sum(sum);
+  const float sum = xhalf_sum(total.value());
   if (g == 0 && slot < capacity) {
     const int64_t at = (int64_t)bh * capacity + slot;
     if (a.row_parts > 1) a.sums[(int64_t)row_part * p.B * p.Hkv * capacity + at] = sum;
