@@ -45,7 +45,7 @@ struct WeightRow {
 
 static __device__ __forceinline__ void add_weight(const WeightArgs &a, int64_t at, float sum) { a.out[at] = (a.weights ? a.weights[at] : 0.f) + sum; }
 
-// Sum over 32 rows of the weights of this lane's slot; shift and see of the rows in LDS.  ALL: every row sees the slot.
+// Sum over 32 rows of the weights of this lane's slot; shift and see of the rows in LDS.  ALL: every row sees the slot, and none that there is has a shift of - infinity.
 template <bool ALL>
 static __device__ __forceinline__ float sum_rows(const f32x16 &sc, const float *shift, const int *see, int slot, float c, int g) {
   float sum = 0.f;
@@ -89,7 +89,8 @@ __device__ __forceinline__ void weights_of_few(const WeightArgs &a, unsigned blo
     }
   }
   __syncthreads();
-  const int first_sees = p.causal ? min(held, held - n.all + 1) : held;
+  // (the logits of a row that does not count may be NaN)
+  const int first_sees = __any(r < n_rows && shift[r] == -INFINITY) ? 0 : p.causal ? min(held, held - n.all + 1) : held;
   char *mine = lds + w * T::bytes(32);
   const unsigned rows0 = F32 ? 0 : T::rows_base(mine, lane);
   const char *kbase = a.k.p + hk * a.k.sh * ESZ;
@@ -231,8 +232,8 @@ __device__ __forceinline__ void weights_of_tiles(const WeightArgs &a, unsigned b
       }
       // (a row that sees all of the wave's slots: so do those behind it)
       const int first_sees = p.causal ? min(held, before + R0 / p.G + 1) : held;
-      total.add(slot0 + 32 <= first_sees && R0 + 32 <= n_rows ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
-                                                              : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g));
+      total.add(slot0 + 32 <= first_sees && R0 + 32 <= n_rows && !__any(shift[stage][r] == -INFINITY) ? sum_rows<true>(sc, shift[stage], see[stage], slot, a.scale_log2e, g)
+                                                                                                  : sum_rows<false>(sc, shift[stage], see[stage], slot, a.scale_log2e, g));
       if (R0 + 32 < R_end) deposit(next, stage ^ 1);
       __syncthreads();
       R0 += 32;
