@@ -72,7 +72,7 @@ ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const ha_view *q,
  * `keep` slots keeps all.  What stays is copied, in its order, to slots 0, 1, .. of the pages out_table[b] (device int32 [B, out_pages],
  * out_pages * page >= keep) of the same pools; rows there behind the last one are left as they were.  No page of out_table is one that a sequence of
  * page_table reads, and none stands in it twice; numbers outside 0 .. n_pages - 1 there store nothing, and a slot that is not there is copied as zeros.
- *   len_out      device int32 [B]: slots that stay
+ *   len_out      device int32 [B]: slots that stay; not key_len itself
  *   weights_out  device fp32 [B, H_kv, max_pages page]: the weights of what stays, zeros behind them; not weights itself
  *   kept         device int32 [B, H_kv, keep]: the slots that stay, rising, -1 behind the last
  * T, max_new, causal, softmax_scale, q_offset and H of the problem are checked but not used.  keep >= 1, keep_first, keep_last >= 0, keep_first + keep_last <= keep.

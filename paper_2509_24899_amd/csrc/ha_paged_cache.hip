@@ -389,6 +389,12 @@ hipError_t launch_append(const AppendArgs &a, bool next, bool norm, hipStream_t 
   return each == 4 ? launch_append<D, F32, 4>(a, grid, next, norm, st) : launch_append<D, F32, 1>(a, grid, next, norm, st);
 }
 
+// Whether two lists of n numbers of 32 bits share memory.
+bool overlap(const void *a, const void *b, int64_t n) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return (x > y ? x - y : y - x) < (uintptr_t)n * 4;
+}
+
 // One workgroup chooses of 8192 slots at most; more are counted by many, in seven launches.
 struct EvictPlan {
   int chunks;                 // 0: one workgroup
@@ -477,10 +483,11 @@ extern "C" ha_status hybrid_attn_paged_evict(const ha_paged_problem *p, int32_t 
   if (keep > (1 << 30) || (int64_t)p->B * p->H_kv * row_blocks > (1 << 23)) return HA_ERR_UNSUPPORTED;
   if ((st = check_pool(*p, k_pages, true, a.k)) != HA_OK || (st = check_pool(*p, v_pages, true, a.v)) != HA_OK) return st;
   if (!out_table || !len_out || !kept || (slots > 0 && (!weights || !weights_out))) return HA_ERR_NULL;
-  if (slots > 0 && weights_out == weights) return HA_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(len_out) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(weights) |
        reinterpret_cast<uintptr_t>(weights_out)) & 3u)
     return HA_ERR_ALIGN;
+  // (the choice and the copy read lengths and weights after the first of them has been written)
+  if (overlap(len_out, p->key_len, p->B) || overlap(weights_out, weights, (int64_t)p->B * p->H_kv * slots)) return HA_ERR_SHAPE;
   const EvictPlan f = evict_plan(*p);
   if ((st = check_workspace(workspace, workspace_bytes, f.total)) != HA_OK) return st;
   a.p = paged_of(*p);
