@@ -589,7 +589,7 @@ struct TileOf {
     const NewRows n(p, b);
     row0 = (tile - first_tile(a, b)) * 128;
     n_rows = n.n * p.G;
-    if (row0 < 0 || row0 >= n_rows || (a.leave_few && n_rows <= 32)) n_rows = 0;
+    if (row0 < 0 || row0 >= n_rows || (a.leave_few && n_rows <= 32)) row0 = n_rows = 0;      // (a row of such a tile is never below n_rows; ahead of the first sequence row0 was negative)
   }
 };
 
