@@ -53,16 +53,18 @@ ha_status hybrid_attn_paged_append(const ha_paged_problem *p, const ha_rotary *r
 /* Enqueues softmax attention of the new tokens over their sequences: out = sum_j p_j v_j, p_j = exp(scale q . k_j - lse), j over the slots that the token sees.  A token
  * that sees none has out = 0 and lse = -infinity.  lse: device fp32 [T, H], or NULL.  What the pools hold in slots that no token of a sequence sees is never used; a NaN or
  * infinity in a slot that some token of a tile of neighbouring ones sees may reach all of that tile.  Logits beyond 2^28 in magnitude may give infinities or NaN, and so may
- * values whose sum, with weights of 2^8 at most, leaves fp32's range before it is divided.  workspace: device, 256-byte aligned,
+ * values whose sum, with weights of 2^8 at most, leaves fp32's range before it is divided.
+ * Sums are fp32.  That of the weights keeps what its roundings leave out, so that lse does not lose with the number of slots; those of the values are the matrix cores', like any fp32 product's:
+ * with values of one sign under nearly equal weights a result is off by some 1e-9 of itself for every slot.  workspace: device, 256-byte aligned,
  * hybrid_attn_paged_workspace_bytes() bytes (0 is possible).  Results are the same bit for bit every time. */
 size_t hybrid_attn_paged_workspace_bytes(const ha_paged_problem *p);
 ha_status hybrid_attn_paged_forward(const ha_paged_problem *p, const ha_view *q, const ha_view *k_pages, const ha_view *v_pages, const ha_view *out, float *lse,
                                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Enqueues weights_out[b][h][j] = weights[b][h][j] + sum of exp(scale q . k_j - lse) over the new tokens of sequence b that see slot j and the query heads of key head h: what the
- * slot got in the attention that wrote lse (fp32 [T, H]).  Tokens whose lse is -infinity count as seeing nothing.  weights, weights_out: device fp32 [B, H_kv, max_pages page], contiguous;
+ * slot got in the attention that wrote lse (fp32 [T, H]).  Tokens whose lse is -infinity count as seeing nothing, whatever their queries hold.  weights, weights_out: device fp32 [B, H_kv, max_pages page], contiguous;
  * weights NULL: zeros; weights_out may be weights itself.  Slots that nothing sees (behind key_len, on pages that are not there) get what weights holds.
- * workspace as above, hybrid_attn_paged_weights_workspace_bytes() bytes.  Sums in fp32 in a fixed order. */
+ * workspace as above, hybrid_attn_paged_weights_workspace_bytes() bytes.  Sums in fp32 in a fixed order, with what roundings leave out of long ones. */
 size_t hybrid_attn_paged_weights_workspace_bytes(const ha_paged_problem *p);
 ha_status hybrid_attn_paged_weights(const ha_paged_problem *p, const ha_view *q, const ha_view *k_pages, const float *lse, const float *weights, float *weights_out,
                                     void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -395,7 +395,7 @@ bool overlap(const void *a, const void *b, int64_t n) {
   return (x > y ? x - y : y - x) < (uintptr_t)n * 4;
 }
 
-// One workgroup chooses of 8192 slots at most; more are counted by many, in seven launches.
+// One workgroup chooses of 8192 slots at most; more are counted by many, in six launches.
 struct EvictPlan {
   int chunks;                 // 0: one workgroup
   size_t off_counts, off_last, total;

@@ -89,7 +89,6 @@ struct Step {
 // one of that page is 32 rows further.  There is one scalar unit for all waves of a CU, so that what a step does here is kept short.
 template <int ESZ, int D, bool SMALL>
 struct Cursor {
-  static constexpr int ROWS = SMALL ? 16 : 32;
   const Paged &p;
   PageWalk walk;
   const View &kv, &vv;
@@ -610,7 +609,8 @@ __device__ __forceinline__ void store_partial(const FwdArgs &a, const f32x16 (&o
 
 // bf16: 32 slots to a step, four steps' keys and values in LDS, asked for three steps ahead.  A step forms the logits of the next slots under the exponentials of its own,
 // then O^T += V^T P^T over the maxima of the next ones, so that the matrix cores and the vector units of a SIMD have work of one wave at the same time, and of two
-// with two workgroups to a CU.  (1560 tokens of 12 128-wide heads over 34320 slots, 329 GFLOP: 380 us and more, by the clock: the matrix cores are busy 39 % of 1.9 GHz, a wave issues 45 % of its time.)
+// with two workgroups to a CU.  (1560 tokens of 12 128-wide heads over 34320 slots, 329 GFLOP: 808 thousand cycles, 368 us in a run of calls and up to 420 in short profiled ones, by the clock: the matrix cores are busy 39 % of them, a wave
+// issues 45 % of its time.)
 constexpr int kTileSlots = 4;
 template <int D>
 static constexpr int tile_bytes() { return kTileSlots * 2 * Tile<D>::bytes(32); }
@@ -808,7 +808,7 @@ __global__ __launch_bounds__(256, 2) void paged_both_kernel(FwdArgs few, FwdArgs
 }
 
 // fp32: 32 slots to a step, in registers a step ahead and in one stage of LDS in three pieces.  (A step of one workgroup takes 4.4 us, of two 6.9, 3.2 of them products: 24 heads on 8 of 2 x 512
-// 128-wide tokens over 4096 slots 324 us.)
+// 128-wide tokens over 4096 slots 294 us, joins 19.)
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_tile_f32_kernel(FwdArgs a) {
   constexpr bool F32 = true;

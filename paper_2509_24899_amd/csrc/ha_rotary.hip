@@ -61,7 +61,7 @@ struct Group {
   static constexpr int TPR = D / 8, ROWS = 256 / TPR;      // threads to a row, tokens to a workgroup
 };
 
-// U: heads whose rows are asked for at once.  Four where there are many tokens (12 + 12 heads of 2 x 75600 tokens: forward 341 us with four, 345 with one, gradients 541 and 564), one
+// U: heads whose rows are asked for at once.  Four where there are many tokens (12 + 12 heads of 2 x 75600 tokens: forward 341 us with four, 346 with one, gradients 506 and 502), one
 // where the launch is short and what counts is the code that has to be fetched (two heads of 1024 tokens: 3.5 us with one, 3.8 with four).
 template <int D, bool F32, bool NEXT, bool NORM, int U, bool ONCE>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
   }
 }
 
-// The gradient.  A workgroup walks groups of tokens and leaves its sums over rows of the weights' gradients, which a second kernel adds up.  (12 + 12 heads of 2 x 75600 tokens: 507 us
-// for three streams, 5.5 TB/s; the forward 342 us for two, 5.4.  Sums by atomics would be in another order every time.)
+// The gradient.  A workgroup walks groups of tokens and leaves its sums over rows of the weights' gradients, which a second kernel adds up.  (12 + 12 heads of 2 x 75600 tokens: 506 us
+// for three streams, 5.5 TB/s; the forward 341 us for two, 5.4.  Sums by atomics would be in another order every time.)
 template <int D, bool F32, bool NEXT, bool SUMS, int U, bool ONCE>
 __global__ __launch_bounds__(256) void rows_grad_kernel(RowsArgs a, unsigned all_groups) {
   typedef Group<D> G;
