@@ -218,7 +218,8 @@ def hybrid_attn_paged_evict(k_pages, v_pages, weights, page_table, key_len, keep
                             kept=None, workspace=None, stream=None):
     """Copy the `keep` slots of every sequence and key head that matter most to slots 0, 1, .. of the pages of out_table (int32 [B, out_pages]), in their order: the first
     keep_first, the last keep_last, and the others of the largest weights (fp32 [B, H_kv, max_pages page]), of equal ones the lower slot.  Returns (int32 [B] slots that
-    stay, their weights with zeros behind them, int32 [B, H_kv, keep] which slots stayed with -1 behind them).  Does not synchronise."""
+    stay, their weights with zeros behind them, int32 [B, H_kv, keep] which slots stayed with -1 behind them); len_out and weights_out may not lie on key_len and weights.
+    Does not synchronise."""
     native = _ha._ROWS or _ha._rows()
     if native and (done := native.paged_evict(k_pages, v_pages, weights, page_table, key_len, keep, out_table, keep_first, keep_last, len_out, weights_out, kept, workspace, stream)) is not None:
         return done
